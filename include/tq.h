@@ -519,6 +519,170 @@ tq_status tq_profile_events(void* scan_start, void* scan_stop);
 tq_status tq_search_kernel(int64_t nq, int64_t n, int d, int bits, int k,
                            int filtered, const char** name);
 
+/*
+ * Key-value cache in 8 bits, for the generator behind the index: the keys and
+ * values of the passages that a search returned, and of the tokens generated
+ * from them, kept as scalar codes with a scale for every 16 tokens and head.
+ * (The paper stops at retrieval; these calls have no passage there.)
+ *
+ * tq_kv_cache describes device memory that the caller owns; the calls read the
+ * struct during the call only.
+ *   k, v        codes [layers][pages][kv_heads][page_tokens][head_dim]
+ *   k_scale, v_scale  float32 [layers][pages][kv_heads][page_tokens / 16]:
+ *               value = code * scale of the token's block
+ *   table       [slots][max_pages] int32: page of tokens p*page_tokens ... of a
+ *               sequence; -1 where it holds none
+ *   lens        [slots] int32: tokens that a sequence holds
+ *   refs        [pages] int32: sequences that hold the page; 0: free
+ *   status      one int32 word, zero at the start; see tq_kv_check
+ *   codes       TQ_KV_INT8 (-127..127) or TQ_KV_E4M3 (8-bit floats up to 448)
+ * Limits: head_dim 64, 128 or 256; page_tokens a power of two in [16, 256];
+ * layers, kv_heads in [1, 1024]; slots in [1, 65536]; pages in [1, 2^31 - 2];
+ * max_pages >= 1 with max_pages * page_tokens < 2^31; k and v 16-byte aligned,
+ * the others 4-byte aligned.
+ *
+ * A sequence lives in a slot.  One decoding step is tq_kv_extend (room for the
+ * new tokens), then per layer tq_kv_append and tq_kv_attend, then, where some
+ * of them were drafts, tq_verify_drafts and tq_kv_truncate.  Slots, counts and
+ * lengths are device arrays, so a step needs no answer on the host.  Entries
+ * that cannot be carried out are recorded in the status word.
+ */
+enum { TQ_KV_INT8 = 0, TQ_KV_E4M3 = 1 };
+enum { TQ_BF16 = 0, TQ_FP16 = 1, TQ_FP32 = 2 };
+
+typedef struct tq_kv_cache {
+  uint8_t* k;
+  uint8_t* v;
+  float* k_scale;
+  float* v_scale;
+  int32_t* table;
+  int32_t* lens;
+  int32_t* refs;
+  int32_t* status;
+  int64_t pages, slots, max_pages;
+  int layers, kv_heads, head_dim, page_tokens, codes;
+} tq_kv_cache;
+
+/*
+ * tq_kv_append - writes the last tokens of n sequences into a layer's pages.
+ *   slots    device [n] int32, distinct
+ *   starts   device [n + 1] int32: sequence i brings tokens starts[i] ..
+ *            starts[i+1] - 1 of k and v; they are its last ones (lens already
+ *            counts them: tq_kv_extend)
+ *   k, v     device, `type` TQ_BF16, TQ_FP16 or TQ_FP32: element (token, head, j)
+ *            at token * token_stride + head * head_stride + j (strides in
+ *            elements, >= 0, any alignment of the elements' own size; 16-byte
+ *            aligned rows are read fastest)
+ *   total    tokens in all (starts[n]); 0 is a no-op
+ * For each block of 16 tokens, head, and of K and V: a = the largest finite |x|
+ * of the new tokens; scale = a / 127 (int8) or a / 448 (e4m3) in float32, or the
+ * block's present scale if it holds older tokens and that is larger; where the
+ * scale grows, the older tokens' codes are multiplied by (old / new) and
+ * rounded again; code = x / scale, rounded to nearest even.  Infinities take
+ * the largest code of their sign, NaN and everything at scale 0 takes 0: no
+ * code stands for a value that is not finite.
+ * Sequences whose slot, length or page is not valid are left out (status).
+ */
+tq_status tq_kv_append(const tq_kv_cache* cache, int layer, const int32_t* slots,
+                       const int32_t* starts, int64_t n, const void* k, const void* v,
+                       int type, int64_t total, int64_t k_token_stride,
+                       int64_t k_head_stride, int64_t v_token_stride,
+                       int64_t v_head_stride, void* stream);
+
+/*
+ * tq_kv_attend - causal attention of the last tokens of n sequences over the
+ * cache.
+ *   slots, starts, n, total  as for tq_kv_append: queries starts[i] ..
+ *            starts[i+1] - 1 stand at the last places of sequence i, the query
+ *            r of m at place p = lens - m + r
+ *   q        device, TQ_BF16 or TQ_FP16, [total][heads][head_dim] with strides in
+ *            elements; heads is a multiple of kv_heads, head h reads the keys
+ *            of head h / (heads / kv_heads)
+ *   scale    s_j = scale * (q . k_j)
+ *   window   0: a query sees tokens j <= p; w > 0: p - w < j <= p
+ *   out      device out [total][heads][head_dim], contiguous, q's type:
+ *            sum_j exp(s_j) v_j / sum_j exp(s_j)
+ *   lse      device out [total][heads] float32 (nullable): ln sum_j exp(s_j)
+ *   workspace  device, 16-byte aligned, of ws_bytes >= tq_kv_attend_workspace
+ * A query that sees no token (an empty sequence) gets zeros and -INFINITY.
+ * Products are taken in fp16 with exact codes and queries scaled by a power
+ * of two; scores, their statistics and the sums are float32.
+ */
+tq_status tq_kv_attend_workspace(const tq_kv_cache* cache, int64_t n, int64_t total,
+                                 int heads, size_t* bytes);
+tq_status tq_kv_attend(const tq_kv_cache* cache, int layer, const int32_t* slots,
+                       const int32_t* starts, int64_t n, const void* q, int type,
+                       int64_t total, int heads, int64_t q_token_stride,
+                       int64_t q_head_stride, float scale, int window, void* out,
+                       float* lse, void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * Pages.  Arrays of n entries are device int32; the slots an array names are
+ * distinct.
+ * tq_kv_fork      slot dst[i] gives up what it held and holds what src[i] holds,
+ *                 in the same pages.  dst and src have no slot in common; entries
+ *                 that break these rules, or name no slot, are left out (status).
+ * tq_kv_extend    room for counts[i] >= 0 more tokens in slots[i]: lens grows by
+ *                 counts[i]; a last page that is part full and held by other
+ *                 sequences too is first replaced by a copy of its used blocks
+ *                 (of every layer); free pages are taken lowest first, in the
+ *                 order of the entries.  All or nothing: with an entry that is
+ *                 not valid, a sequence beyond max_pages, or too few free pages
+ *                 nothing changes (status).
+ * tq_kv_truncate  slots[i] keeps its first lens[i] tokens (0: none); pages behind
+ *                 them are given up.  Entries longer than the sequence are left
+ *                 out (status).
+ * tq_kv_compact   with L pages in use, the i-th used page at or past L (in
+ *                 ascending order) moves to the i-th free one below L, in every
+ *                 layer, and the tables follow.  *used (device, nullable)
+ *                 receives L: the pool's end from page L on is free.
+ */
+tq_status tq_kv_fork(const tq_kv_cache* cache, const int32_t* dst, const int32_t* src,
+                     int64_t n, void* stream);
+tq_status tq_kv_extend_workspace(const tq_kv_cache* cache, int64_t n, size_t* bytes);
+tq_status tq_kv_extend(const tq_kv_cache* cache, const int32_t* slots,
+                       const int32_t* counts, int64_t n, void* workspace,
+                       size_t ws_bytes, void* stream);
+tq_status tq_kv_truncate(const tq_kv_cache* cache, const int32_t* slots,
+                         const int32_t* lens, int64_t n, void* stream);
+tq_status tq_kv_compact_workspace(const tq_kv_cache* cache, size_t* bytes);
+tq_status tq_kv_compact(const tq_kv_cache* cache, int32_t* used, void* workspace,
+                        size_t ws_bytes, void* stream);
+
+/*
+ * tq_kv_check - waits for `stream`, reads and clears the status word: TQ_ENOMEM
+ * if a tq_kv_extend since the last check found too few free pages, TQ_EINVAL if
+ * a call left entries out, TQ_ETIMEOUT if tq_kv_attend gave up on a bounded wait,
+ * else TQ_OK.
+ */
+tq_status tq_kv_check(const tq_kv_cache* cache, void* stream);
+
+/*
+ * tq_verify_drafts - accepts or rejects drafted tokens so that what is kept is
+ * distributed as the target model's own samples, from given random numbers.
+ *   target   device [n][t + 1][vocab], `type` TQ_FP32, TQ_BF16 or TQ_FP16: the target
+ *            model's probabilities at each drafted place and behind the last
+ *   draft    device [n][t][vocab] of the same type: the drafting model's
+ *            probabilities; NULL: drafts that were proposed with certainty
+ *            (probability 1 for the token, 0 for the others)
+ *   drafts   device [n][t] int32 tokens; draft_lens device [n] int32 in [0, t]
+ *            (nullable: t for all)
+ *   uniforms device [n][t] float32 in [0, 1)
+ *   noise    device [n][vocab] float32 > 0, exponentially distributed
+ *   tokens   device out [n][t + 1] int32; accepted device out [n] int32
+ * With p_i and q_i the two rows of place i: draft x_i is accepted if u_i q_i(x_i)
+ * < p_i(x_i) and those before it were.  Behind a accepted drafts comes argmax_v
+ * w(v) / noise(v) (float32; the lowest token of equals), w = max(p_a - q_a, 0) if
+ * draft a was rejected (p_a if that is 0 everywhere), p_a if none was; then -1.
+ * A draft outside [0, vocab) is rejected.  t in [0, 64], vocab in [1, 2^24].
+ */
+tq_status tq_verify_drafts_workspace(int64_t n, int64_t vocab, size_t* bytes);
+tq_status tq_verify_drafts(const void* target, const void* draft, int type,
+                           const int32_t* drafts, const int32_t* draft_lens,
+                           const float* uniforms, const float* noise, int64_t n, int t,
+                           int vocab, int32_t* tokens, int32_t* accepted,
+                           void* workspace, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -13,6 +13,17 @@ STATUS_NAMES = {0: "TQ_OK", 1: "TQ_EINVAL", 2: "TQ_ENOMEM", 3: "TQ_ECUDA", 4: "T
 MARGINALS = {"beta": 0, "gauss": 1}
 SCALE_MODES = {"norm": 0, "none": 1, "unbiased": 2}
 PATHS = {"auto": 0, "lut": 1, "mma": 2, "lut_fixed": 3, "lut_fold": 4}
+KV_CODES = {"int8": 0, "e4m3": 1}
+
+
+class KvCacheStruct(C.Structure):
+    """tq_kv_cache."""
+    _fields_ = ([(name, C.c_void_p) for name in ("k", "v", "k_scale", "v_scale", "table", "lens", "refs", "status")] +
+                [(name, C.c_int64) for name in ("pages", "slots", "max_pages")] +
+                [(name, C.c_int) for name in ("layers", "kv_heads", "head_dim", "page_tokens", "codes")])
+
+
+_KV = C.POINTER(KvCacheStruct)
 
 # name -> (restype, argtypes); every symbol include/tq.h declares
 SIGNATURES = {
@@ -76,6 +87,23 @@ SIGNATURES = {
     "tq_set_search_path": (C.c_int, [C.c_int]),
     "tq_search_kernel": (C.c_int, [C.c_int64, C.c_int64, C.c_int, C.c_int, C.c_int, C.c_int, C.POINTER(C.c_char_p)]),
     "tq_profile_events": (C.c_int, [C.c_void_p, C.c_void_p]),
+    "tq_kv_append": (C.c_int, [_KV, C.c_int, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int,
+                               C.c_int64, C.c_int64, C.c_int64, C.c_int64, C.c_int64, C.c_void_p]),
+    "tq_kv_attend_workspace": (C.c_int, [_KV, C.c_int64, C.c_int64, C.c_int, C.POINTER(C.c_size_t)]),
+    "tq_kv_attend": (C.c_int, [_KV, C.c_int, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int, C.c_int64,
+                               C.c_int, C.c_int64, C.c_int64, C.c_float, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p,
+                               C.c_size_t, C.c_void_p]),
+    "tq_kv_fork": (C.c_int, [_KV, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]),
+    "tq_kv_extend_workspace": (C.c_int, [_KV, C.c_int64, C.POINTER(C.c_size_t)]),
+    "tq_kv_extend": (C.c_int, [_KV, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "tq_kv_truncate": (C.c_int, [_KV, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]),
+    "tq_kv_compact_workspace": (C.c_int, [_KV, C.POINTER(C.c_size_t)]),
+    "tq_kv_compact": (C.c_int, [_KV, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "tq_kv_check": (C.c_int, [_KV, C.c_void_p]),
+    "tq_verify_drafts_workspace": (C.c_int, [C.c_int64, C.c_int64, C.POINTER(C.c_size_t)]),
+    "tq_verify_drafts": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                   C.c_int64, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t,
+                                   C.c_void_p]),
 }
 
 _lib = None

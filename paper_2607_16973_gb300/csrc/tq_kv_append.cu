@@ -1,0 +1,167 @@
+// tq_kv_append: new keys and values quantised into the cache's pages.
+//
+// A warp takes one block of 16 tokens of one head, of K or of V: it reads the
+// block's new elements once into registers, takes their largest magnitude,
+// settles the block's scale, brings the codes of older tokens of the block to
+// it where it grew, and writes the new codes.  Nothing is shared between
+// warps, so there is one launch and no scratch.
+//
+// Bound: HBM, 2 + 1 bytes per element (16-bit input); for single tokens
+// (a decoding step) the latency of the chain starts -> lens -> table -> codes.
+#include <algorithm>
+
+#include "tq_kv.cuh"
+
+namespace tq {
+namespace {
+
+constexpr int APPEND_WARPS = 8;
+
+template <typename T, int D, int CODES, bool VEC>
+__global__ __launch_bounds__(APPEND_WARPS * 32) void k_kv_append(KvView kv, int layer,
+                                                                 const int32_t* __restrict__ slots,
+                                                                 const int32_t* __restrict__ starts, int64_t n,
+                                                                 KvRows k, KvRows v, int64_t total, int64_t work) {
+  constexpr int E = 16 / sizeof(T);           // elements of a 16-byte chunk
+  constexpr int CHUNKS = kKvBlock * D / E / 32;  // chunks of the block per lane
+  const int lane = threadIdx.x & 31;
+  const int64_t w = (int64_t)blockIdx.x * APPEND_WARPS + (threadIdx.x >> 5);
+  if (w >= work) return;
+  const int head = (int)(w % kv.c.kv_heads);
+  const int64_t rest = w / kv.c.kv_heads;
+  const bool is_v = rest & 1;
+  const int64_t unit = rest >> 1;
+  // m tokens touch at most m / 16 + 2 blocks (rounded down), so units
+  // starts[i] / 16 + 2 i on are enough for sequence i, whatever its length
+  const int64_t i = warp_last_not_above(n, unit, [&](int64_t j) { return (int64_t)(starts[j] >> 4) + 2 * j; });
+  KvSeq q;
+  if (!kv_seq(kv, slots, starts, i, total, false, q)) {
+    if (lane == 0) kv_status(kv, kKvBadEntry);
+    return;
+  }
+  const int first = q.len - q.count;
+  const int64_t block = (first >> 4) + unit - ((int64_t)(starts[i] >> 4) + 2 * i);
+  const int64_t at = block * kKvBlock;
+  if (unit < (int64_t)(starts[i] >> 4) + 2 * i || at >= q.len || q.count == 0) return;
+  const int lo = max(first - (int)at, 0), hi = min(q.len - (int)at, kKvBlock);  // new tokens of the block
+  const int page = kv.c.table[q.slot * kv.c.max_pages + (at >> kv.page_shift)];
+  if (page < 0 || page >= kv.c.pages) {
+    if (lane == 0) kv_status(kv, kKvBadEntry);
+    return;
+  }
+  const int64_t inside = at & (kv.c.page_tokens - 1);
+  uint8_t* codes = (is_v ? kv.c.v : kv.c.k) + kv.codes_at(layer, page, head) + inside * D;
+  float* scale = (is_v ? kv.c.v_scale : kv.c.k_scale) + kv.scales_at(layer, page, head) + inside / kKvBlock;
+  const KvRows& src = is_v ? v : k;
+  const T* x = static_cast<const T*>(src.p) + (q.token + (at - first)) * src.token_stride + head * src.head_stride;
+
+  union Chunk {
+    uint4 u;
+    T e[E];
+  } r[CHUNKS];
+  float top = 0.0f;
+#pragma unroll
+  for (int c = 0; c < CHUNKS; ++c) {
+    const int e = (c * 32 + lane) * E, row = e / D, col = e % D;
+    r[c].u = make_uint4(0, 0, 0, 0);
+    if (row >= lo && row < hi) {
+      const T* p = x + row * src.token_stride + col;
+      if (VEC) {
+        r[c].u = __ldg(reinterpret_cast<const uint4*>(p));
+      } else {
+#pragma unroll
+        for (int j = 0; j < E; ++j) r[c].e[j] = p[j];
+      }
+    }
+  }
+#pragma unroll
+  for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+    for (int j = 0; j < E; ++j) {
+      const float a = fabsf(to_float(r[c].e[j]));
+      if (a < INFINITY) top = fmaxf(top, a);  // (not for NaN)
+    }
+#pragma unroll
+  for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+
+  float s = __fdiv_rn(top, kv_qmax<CODES>());
+  if (lo > 0) {
+    const float old = *scale;
+    if (s > old) {
+      const float ratio = __fdiv_rn(old, s);
+      uint32_t* words = reinterpret_cast<uint32_t*>(codes);
+      for (int e = lane; e < lo * D / 4; e += 32) {
+        const uint32_t u = words[e];
+        words[e] = kv_pack4<CODES>(kv_value<CODES>(u, 0) * ratio, kv_value<CODES>(u, 1) * ratio,
+                                   kv_value<CODES>(u, 2) * ratio, kv_value<CODES>(u, 3) * ratio);
+      }
+    } else {
+      s = old;
+    }
+  }
+  __syncwarp();
+  if (lane == 0) *scale = s;
+#pragma unroll
+  for (int c = 0; c < CHUNKS; ++c) {
+    const int e = (c * 32 + lane) * E, row = e / D;
+    if (row < lo || row >= hi) continue;
+    float y[E];
+#pragma unroll
+    for (int j = 0; j < E; ++j) {
+      const float a = to_float(r[c].e[j]);
+      y[j] = s > 0.0f && a == a ? __fdiv_rn(a, s) : 0.0f;
+      y[j] = fminf(fmaxf(y[j], -kv_qmax<CODES>()), kv_qmax<CODES>());
+    }
+    uint32_t out[E / 4];
+#pragma unroll
+    for (int j = 0; j < E / 4; ++j) out[j] = kv_pack4<CODES>(y[4 * j], y[4 * j + 1], y[4 * j + 2], y[4 * j + 3]);
+    if (E == 8)
+      *reinterpret_cast<uint2*>(codes + e) = make_uint2(out[0], out[E / 4 - 1]);
+    else
+      *reinterpret_cast<uint32_t*>(codes + e) = out[0];
+  }
+}
+
+template <typename T, int D, int CODES>
+cudaError_t append(const KvView& kv, int layer, const int32_t* slots, const int32_t* starts, int64_t n,
+                   const KvRows& k, const KvRows& v, int64_t total, cudaStream_t s) {
+  const int64_t units = total / kKvBlock + 2 * n;
+  const int64_t work = units * 2 * kv.c.kv_heads;
+  const unsigned grid = (unsigned)((work + APPEND_WARPS - 1) / APPEND_WARPS);
+  bool vec = true;
+  for (const KvRows* r : {&k, &v})
+    vec = vec && aligned16(r->p) && (r->token_stride * sizeof(T)) % 16 == 0 && (r->head_stride * sizeof(T)) % 16 == 0;
+  (vec ? k_kv_append<T, D, CODES, true> : k_kv_append<T, D, CODES, false>)<<<grid, APPEND_WARPS * 32, 0, s>>>(
+      kv, layer, slots, starts, n, k, v, total, work);
+  return cudaGetLastError();
+}
+
+template <typename T>
+cudaError_t append_for(const KvView& kv, int layer, const int32_t* slots, const int32_t* starts, int64_t n,
+                       const KvRows& k, const KvRows& v, int64_t total, cudaStream_t s) {
+  const bool i8 = kv.c.codes == TQ_KV_INT8;
+  switch (kv.c.head_dim) {
+    case 64:
+      return (i8 ? append<T, 64, TQ_KV_INT8> : append<T, 64, TQ_KV_E4M3>)(kv, layer, slots, starts, n, k, v, total, s);
+    case 128:
+      return (i8 ? append<T, 128, TQ_KV_INT8> : append<T, 128, TQ_KV_E4M3>)(kv, layer, slots, starts, n, k, v, total, s);
+    default:
+      return (i8 ? append<T, 256, TQ_KV_INT8> : append<T, 256, TQ_KV_E4M3>)(kv, layer, slots, starts, n, k, v, total, s);
+  }
+}
+
+}  // namespace
+
+cudaError_t launch_kv_append(const KvView& kv, int layer, const int32_t* slots, const int32_t* starts, int64_t n,
+                             const KvRows& k, const KvRows& v, int type, int64_t total, cudaStream_t s) {
+  switch (type) {
+    case TQ_BF16:
+      return append_for<__nv_bfloat16>(kv, layer, slots, starts, n, k, v, total, s);
+    case TQ_FP16:
+      return append_for<__half>(kv, layer, slots, starts, n, k, v, total, s);
+    default:
+      return append_for<float>(kv, layer, slots, starts, n, k, v, total, s);
+  }
+}
+
+}  // namespace tq

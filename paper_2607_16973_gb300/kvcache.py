@@ -1,0 +1,260 @@
+"""The 8-bit key-value cache of the generator behind the index, and the
+verification of its drafts: tq_kv_* and tq_verify_drafts of include/tq.h.
+
+A retrieved passage is prompted once, its keys and values stay in pages of
+8-bit codes (one scale for every 16 tokens and head), and each request that
+retrieves it forks those pages.  One decoding step of a batch is
+
+    cache.extend(slots, counts)                        # room for the new tokens
+    for layer in ...:
+        cache.append(layer, slots, starts, k, v)       # their keys and values
+        o = cache.attention(layer, slots, starts, q)   # causal, over all that is held
+    tokens, accepted = tq.verify_drafts(...)           # where some were drafts
+    cache.truncate(slots, lens)                        # rejected ones go
+
+with slots, counts and lengths on the device: nothing in it waits for the host,
+and the same calls can be captured into a CUDA graph.  `check()` reports what a
+call could not carry out.
+"""
+from __future__ import annotations
+
+import ctypes as C
+import math
+
+from . import _dev_ptr, _on_stream, _stream_handle, _torch, _used_on
+from ._lib import KV_CODES, KvCacheStruct, check, load
+
+BLOCK = 16  # tokens that share a scale
+
+
+def _types():
+    torch = _torch()
+    return {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+
+
+def _rows(t, name: str, heads: int, dim: int, types):
+    """Rows [tokens, heads, dim] with any strides but the last: (pointer, type,
+    token stride, head stride)."""
+    ptr = _dev_ptr(t, name, types, contiguous=False)
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim:
+        raise ValueError(f"{name} must be [tokens, {heads}, {dim}], got {tuple(t.shape)}")
+    if t.numel() and t.stride(2) != 1:
+        raise ValueError(f"{name}: the elements of a row must lie side by side")
+    return ptr, _types()[t.dtype], t.stride(0), t.stride(1)
+
+
+class KVCache:
+    """Keys and values of sequences in slots, as 8-bit codes in pages.
+
+    pages, slots, max_pages (pages of one slot's table), page_tokens (a power of
+    two from 16 to 256), layers, kv_heads, head_dim (64, 128 or 256); codes:
+    "int8" or "e4m3".  The tensors are attributes: k, v (uint8), k_scale,
+    v_scale, table, lens, refs, status; `from_tensors` makes a cache of given
+    ones.  Work on a cache belongs on one stream at a time, except that
+    attention only reads it."""
+
+    def __init__(self, pages: int, slots: int, max_pages: int, kv_heads: int, head_dim: int, page_tokens: int = 64,
+                 layers: int = 1, codes: str = "int8", device="cuda"):
+        torch = _torch()
+        if min(pages, slots, max_pages, kv_heads, head_dim, page_tokens // BLOCK, layers) < 1:
+            raise ValueError("pages, slots, max_pages, kv_heads, head_dim and layers must be positive, "
+                             "page_tokens at least 16")
+        shape = (layers, pages, kv_heads, page_tokens, head_dim)
+        scales = (layers, pages, kv_heads, page_tokens // BLOCK)
+        i32 = torch.int32
+        self._set(torch.zeros(shape, dtype=torch.uint8, device=device),
+                  torch.zeros(shape, dtype=torch.uint8, device=device), torch.zeros(scales, device=device),
+                  torch.zeros(scales, device=device), torch.full((slots, max_pages), -1, dtype=i32, device=device),
+                  torch.zeros(slots, dtype=i32, device=device), torch.zeros(pages, dtype=i32, device=device), codes)
+
+    @classmethod
+    def from_tensors(cls, k, v, k_scale, v_scale, table, lens, refs, codes: str = "int8") -> "KVCache":
+        """A cache of tensors that the caller keeps (not copied): k, v uint8
+        [layers, pages, kv_heads, page_tokens, head_dim], scales float32
+        [layers, pages, kv_heads, page_tokens / 16], table int32 [slots,
+        max_pages], lens int32 [slots], refs int32 [pages]."""
+        self = cls.__new__(cls)
+        self._set(k, v, k_scale, v_scale, table, lens, refs, codes)
+        return self
+
+    def _set(self, k, v, k_scale, v_scale, table, lens, refs, codes):
+        torch = _torch()
+        if codes not in KV_CODES:
+            raise ValueError(f"codes must be one of {sorted(KV_CODES)}, got {codes!r}")
+        if k.dim() != 5 or k.shape != v.shape:
+            raise ValueError("k and v must both be [layers, pages, kv_heads, page_tokens, head_dim]")
+        layers, pages, kv_heads, page_tokens, head_dim = k.shape
+        scales = (layers, pages, kv_heads, page_tokens // BLOCK)
+        if tuple(k_scale.shape) != scales or tuple(v_scale.shape) != scales:
+            raise ValueError(f"k_scale and v_scale must be {scales}")
+        if table.dim() != 2 or lens.shape != (table.shape[0],) or refs.shape != (pages,):
+            raise ValueError("table must be [slots, max_pages], lens [slots], refs [pages]")
+        u8, f32, i32 = torch.uint8, torch.float32, torch.int32
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.table, self.lens, self.refs, self.codes = table, lens, refs, codes
+        self.status = torch.zeros(1, dtype=i32, device=k.device)
+        self._c = KvCacheStruct(
+            _dev_ptr(k, "k", u8), _dev_ptr(v, "v", u8), _dev_ptr(k_scale, "k_scale", f32),
+            _dev_ptr(v_scale, "v_scale", f32), _dev_ptr(table, "table", i32), _dev_ptr(lens, "lens", i32),
+            _dev_ptr(refs, "refs", i32), _dev_ptr(self.status, "status"), pages, table.shape[0], table.shape[1],
+            layers, kv_heads, head_dim, page_tokens, KV_CODES[codes])
+
+    @property
+    def _handle(self):
+        return C.byref(self._c)
+
+    def _entries(self, a, b, names, stream, extra: int = 0):
+        """Two int32 arrays of as many entries (the second `extra` more)."""
+        i32 = _torch().int32
+        pa, pb = _dev_ptr(a, names[0], i32), _dev_ptr(b, names[1], i32)
+        if a.dim() != 1 or b.dim() != 1 or b.numel() != a.numel() + extra:
+            raise ValueError(f"{names[0]} must be [n] and {names[1]} [n{' + 1' if extra else ''}]")
+        for t in (a, b):
+            _used_on(t, stream)
+        return pa, pb, a.numel()
+
+    def _workspace(self, workspace, need: int, stream):
+        if workspace is None:
+            with _on_stream(stream):
+                workspace = _torch().empty(max(need, 16), dtype=_torch().uint8, device=self.k.device)
+        return workspace, _dev_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size()
+
+    def append(self, layer: int, slots, starts, k, v, stream=None) -> None:
+        """tq_kv_append: the last tokens of the sequences in `slots` (int32 [n]),
+        sequence i's at starts[i] .. starts[i+1] - 1 (int32 [n + 1]) of k and v
+        ([tokens, kv_heads, head_dim], bfloat16, float16 or float32, any strides
+        but the last)."""
+        c = self._c
+        ps, pt, n = self._entries(slots, starts, ("slots", "starts"), stream, 1)
+        types = tuple(_types())
+        kp, kt, k0, k1 = _rows(k, "k", c.kv_heads, c.head_dim, types)
+        vp, vt, v0, v1 = _rows(v, "v", c.kv_heads, c.head_dim, types)
+        if kt != vt or k.shape != v.shape:
+            raise ValueError("k and v must have one type and shape")
+        for t in (k, v):
+            _used_on(t, stream)
+        check(load().tq_kv_append(self._handle, layer, ps, pt, n, kp, vp, kt, k.shape[0], k0, k1, v0, v1,
+                                  _stream_handle(stream)))
+
+    def attention_workspace(self, n: int, total: int, heads: int) -> int:
+        """tq_kv_attend_workspace: device bytes for `total` queries of n sequences."""
+        need = C.c_size_t()
+        check(load().tq_kv_attend_workspace(self._handle, n, total, heads, C.byref(need)))
+        return need.value
+
+    def attention(self, layer: int, slots, starts, q, scale: float | None = None, window: int = 0, out=None,
+                  lse=None, return_lse: bool = False, workspace=None, stream=None):
+        """tq_kv_attend: causal attention of the last tokens of the sequences over
+        the cache; q [tokens, heads, head_dim] bfloat16 or float16 (any strides but
+        the last), heads a multiple of kv_heads; scale 1 / sqrt(head_dim) by
+        default; window 0, or the tokens that a query sees.  Returns out
+        [tokens, heads, head_dim], or (out, lse float32 [tokens, heads]) with
+        `return_lse`."""
+        torch = _torch()
+        c = self._c
+        ps, pt, n = self._entries(slots, starts, ("slots", "starts"), stream, 1)
+        if q.dim() != 3:
+            raise ValueError(f"q must be [tokens, heads, {c.head_dim}]")
+        total, heads = q.shape[0], q.shape[1]
+        qp, qt, q0, q1 = _rows(q, "q", heads, c.head_dim, (torch.bfloat16, torch.float16))
+        _used_on(q, stream)
+        with _on_stream(stream):
+            if out is None:
+                out = torch.empty((total, heads, c.head_dim), dtype=q.dtype, device=q.device)
+            if lse is None and return_lse:
+                lse = torch.empty((total, heads), dtype=torch.float32, device=q.device)
+        if tuple(out.shape) != (total, heads, c.head_dim):
+            raise ValueError(f"out must be {(total, heads, c.head_dim)}")
+        if lse is not None and tuple(lse.shape) != (total, heads):
+            raise ValueError(f"lse must be {(total, heads)}")
+        need = self.attention_workspace(n, total, heads) if workspace is None else 0
+        workspace, wp, wb = self._workspace(workspace, need, stream)
+        check(load().tq_kv_attend(self._handle, layer, ps, pt, n, qp, qt, total, heads, q0, q1,
+                                  1.0 / math.sqrt(c.head_dim) if scale is None else scale, window,
+                                  _dev_ptr(out, "out", q.dtype), _dev_ptr(lse, "lse", torch.float32) or None, wp, wb,
+                                  _stream_handle(stream)))
+        return (out, lse) if return_lse else out
+
+    def fork(self, dst, src, stream=None) -> None:
+        """tq_kv_fork: slots dst hold what slots src hold, in the same pages."""
+        pd, ps, n = self._entries(dst, src, ("dst", "src"), stream)
+        check(load().tq_kv_fork(self._handle, pd, ps, n, _stream_handle(stream)))
+
+    def extend(self, slots, counts, workspace=None, stream=None) -> None:
+        """tq_kv_extend: room for counts[i] more tokens in slots[i]; a shared last
+        page that is part full is replaced by a copy."""
+        ps, pc, n = self._entries(slots, counts, ("slots", "counts"), stream)
+        need = C.c_size_t()
+        if workspace is None:
+            check(load().tq_kv_extend_workspace(self._handle, n, C.byref(need)))
+        workspace, wp, wb = self._workspace(workspace, need.value, stream)
+        check(load().tq_kv_extend(self._handle, ps, pc, n, wp, wb, _stream_handle(stream)))
+
+    def truncate(self, slots, lens, stream=None) -> None:
+        """tq_kv_truncate: slots[i] keeps its first lens[i] tokens (0: none)."""
+        ps, pl, n = self._entries(slots, lens, ("slots", "lens"), stream)
+        check(load().tq_kv_truncate(self._handle, ps, pl, n, _stream_handle(stream)))
+
+    def compact(self, workspace=None, stream=None):
+        """tq_kv_compact: moves the pages in use to the front of the pool; returns
+        how many there are (int32 [1] on the device)."""
+        torch = _torch()
+        need = C.c_size_t()
+        if workspace is None:
+            check(load().tq_kv_compact_workspace(self._handle, C.byref(need)))
+        workspace, wp, wb = self._workspace(workspace, need.value, stream)
+        with _on_stream(stream):
+            used = torch.empty(1, dtype=torch.int32, device=self.k.device)
+        check(load().tq_kv_compact(self._handle, _dev_ptr(used, "used"), wp, wb, _stream_handle(stream)))
+        return used
+
+    def check(self, stream=None) -> None:
+        """tq_kv_check: waits for the stream; raises TQError if a call since the
+        last check found too few free pages (TQ_ENOMEM) or left entries out
+        (TQ_EINVAL)."""
+        check(load().tq_kv_check(self._handle, _stream_handle(stream)))
+
+
+def verify_drafts(target_probs, drafts, uniforms, noise, draft_probs=None, draft_lens=None, tokens=None, accepted=None,
+                  workspace=None, stream=None):
+    """tq_verify_drafts: drafted tokens against the target's probabilities.
+
+    target_probs [n, t + 1, vocab] and draft_probs [n, t, vocab] (None: drafts
+    proposed with certainty, such as a retrieved passage's own words) float32,
+    bfloat16 or float16; drafts int32 [n, t]; draft_lens int32 [n] (None: t for
+    all); uniforms float32 [n, t] in [0, 1); noise float32 [n, vocab],
+    exponentially distributed.  Returns (tokens int32 [n, t + 1]: the accepted
+    drafts, the token drawn behind them, then -1; accepted int32 [n])."""
+    torch = _torch()
+    types = _types()
+    if target_probs.dim() != 3:
+        raise ValueError("target_probs must be [n, t + 1, vocab]")
+    n, t, vocab = target_probs.shape[0], target_probs.shape[1] - 1, target_probs.shape[2]
+    shapes = ((drafts, "drafts", (n, t)), (uniforms, "uniforms", (n, t)), (noise, "noise", (n, vocab)),
+              (draft_probs, "draft_probs", (n, t, vocab)), (draft_lens, "draft_lens", (n,)),
+              (tokens, "tokens", (n, t + 1)), (accepted, "accepted", (n,)))
+    for x, name, shape in shapes:
+        if x is not None and tuple(x.shape) != shape:
+            raise ValueError(f"{name} must be {shape}, got {tuple(x.shape)}")
+    tp = _dev_ptr(target_probs, "target_probs", tuple(types))
+    dp = _dev_ptr(draft_probs, "draft_probs", target_probs.dtype)
+    for x in (target_probs, draft_probs, drafts, draft_lens, uniforms, noise):
+        if x is not None:
+            _used_on(x, stream)
+    dev, i32, f32 = target_probs.device, torch.int32, torch.float32
+    need = C.c_size_t()
+    with _on_stream(stream):
+        if tokens is None:
+            tokens = torch.empty((n, t + 1), dtype=i32, device=dev)
+        if accepted is None:
+            accepted = torch.empty(n, dtype=i32, device=dev)
+        if workspace is None:
+            check(load().tq_verify_drafts_workspace(n, vocab, C.byref(need)))
+            workspace = torch.empty(max(need.value, 16), dtype=torch.uint8, device=dev)
+    check(load().tq_verify_drafts(
+        tp, dp or None, types[target_probs.dtype], _dev_ptr(drafts, "drafts", i32),
+        _dev_ptr(draft_lens, "draft_lens", i32) or None, _dev_ptr(uniforms, "uniforms", f32),
+        _dev_ptr(noise, "noise", f32), n, t, vocab, _dev_ptr(tokens, "tokens", i32),
+        _dev_ptr(accepted, "accepted", i32), _dev_ptr(workspace, "workspace"),
+        workspace.numel() * workspace.element_size(), _stream_handle(stream)))
+    return tokens, accepted
