@@ -1,105 +1,690 @@
 // tq_kv_attend: causal attention of the last tokens of each sequence over the
-// 8-bit cache.
+// 8-bit cache, in one pass over the codes.
 //
-// out = sum_j e^(s_j) v_j / sum_j e^(s_j), s_j = scale * q . k_j, with the running
-// maximum m and sum l of the softmax: one pass over the tokens a query sees.
-// A warp takes one query of one head; lane l holds D / 32 of its elements.
+//   out = sum_j e^(s_j) v_j / sum_j e^(s_j),   s_j = scale * q . k_j
+//
+// The queries that read one key head (its group of query heads, times the new
+// tokens) are the columns of two small products with a block of 16 tokens,
+//
+//   S^T [16 tokens x rows] = K [16 x D] Q^T,     O^T [D x rows] += V^T [D x 16] P^T
+//
+// with the codes as the A operands, converted in registers (exact in fp16),
+// so that a lane loads exactly the 16-byte pieces it needs, straight from HBM
+// to registers: no shared memory, no layout but the plain one.  The order of
+// the contraction index is free as long as both operands agree on it, which is
+// what makes plain 16-byte loads fit the fragments:
+//   K: lane (g, t) loads bytes 16t .. 16t+15 of tokens g and g + 8 (and the same
+//      64, 128, 192 further on); word s of a piece is contraction step s;
+//   V: lane (g, t) loads bytes 16g .. of tokens 2t, 2t+1, 2t+8, 2t+9; two byte
+//      permutes pair the tokens of one element.
+// The probabilities go from the layout of S^T to that of the B operand by
+// movmatrix.  Scales: a block of keys has one factor, applied to the scores; a
+// block of values has one, applied to the block's product, which is therefore
+// taken by itself and added in float32.
+//
+// The softmax keeps a reference m per row that only moves when a score passes
+// the one it was set to by LAZY: most blocks need no reduction over the warp.
+//
+// Work: (sequence, tile of rows, key head) items of 16-token blocks, laid end to
+// end and cut into equal runs, one for each block of threads, so that ragged
+// batches and single long sequences load every SM alike.  A run's ends are
+// written as partial sums (m, l, O) and joined, in a fixed order, by
+// k_kv_join.
+//
+// Bound: HBM, 2 (D + 1/4) bytes per token and key head.
 #include <algorithm>
 
 #include "tq_kv.cuh"
+#include "tq_topk.cuh"
 
 namespace tq {
 namespace {
 
-constexpr int ATTEND_WARPS = 8;
+constexpr int WARPS = 4;
+constexpr int THREADS = WARPS * 32;
+constexpr int CHUNK = 1024;      // sequences whose units are kept in shared memory at a time
+constexpr int MIN_UNITS = 4;     // blocks that are worth a block of threads
+// Weights are held as 2^(s - m) with the reference m LEAD below the largest score
+// that it was last set to, and moved again when a score passes that by LAZY:
+// they stay under 2^15, fp16's largest, and those down to 2^-24 of the largest
+// one keep all of fp16's bits.
+constexpr float LEAD = 10.0f, LAZY = 5.0f;
+constexpr float LN2 = 0.6931471805599453f, LOG2E = 1.4426950408889634f;
+
+struct AttendArgs {
+  KvView kv;
+  int layer;
+  const int32_t *slots, *starts;
+  int64_t n, total;
+  KvRows q;
+  int heads, group;
+  float scale;
+  int window;
+  void* out;
+  float* lse;
+  float* parts;   // [2 * grid][rows * (D + 2)]: partial O, m, l
+  struct Split* splits;  // [grid]
+};
+
+// The item that a run continues, left for k_kv_join by the first run that does.
+struct Split {
+  int first, last;      // runs that have a part of it; first = -1: none to join
+  int token, head;      // first token of its sequence, its key head
+  int64_t row0, rows;   // first row of its tile, rows of its sequence
+};
 
 template <typename T> __device__ __forceinline__ T from_float(float x);
 template <> __device__ __forceinline__ __half from_float<__half>(float x) { return __float2half_rn(x); }
 template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 
-template <typename T, int D, int CODES>
-__global__ __launch_bounds__(ATTEND_WARPS * 32) void k_kv_attend(KvView kv, int layer,
-                                                                 const int32_t* __restrict__ slots,
-                                                                 const int32_t* __restrict__ starts, int64_t n,
-                                                                 KvRows q, int64_t total, int heads, float scale,
-                                                                 int window, T* __restrict__ out,
-                                                                 float* __restrict__ lse) {
-  constexpr int E = D / 32;  // elements of a lane
-  const int lane = threadIdx.x & 31;
-  const int64_t w = (int64_t)blockIdx.x * ATTEND_WARPS + (threadIdx.x >> 5);
-  if (w >= total * heads) return;
-  const int64_t token = w / heads;
-  const int head = (int)(w % heads), kv_head = head / (heads / kv.c.kv_heads);
-  const int64_t i = warp_last_not_above(n, token, [&](int64_t j) { return (int64_t)starts[j]; });
-  KvSeq seq;
-  const bool ok = kv_seq(kv, slots, starts, i, total, true, seq);
-  if (!ok && lane == 0) kv_status(kv, kKvBadEntry);
-  const int place = ok ? seq.len - seq.count + (int)(token - seq.token) : -1;
-  const T* x = static_cast<const T*>(q.p) + token * q.token_stride + head * q.head_stride + lane * E;
-  float qv[E], o[E], m = -INFINITY, l = 0.0f;
-#pragma unroll
-  for (int e = 0; e < E; ++e) {
-    qv[e] = to_float(x[e]) * scale;
-    o[e] = 0.0f;
-  }
-  for (int t = window ? max(0, place - window + 1) : 0; t <= place; ++t) {
-    const int page = kv.c.table[seq.slot * kv.c.max_pages + (t >> kv.page_shift)];
-    if (page < 0 || page >= kv.c.pages) {
-      if (lane == 0) kv_status(kv, kKvBadEntry);
-      break;
-    }
-    const int inside = t & (kv.c.page_tokens - 1);
-    const int64_t at = kv.codes_at(layer, page, kv_head) + (int64_t)inside * D + lane * E;
-    const int64_t sat = kv.scales_at(layer, page, kv_head) + inside / kKvBlock;
-    float s = 0.0f;
-#pragma unroll
-    for (int e = 0; e < E; ++e) s += qv[e] * kv_value<CODES>(kv.c.k[at + e], 0);
-#pragma unroll
-    for (int b = 16; b; b >>= 1) s += __shfl_xor_sync(0xffffffffu, s, b);
-    s *= kv.c.k_scale[sat];
-    const float top = fmaxf(m, s), keep = expf(m - top), p = expf(s - top);
-    const float pv = p * kv.c.v_scale[sat];
-    l = l * keep + p;
-    m = top;
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = o[e] * keep + pv * kv_value<CODES>(kv.c.v[at + e], 0);
-  }
-  const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-  T* y = out + (token * heads + head) * D + lane * E;
-#pragma unroll
-  for (int e = 0; e < E; ++e) y[e] = from_float<T>(o[e] * inv);
-  if (lse && lane == 0) lse[token * heads + head] = l > 0.0f ? m + logf(l) : -INFINITY;
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
 }
 
-template <typename T, int D>
-cudaError_t attend(const KvView& kv, int layer, const int32_t* slots, const int32_t* starts, int64_t n,
-                   const KvRows& q, int64_t total, int heads, float scale, int window, void* out, float* lse,
-                   cudaStream_t s) {
-  const unsigned grid = (unsigned)((total * heads + ATTEND_WARPS - 1) / ATTEND_WARPS);
-  (kv.c.codes == TQ_KV_INT8 ? k_kv_attend<T, D, TQ_KV_INT8> : k_kv_attend<T, D, TQ_KV_E4M3>)<<<grid, ATTEND_WARPS * 32, 0, s>>>(
-      kv, layer, slots, starts, n, q, total, heads, scale, window, static_cast<T*>(out), lse);
-  return cudaGetLastError();
+// What a sequence brings: its rows, and the blocks that any of them sees.
+struct SeqWork {
+  KvSeq s;
+  int64_t tiles;
+  int first_block, blocks;  // blocks >= 1, so that a row that sees nothing is written too
+  bool ok;
+};
+
+template <int ROWS>
+__device__ __forceinline__ SeqWork seq_work(const AttendArgs& a, int64_t i) {
+  SeqWork w;
+  w.ok = kv_seq(a.kv, a.slots, a.starts, i, a.total, true, w.s);
+  if (!w.ok) {
+    w.s.len = 0;
+    if (w.s.token < 0 || w.s.count < 0 || w.s.count > a.total || w.s.token > a.total - w.s.count) w.s.count = 0;
+  }
+  w.tiles = ((int64_t)w.s.count * a.group + ROWS - 1) / ROWS;
+  const int place = w.s.len - w.s.count;
+  const int lo = a.window ? max(0, place - a.window + 1) : 0;
+  w.first_block = lo / kKvBlock;
+  w.blocks = max(1, (w.s.len + kKvBlock - 1) / kKvBlock - w.first_block);
+  return w;
+}
+
+template <int ROWS>
+__device__ __forceinline__ int64_t seq_units(const AttendArgs& a, int64_t i) {
+  const SeqWork w = seq_work<ROWS>(a, i);
+  if (!w.ok && blockIdx.x == 0) kv_status(a.kv, kKvBadEntry);
+  return w.tiles * a.kv.c.kv_heads * w.blocks;
+}
+
+// The units of all sequences, found by a whole block: `before` holds the sums in
+// front of sequences base .. base + CHUNK.
+struct Units {
+  int64_t before[CHUNK + 1];
+  int64_t warp_sums[WARPS];
+  int64_t base, total;
+};
+
+template <int ROWS>
+__device__ void load_chunk(const AttendArgs& a, Units& u, int64_t base, int64_t sum) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  for (int j0 = 0; j0 < CHUNK; j0 += THREADS) {
+    const int64_t i = base + j0 + threadIdx.x;
+    if (base + j0 >= a.n && j0) break;
+    const int64_t mine = i < a.n ? seq_units<ROWS>(a, i) : 0;
+    int64_t run = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t y = __shfl_up_sync(FULL, run, o);
+      if (lane >= o) run += y;
+    }
+    if (lane == 31) u.warp_sums[warp] = run;
+    __syncthreads();
+    int64_t front = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) {
+      if (w < warp) front += u.warp_sums[w];
+      all += u.warp_sums[w];
+    }
+    u.before[j0 + threadIdx.x] = sum + front + run - mine;
+    if (threadIdx.x == THREADS - 1) u.before[j0 + THREADS] = sum + all;
+    sum += all;
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) {
+    u.base = base;
+    u.total = sum;
+  }
+  __syncthreads();
+}
+
+// Sets u up for the whole call (its total), the first chunk loaded last.
+template <int ROWS>
+__device__ int64_t load_units(const AttendArgs& a, Units& u) {
+  load_chunk<ROWS>(a, u, 0, 0);
+  if (a.n <= CHUNK) return u.total;
+  int64_t sum = u.total;
+  for (int64_t base = CHUNK; base < a.n; base += CHUNK) {
+    load_chunk<ROWS>(a, u, base, sum);
+    sum = u.total;
+  }
+  load_chunk<ROWS>(a, u, 0, 0);
+  return sum;
+}
+
+// The sequence that unit x falls into, and the sum in front of it; x does not go
+// back behind the chunk that is loaded.
+template <int ROWS>
+__device__ int64_t find_unit(const AttendArgs& a, Units& u, int64_t x, int64_t& before) {
+  while (x >= u.total) load_chunk<ROWS>(a, u, u.base + CHUNK, u.total);  // (uniform: x and u are the block's)
+  const int64_t count = min((int64_t)CHUNK, a.n - u.base);
+  const int64_t j = warp_last_not_above(count, x, [&](int64_t i) { return u.before[i]; });
+  before = u.before[j];
+  return u.base + j;
+}
+
+// Blocks of threads that share `units`, and the first unit of one of them.
+__device__ __forceinline__ int64_t runs(int64_t units, int64_t grid) {
+  return max((int64_t)1, min(grid, units / MIN_UNITS));
+}
+__device__ __forceinline__ int64_t run_start(int64_t c, int64_t units, int64_t n) { return c * units / n; }
+// The last run that starts at or in front of a unit, the first at or behind it.
+__device__ __forceinline__ int64_t last_run(int64_t unit, int64_t units, int64_t n) { return ((unit + 1) * n - 1) / units; }
+__device__ __forceinline__ int64_t first_run(int64_t unit, int64_t units, int64_t n) { return (unit * n + units - 1) / units; }
+
+// Where run c really starts: not within MIN_UNITS of an item's ends, but at that
+// end.  Items of less than 2 MIN_UNITS blocks are never cut, so that a short
+// sequence's result does not depend on the others of its batch.
+template <int ROWS>
+__device__ int64_t cut(const AttendArgs& a, Units& u, int64_t c, int64_t units, int64_t n) {
+  const int64_t x = run_start(c, units, n);
+  if (x >= units) return units;
+  int64_t before;
+  const int64_t i = find_unit<ROWS>(a, u, x, before);
+  const int64_t blocks = seq_work<ROWS>(a, i).blocks, in = (x - before) % blocks;
+  return in < MIN_UNITS ? x - in : blocks - in < MIN_UNITS ? x - in + blocks : x;
+}
+
+// Two pairs of fp16 values from the four codes of a word.  e4m3 codes come out
+// 2^-8 of their value: sign, exponent and mantissa are moved to their places in
+// fp16, whose exponents' bias is 8 larger; every code, the subnormal ones too,
+// is exact, and bytes that no token owns give finite values.
+template <int CODES>
+__device__ __forceinline__ void to_half4(uint32_t w, uint32_t& lo, uint32_t& hi) {
+  if (CODES == TQ_KV_INT8) {
+    const uint32_t u = w ^ 0x80808080u;  // code + 128
+    const __half2 bias = __halves2half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480));  // 1024 + 128
+    union { uint32_t r; __half2 h; } x;
+    x.r = __byte_perm(u, 0x64646464u, 0x4140);  // 1024 + byte
+    x.h = __hsub2(x.h, bias);
+    lo = x.r;
+    x.r = __byte_perm(u, 0x64646464u, 0x4342);
+    x.h = __hsub2(x.h, bias);
+    hi = x.r;
+  } else {
+    const uint32_t a = __byte_perm(w, 0, 0x1404), b = __byte_perm(w, 0, 0x3424);
+    lo = (a & 0x80008000u) | ((a >> 1) & 0x3F803F80u);
+    hi = (b & 0x80008000u) | ((b >> 1) & 0x3F803F80u);
+  }
+}
+template <int CODES>
+constexpr float code_unit() { return CODES == TQ_KV_INT8 ? 1.0f : 256.0f; }
+
+__device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                         uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+
+__device__ __forceinline__ uint32_t pack_half2(float a, float b) {
+  const __half2 h = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+template <int D>
+struct Piece {  // what a lane loads of a row: K pieces of 16 bytes, V pieces of 16 (8 at D = 64)
+  static constexpr int K = D / 64;
+  static constexpr int VW = D == 64 ? 2 : 4;      // words of a V piece
+  static constexpr int V = D == 256 ? 2 : 1;
+};
+
+template <typename T, int D, int CODES, int NT>
+__global__ __launch_bounds__(THREADS, D == 256 ? 2 : NT == 1 ? 4 : 3) void k_kv_attend(AttendArgs a) {
+  constexpr int ROWS = 8 * NT;
+  constexpr int KP = Piece<D>::K, VP = Piece<D>::V, VW = Piece<D>::VW;
+  constexpr int MT = D / 16;  // m-tiles of O^T
+  __shared__ Units units;
+  __shared__ float sh_o[WARPS][ROWS][D + 4];
+  __shared__ float sh_m[WARPS][ROWS], sh_l[WARPS][ROWS];
+
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+  const KvView& kv = a.kv;
+  const int kv_heads = kv.c.kv_heads;
+  griddep_launch_dependents();
+  const int64_t all = load_units<ROWS>(a, units);
+  const int64_t n_runs = runs(all, gridDim.x);
+  if (threadIdx.x == 0) a.splits[blockIdx.x].first = -1;
+  if (blockIdx.x >= n_runs) return;
+  int64_t u = cut<ROWS>(a, units, blockIdx.x, all, n_runs);
+  const int64_t chunk = units.base, chunk_sum = units.before[0];
+  const int64_t end = cut<ROWS>(a, units, blockIdx.x + 1, all, n_runs);
+  if (units.base != chunk) load_chunk<ROWS>(a, units, chunk, chunk_sum);  // (uniform)
+
+  while (u < end) {
+    int64_t before;
+    const int64_t i = find_unit<ROWS>(a, units, u, before);
+    const SeqWork w = seq_work<ROWS>(a, i);
+    const int64_t item = (u - before) / w.blocks;
+    const int b_first = (int)((u - before) % w.blocks);
+    const int b_last = (int)min((int64_t)w.blocks, b_first + (end - u));
+    u += b_last - b_first;
+    const int head = (int)(item % kv_heads);
+    const int64_t row0 = item / kv_heads * ROWS, rows = (int64_t)w.s.count * a.group;
+    if (b_first && threadIdx.x == 0) {
+      const int64_t begin = before + item * w.blocks;
+      const int first = (int)first_run(begin + MIN_UNITS, all, n_runs) - 1;
+      if (first + 1 == (int)blockIdx.x)
+        a.splits[blockIdx.x] = {first, (int)last_run(begin + w.blocks - MIN_UNITS, all, n_runs), w.s.token, head, row0, rows};
+    }
+
+    // the queries, scaled by a power of two to fp16's middle: row n = g of each 8
+    uint32_t qf[NT][KP * 4][2];
+    float unscale[NT][2];         // of rows 2t and 2t + 1: scores in log2 units
+    int place[NT][2];             // last token that they see; -1: none
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const int64_t row = row0 + nt * 8 + g;
+      const bool real = row < rows;
+      const int64_t token = w.s.token + row / a.group;
+      const T* p = static_cast<const T*>(a.q.p) + token * a.q.token_stride +
+                   (int64_t)(head * a.group + (int)(row % a.group)) * a.q.head_stride + 16 * t;
+      union { uint4 v[2]; T e[16]; } x[KP];
+      float top = 0.0f;
+#pragma unroll
+      for (int c = 0; c < KP; ++c) {
+        x[c].v[0] = x[c].v[1] = make_uint4(0, 0, 0, 0);
+        if (real) {
+          if (((uintptr_t)(p + 64 * c) & 15) == 0) {
+            x[c].v[0] = __ldg(reinterpret_cast<const uint4*>(p + 64 * c));
+            x[c].v[1] = __ldg(reinterpret_cast<const uint4*>(p + 64 * c) + 1);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) x[c].e[e] = p[64 * c + e];
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) top = fmaxf(top, fabsf(to_float(x[c].e[e])));
+      }
+      top = fmaxf(top, __shfl_xor_sync(FULL, top, 1));
+      top = fmaxf(top, __shfl_xor_sync(FULL, top, 2));
+      // the largest element to [2^8, 2^9): both factors are powers of two within float32's normal range
+      const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -110), 127);
+      const float up = __uint_as_float((uint32_t)(127 + min(8 - e, 118)) << 23);
+      const float down = a.scale * LOG2E * code_unit<CODES>() / up;
+#pragma unroll
+      for (int c = 0; c < KP; ++c)
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+            qf[nt][c * 4 + s][h] =
+                pack_half2(to_float(x[c].e[4 * s + 2 * h]) * up, to_float(x[c].e[4 * s + 2 * h + 1]) * up);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        unscale[nt][h] = __shfl_sync(FULL, down, (2 * t + h) * 4);
+        const int64_t r = row0 + nt * 8 + 2 * t + h;
+        place[nt][h] = r < rows ? w.s.len - w.s.count + (int)(r / a.group) : -1;
+      }
+    }
+    // the blocks of this run that some row of the tile sees
+    const int64_t last_row = min(rows, row0 + ROWS) - 1;
+    const int place_hi = w.s.len - w.s.count + (int)(last_row / a.group);
+    const int place_lo = w.s.len - w.s.count + (int)(row0 / a.group);
+    int blk = w.first_block + b_first, blk_end = w.first_block + b_last;
+    if (a.window) blk = max(blk, max(0, place_lo - a.window + 1) / kKvBlock);
+    blk_end = min(blk_end, place_hi < 0 ? 0 : place_hi / kKvBlock + 1);
+    // blocks that every row of the tile sees whole
+    const int whole_from = a.window ? max(0, place_hi - a.window + kKvBlock) / kKvBlock : 0;
+    const int whole_to = place_lo >= 0 ? (place_lo + 1) / kKvBlock : 0;
+
+    float o[NT][MT][4], m[NT][2], l[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+      for (int j = 0; j < MT; ++j) o[nt][j][0] = o[nt][j][1] = o[nt][j][2] = o[nt][j][3] = 0.0f;
+      m[nt][0] = m[nt][1] = -INFINITY;
+      l[nt][0] = l[nt][1] = 0.0f;
+    }
+
+    // This warp's blocks: blk + warp, + WARPS, ...; lane l looks up the page and the
+    // scales of the l-th of 32 of them.
+    const int32_t* table = kv.c.table + w.s.slot * kv.c.max_pages;
+    int64_t line = -1;      // first row (token) of lane's block in the pool, in units of 16 tokens
+    float ks = 0.0f, vs = 0.0f;
+    auto look_up = [&](int it) {
+      const int b = blk + warp + (it + lane) * WARPS;
+      line = -1;
+      if (b < blk_end) {
+        const int64_t tok = (int64_t)b * kKvBlock;
+        const int page = table[tok >> kv.page_shift];
+        if (page >= 0 && page < kv.c.pages) {
+          line = kv.scales_at(a.layer, page, head) + ((tok & (kv.c.page_tokens - 1)) / kKvBlock);
+          ks = __ldg(kv.c.k_scale + line);
+          vs = __ldg(kv.c.v_scale + line);
+        } else {
+          kv_status(kv, kKvBadEntry);
+        }
+      }
+    };
+    uint4 kr[KP][2];
+    uint32_t vr[VP][4][VW];
+    auto load_k = [&](int64_t ln) {
+      const uint8_t* p = kv.c.k + ln * (kKvBlock * D) + g * D + 16 * t;
+#pragma unroll
+      for (int c = 0; c < KP; ++c) {
+        kr[c][0] = __ldg(reinterpret_cast<const uint4*>(p + 64 * c));
+        kr[c][1] = __ldg(reinterpret_cast<const uint4*>(p + 64 * c + 8 * D));
+      }
+    };
+    auto load_v = [&](int64_t ln) {
+      const uint8_t* p = kv.c.v + ln * (kKvBlock * D) + 2 * t * D + (D == 64 ? 8 : 16) * g;
+#pragma unroll
+      for (int c = 0; c < VP; ++c)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const uint8_t* x = p + 128 * c + ((r & 1) + (r >> 1) * 8) * D;
+          if (VW == 2) {
+            const uint2 y = __ldg(reinterpret_cast<const uint2*>(x));
+            vr[c][r][0] = y.x, vr[c][r][1] = y.y;
+          } else {
+            const uint4 y = __ldg(reinterpret_cast<const uint4*>(x));
+            vr[c][r][0] = y.x, vr[c][r][1] = y.y, vr[c][r][VW - 2] = y.z, vr[c][r][VW - 1] = y.w;
+          }
+        }
+    };
+    const int steps = (blk_end - blk - warp + WARPS - 1) / WARPS;  // (<= 0: none)
+    int64_t now = -1;
+    if (steps > 0) {
+      look_up(0);
+      now = __shfl_sync(FULL, line, 0);
+      if (now >= 0) {
+        load_k(now);
+        load_v(now);
+      }
+    }
+    for (int it = 0; it < steps; ++it) {
+      const float k_scale = __shfl_sync(FULL, ks, it & 31), v_scale = __shfl_sync(FULL, vs, it & 31);
+      int64_t next = -1;
+      if (it + 1 < steps) {
+        if (((it + 1) & 31) == 0) look_up(it + 1);
+        next = __shfl_sync(FULL, line, (it + 1) & 31);
+      }
+      const int b = blk + warp + it * WARPS;
+      float s[NT][4];
+      if (now >= 0) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.0f;
+#pragma unroll
+        for (int c = 0; c < KP; ++c) {
+          const uint32_t x[4] = {kr[c][0].x, kr[c][0].y, kr[c][0].z, kr[c][0].w};
+          const uint32_t y[4] = {kr[c][1].x, kr[c][1].y, kr[c][1].z, kr[c][1].w};
+#pragma unroll
+          for (int st = 0; st < 4; ++st) {
+            uint32_t a0, a1, a2, a3;
+            to_half4<CODES>(x[st], a0, a2);
+            to_half4<CODES>(y[st], a1, a3);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) mma16816(s[nt], a0, a1, a2, a3, qf[nt][c * 4 + st][0], qf[nt][c * 4 + st][1]);
+          }
+        }
+      }
+      if (next >= 0) load_k(next);
+      if (now >= 0) {
+        bool rise = false;
+        const bool whole = b >= whole_from && b < whole_to;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const int h = x & 1;
+            float y = s[nt][x] * (k_scale * unscale[nt][h]);
+            if (!whole) {
+              const int tok = b * kKvBlock + g + (x >> 1) * 8;
+              if (tok > place[nt][h] || (a.window && tok <= place[nt][h] - a.window)) y = -INFINITY;
+            }
+            s[nt][x] = y;
+            rise |= y > m[nt][h] + (LEAD + LAZY);
+          }
+        if (__any_sync(FULL, rise)) {
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              float top = fmaxf(m[nt][h], fmaxf(s[nt][h], s[nt][2 + h]) - LEAD);
+              top = fmaxf(top, __shfl_xor_sync(FULL, top, 4));
+              top = fmaxf(top, __shfl_xor_sync(FULL, top, 8));
+              top = fmaxf(top, __shfl_xor_sync(FULL, top, 16));
+              const float keep = top > m[nt][h] ? ex2(m[nt][h] - top) : 1.0f;
+              m[nt][h] = top;
+              l[nt][h] *= keep;
+#pragma unroll
+              for (int j = 0; j < MT; ++j) {
+                o[nt][j][h] *= keep;
+                o[nt][j][2 + h] *= keep;
+              }
+            }
+        }
+        uint32_t pf[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          const float m0 = m[nt][0] == -INFINITY ? 0.0f : m[nt][0], m1 = m[nt][1] == -INFINITY ? 0.0f : m[nt][1];
+          const float p0 = ex2(s[nt][0] - m0), p1 = ex2(s[nt][1] - m1);
+          const float p2 = ex2(s[nt][2] - m0), p3 = ex2(s[nt][3] - m1);
+          l[nt][0] += p0 + p2;
+          l[nt][1] += p1 + p3;
+          pf[nt][0] = transpose8x8(pack_half2(p0, p1));
+          pf[nt][1] = transpose8x8(pack_half2(p2, p3));
+        }
+        const float vf = v_scale * code_unit<CODES>();
+#pragma unroll
+        for (int c = 0; c < VP; ++c)
+#pragma unroll
+          for (int x = 0; x < VW; ++x)
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {  // elements 0, 1 and 2, 3 of the word
+              const uint32_t sel = half ? 0x7362 : 0x5140;
+              uint32_t a0, a1, a2, a3;
+              to_half4<CODES>(__byte_perm(vr[c][0][x], vr[c][1][x], sel), a0, a1);
+              to_half4<CODES>(__byte_perm(vr[c][2][x], vr[c][3][x], sel), a2, a3);
+              const int j = (c * VW + x) * 2 + half;
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) {
+                float y[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                mma16816(y, a0, a1, a2, a3, pf[nt][0], pf[nt][1]);
+#pragma unroll
+                for (int z = 0; z < 4; ++z) o[nt][j][z] = fmaf(y[z], vf, o[nt][j][z]);
+              }
+            }
+      }
+      if (next >= 0) load_v(next);
+      now = next;
+    }
+
+    // the warps' sums to shared memory, as [row][element]
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float sum = l[nt][h];
+        sum += __shfl_xor_sync(FULL, sum, 4);
+        sum += __shfl_xor_sync(FULL, sum, 8);
+        sum += __shfl_xor_sync(FULL, sum, 16);
+        const int row = nt * 8 + 2 * t + h;
+        if (g == 0) {
+          sh_m[warp][row] = m[nt][h];
+          sh_l[warp][row] = sum;
+        }
+#pragma unroll
+        for (int j = 0; j < MT; ++j) {
+          constexpr int PER = VW * 2;  // m-tiles of a V piece, two elements each
+          const int d = j / PER * 128 + (D == 64 ? 8 : 16) * g + j % PER * 2;
+          *reinterpret_cast<float2*>(&sh_o[warp][row][d]) = make_float2(o[nt][j][h], o[nt][j][2 + h]);
+        }
+      }
+    __syncthreads();
+    // joined; whole items go to the output, the others to the partial sums
+    const bool is_whole = b_first == 0 && b_last == w.blocks;
+    float* part = a.parts + ((int64_t)blockIdx.x * 2 + (b_first == 0)) * (ROWS * (D + 2));
+    for (int row = threadIdx.x / 32; row < ROWS; row += WARPS) {
+      if (row0 + row >= rows) break;
+      float top = -INFINITY, sum = 0.0f, f[WARPS];
+#pragma unroll
+      for (int x = 0; x < WARPS; ++x) top = fmaxf(top, sh_m[x][row]);
+#pragma unroll
+      for (int x = 0; x < WARPS; ++x) {
+        f[x] = top == -INFINITY ? 0.0f : ex2(sh_m[x][row] - top);
+        sum += f[x] * sh_l[x][row];
+      }
+      const int64_t r = row0 + row;
+      const int64_t at = (w.s.token + r / a.group) * a.heads + head * a.group + r % a.group;
+      const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+      for (int d = lane * 2; d < D; d += 64) {
+        float y0 = 0.0f, y1 = 0.0f;
+#pragma unroll
+        for (int x = 0; x < WARPS; ++x) {
+          const float2 z = *reinterpret_cast<const float2*>(&sh_o[x][row][d]);
+          y0 += f[x] * z.x;
+          y1 += f[x] * z.y;
+        }
+        if (is_whole) {
+          T* out = static_cast<T*>(a.out) + at * D + d;
+          out[0] = from_float<T>(y0 * inv);
+          out[1] = from_float<T>(y1 * inv);
+        } else {
+          *reinterpret_cast<float2*>(part + row * D + d) = make_float2(y0, y1);
+        }
+      }
+      if (lane == 0) {
+        if (!is_whole) {
+          part[ROWS * D + row] = top;
+          part[ROWS * (D + 1) + row] = sum;
+        } else if (a.lse) {
+          a.lse[at] = sum > 0.0f ? top * LN2 + logf(sum) : -INFINITY;
+        }
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// Joins the items that several runs share: a block per run that continues one,
+// and row.
+template <typename T, int D, int ROWS>
+__global__ __launch_bounds__(THREADS) void k_kv_join(AttendArgs a) {
+  constexpr int LANES = D / 4, GROUPS = THREADS / LANES;  // a thread sums 4 elements over every GROUPS-th part
+  __shared__ float4 sh_o[GROUPS][LANES];
+  __shared__ float sh_l[GROUPS];
+  griddep_wait();
+  const Split sp = a.splits[blockIdx.x];
+  const int row = blockIdx.y;
+  const int64_t r = sp.row0 + row;
+  if (sp.first < 0 || r >= sp.rows) return;
+  const int first = sp.first, last = sp.last;
+  const int group = threadIdx.x / LANES, at = threadIdx.x % LANES;
+  auto part = [&](int x) { return a.parts + ((int64_t)x * 2 + (x == first)) * (ROWS * (D + 2)); };
+  float top = -INFINITY;
+  for (int x = first + (threadIdx.x & 31); x <= last; x += 32) top = fmaxf(top, part(x)[ROWS * D + row]);
+#pragma unroll
+  for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(FULL, top, o));
+  float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  float sum = 0.0f;
+  if (top > -INFINITY) {
+#pragma unroll 4
+    for (int x = first + group; x <= last; x += GROUPS) {
+      const float* p = part(x);
+      const float f = ex2(p[ROWS * D + row] - top);
+      const float4 z = *reinterpret_cast<const float4*>(p + row * D + 4 * at);
+      sum += f * p[ROWS * (D + 1) + row];
+      y.x += f * z.x, y.y += f * z.y, y.z += f * z.z, y.w += f * z.w;
+    }
+  }
+  sh_o[group][at] = y;
+  if (at == 0) sh_l[group] = sum;
+  __syncthreads();
+  if (group) return;
+#pragma unroll
+  for (int x = 1; x < GROUPS; ++x) {
+    const float4 z = sh_o[x][at];
+    y.x += z.x, y.y += z.y, y.z += z.z, y.w += z.w;
+    sum += sh_l[x];
+  }
+  const int64_t o = (sp.token + r / a.group) * a.heads + sp.head * a.group + r % a.group;
+  const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+  T* out = static_cast<T*>(a.out) + o * D + 4 * at;
+  out[0] = from_float<T>(y.x * inv), out[1] = from_float<T>(y.y * inv);
+  out[2] = from_float<T>(y.z * inv), out[3] = from_float<T>(y.w * inv);
+  if (a.lse && at == 0) a.lse[o] = sum > 0.0f ? top * LN2 + logf(sum) : -INFINITY;
+}
+
+// Workspace: Split [grid] | partial sums.
+size_t split_bytes(int grid) { return ((size_t)grid * sizeof(Split) + 255) / 256 * 256; }
+
+constexpr int per_sm(int dim, int nt) { return dim == 256 ? 2 : nt == 1 ? 4 : 3; }
+
+// Rows of a tile: 16 where the sequences bring more than 8 on average and the
+// accumulators of 16 fit (head_dim up to 128).
+int row_tiles_of(const KvView& kv, int64_t n, int64_t total, int heads) {
+  const int64_t rows = (total + n - 1) / n * (heads / kv.c.kv_heads);
+  return rows > 8 && kv.c.head_dim <= 128 ? 2 : 1;
+}
+
+template <typename T, int D, int NT>
+cudaError_t attend(AttendArgs a, cudaStream_t s) {
+  const int grid = device_sm_count() * per_sm(D, NT);
+  a.splits = reinterpret_cast<Split*>(a.parts);
+  a.parts += split_bytes(grid) / sizeof(float);
+  (a.kv.c.codes == TQ_KV_INT8 ? k_kv_attend<T, D, TQ_KV_INT8, NT> : k_kv_attend<T, D, TQ_KV_E4M3, NT>)<<<grid, THREADS, 0, s>>>(a);
+  cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) return e;
+  return launch_maybe_pdl(true, k_kv_join<T, D, 8 * NT>, dim3(grid, 8 * NT), dim3(THREADS), 0, s, a);
 }
 
 template <typename T>
-cudaError_t attend_for(const KvView& kv, int layer, const int32_t* slots, const int32_t* starts, int64_t n,
-                       const KvRows& q, int64_t total, int heads, float scale, int window, void* out, float* lse,
-                       cudaStream_t s) {
-  return (kv.c.head_dim == 64    ? attend<T, 64>
-          : kv.c.head_dim == 128 ? attend<T, 128>
-                                 : attend<T, 256>)(kv, layer, slots, starts, n, q, total, heads, scale, window, out,
-                                                   lse, s);
+cudaError_t attend_for(const AttendArgs& a, int nt, cudaStream_t s) {
+  switch (a.kv.c.head_dim) {
+    case 64:
+      return nt == 1 ? attend<T, 64, 1>(a, s) : attend<T, 64, 2>(a, s);
+    case 128:
+      return nt == 1 ? attend<T, 128, 1>(a, s) : attend<T, 128, 2>(a, s);
+    default:
+      return attend<T, 256, 1>(a, s);
+  }
 }
 
 }  // namespace
 
-size_t kv_attend_workspace(const KvView&, int64_t, int64_t, int) { return 16; }
+size_t kv_attend_workspace(const KvView& kv, int64_t, int64_t, int) {
+  const int dim = kv.c.head_dim;
+  size_t need = 0;
+  for (int nt = 1; nt <= 2; ++nt) {
+    const int grid = device_sm_count() * per_sm(dim, nt);
+    need = std::max(need, split_bytes(grid) + (size_t)grid * 2 * 8 * nt * (dim + 2) * sizeof(float));
+  }
+  return need;
+}
 
 cudaError_t launch_kv_attend(const KvView& kv, int layer, const int32_t* slots, const int32_t* starts, int64_t n,
                              const KvRows& q, int type, int64_t total, int heads, float scale, int window, void* out,
                              float* lse, void* workspace, cudaStream_t s) {
-  return (type == TQ_BF16 ? attend_for<__nv_bfloat16> : attend_for<__half>)(kv, layer, slots, starts, n, q, total,
-                                                                            heads, scale, window, out, lse, s);
+  const AttendArgs a = {kv, layer, slots, starts, n, total, q, heads, heads / kv.c.kv_heads, scale, window, out, lse,
+                        static_cast<float*>(workspace), nullptr};
+  const int nt = row_tiles_of(kv, n, total, heads);
+  return type == TQ_BF16 ? attend_for<__nv_bfloat16>(a, nt, s) : attend_for<__half>(a, nt, s);
 }
 
 }  // namespace tq
