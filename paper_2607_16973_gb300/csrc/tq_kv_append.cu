@@ -9,6 +9,7 @@
 // Bound: HBM, 2 + 1 bytes per element (16-bit input); for single tokens
 // (a decoding step) the latency of the chain starts -> lens -> table -> codes.
 #include <algorithm>
+#include <cstring>
 
 #include "tq_kv.cuh"
 
@@ -16,6 +17,33 @@ namespace tq {
 namespace {
 
 constexpr int APPEND_WARPS = 8;
+
+// Largest magnitude of the elements of two words (one element of float32, two of
+// the 16-bit types side by side), as bits without sign: they order as the values
+// do.
+template <typename T>
+__device__ __forceinline__ uint32_t max_magnitude(uint32_t a, uint32_t b) {
+  return sizeof(T) == 2 ? __vmaxu2(a, b & 0x7FFF7FFFu) : max(a, b & 0x7FFFFFFFu);
+}
+template <typename T>
+__device__ __forceinline__ float magnitude(uint32_t bits) {
+  if (sizeof(T) == 4) return __uint_as_float(bits);
+  const uint32_t top = max(bits & 0xFFFFu, bits >> 16);
+  T x;
+  memcpy(&x, &top, sizeof(T));
+  return to_float(x);
+}
+
+// Whether a quotient that is off by up to 2^-22 of itself might round to another
+// code than the exact one: within that of a half for int8 (4e-5 at 127), within
+// 4 steps of a middle for e4m3 (of 2^20 steps of a float32 between two codes), or
+// below e4m3's normal range.
+template <int CODES>
+__device__ __forceinline__ bool near_turn(float y) {
+  if (CODES == TQ_KV_INT8) return fabsf(y - rintf(y)) > 0.49996f;
+  const uint32_t low = __float_as_uint(y) & 0xFFFFFu;
+  return low - 0x7FFFCu <= 8u || (fabsf(y) < 0.015625f && y != 0.0f);
+}
 
 template <typename T, int D, int CODES, bool VEC>
 __global__ __launch_bounds__(APPEND_WARPS * 32) void k_kv_append(KvView kv, int layer,
@@ -59,7 +87,6 @@ __global__ __launch_bounds__(APPEND_WARPS * 32) void k_kv_append(KvView kv, int 
     uint4 u;
     T e[E];
   } r[CHUNKS];
-  float top = 0.0f;
 #pragma unroll
   for (int c = 0; c < CHUNKS; ++c) {
     const int e = (c * 32 + lane) * E, row = e / D, col = e % D;
@@ -67,22 +94,35 @@ __global__ __launch_bounds__(APPEND_WARPS * 32) void k_kv_append(KvView kv, int 
     if (row >= lo && row < hi) {
       const T* p = x + row * src.token_stride + col;
       if (VEC) {
-        r[c].u = __ldg(reinterpret_cast<const uint4*>(p));
+        r[c].u = __ldcs(reinterpret_cast<const uint4*>(p));
       } else {
 #pragma unroll
         for (int j = 0; j < E; ++j) r[c].e[j] = p[j];
       }
     }
   }
+  // the largest magnitude, by the bits without their sign; an infinity or a NaN
+  // shows in it, and only then are the finite values looked for one by one
+  uint32_t bits = 0;
 #pragma unroll
   for (int c = 0; c < CHUNKS; ++c)
+    bits = max_magnitude<T>(max_magnitude<T>(max_magnitude<T>(max_magnitude<T>(bits, r[c].u.x), r[c].u.y), r[c].u.z), r[c].u.w);
 #pragma unroll
-    for (int j = 0; j < E; ++j) {
-      const float a = fabsf(to_float(r[c].e[j]));
-      if (a < INFINITY) top = fmaxf(top, a);  // (not for NaN)
-    }
+  for (int o = 16; o; o >>= 1) bits = max_magnitude<T>(bits, __shfl_xor_sync(0xffffffffu, bits, o));
+  float top = magnitude<T>(bits);
+  const bool finite = top < INFINITY;
+  if (!finite) {
+    top = 0.0f;
 #pragma unroll
-  for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+      for (int j = 0; j < E; ++j) {
+        const float a = fabsf(to_float(r[c].e[j]));
+        if (a < INFINITY) top = fmaxf(top, a);  // (not for NaN)
+      }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  }
 
   float s = __fdiv_rn(top, kv_qmax<CODES>());
   if (lo > 0) {
@@ -101,16 +141,29 @@ __global__ __launch_bounds__(APPEND_WARPS * 32) void k_kv_append(KvView kv, int 
   }
   __syncwarp();
   if (lane == 0) *scale = s;
+  // x / s as a product where that gives the same code: not for values that are
+  // not finite, scales whose reciprocal leaves the normal range, and quotients
+  // close to where the rounding turns
+  const bool fast = finite && s > 0x1p-100f && s < 0x1p100f;
+  const float inv = fast ? __frcp_rn(s) : 0.0f;
 #pragma unroll
   for (int c = 0; c < CHUNKS; ++c) {
     const int e = (c * 32 + lane) * E, row = e / D;
     if (row < lo || row >= hi) continue;
     float y[E];
+    bool exact = !fast;
 #pragma unroll
     for (int j = 0; j < E; ++j) {
-      const float a = to_float(r[c].e[j]);
-      y[j] = s > 0.0f && a == a ? __fdiv_rn(a, s) : 0.0f;
-      y[j] = fminf(fmaxf(y[j], -kv_qmax<CODES>()), kv_qmax<CODES>());
+      y[j] = to_float(r[c].e[j]) * inv;
+      exact |= near_turn<CODES>(y[j]);
+    }
+    if (exact) {
+#pragma unroll
+      for (int j = 0; j < E; ++j) {
+        const float a = to_float(r[c].e[j]);
+        y[j] = s > 0.0f && a == a ? __fdiv_rn(a, s) : 0.0f;
+        y[j] = fminf(fmaxf(y[j], -kv_qmax<CODES>()), kv_qmax<CODES>());
+      }
     }
     uint32_t out[E / 4];
 #pragma unroll

@@ -13,6 +13,7 @@
 #include <algorithm>
 
 #include "tq_kv.cuh"
+#include "tq_topk.cuh"
 
 namespace tq {
 namespace {
@@ -175,6 +176,7 @@ __global__ __launch_bounds__(ONE) void k_kv_extend(KvView kv, const int32_t* __r
                                                    const int32_t* __restrict__ counts, int64_t n, ExtendWork w) {
   __shared__ int64_t warp_sums[ONE / 32];
   __shared__ uint32_t seen[kKvMaxSlots / 32];
+  griddep_launch_dependents();
   for (int i = threadIdx.x; i < kKvMaxSlots / 32; i += ONE) seen[i] = 0;
   __syncthreads();
   bool bad = false;
@@ -267,6 +269,7 @@ __device__ __forceinline__ void copy_codes(uint8_t* __restrict__ to, const uint8
 // threads per entry, layer, head, and K or V.
 __global__ __launch_bounds__(COPY) void k_kv_copy_parts(KvView kv, ExtendWork w) {
   const int64_t i = blockIdx.x;
+  griddep_wait();
   const int from = w.from[i];
   if (from < 0) return;
   const int to = w.to[i], blocks = w.blocks[i];
@@ -304,6 +307,7 @@ CompactWork compact_work(const KvView& kv, void* ws, size_t* bytes) {
 
 __global__ __launch_bounds__(ONE) void k_kv_compact(KvView kv, CompactWork w, int32_t* used) {
   __shared__ int64_t warp_sums[ONE / 32];
+  griddep_launch_dependents();
   const int64_t pages = kv.c.pages;
   const int64_t live = ranked_pages<true>(kv, 0, pages, pages, warp_sums, [](int64_t, int64_t) {});
   const int64_t holes = ranked_pages<false>(kv, 0, live, pages, warp_sums,
@@ -327,6 +331,8 @@ __global__ __launch_bounds__(ONE) void k_kv_compact(KvView kv, CompactWork w, in
 
 // Moves pages: pieces of COPY_BYTES of (page, layer, K or V), in turn over the grid.
 __global__ __launch_bounds__(COPY) void k_kv_move(KvView kv, CompactWork w) {
+  griddep_launch_dependents();
+  griddep_wait();
   const int64_t moves = w.sizes[1];
   const int64_t bytes = (int64_t)kv.c.kv_heads * kv.c.page_tokens * kv.c.head_dim;
   const int64_t scales = (int64_t)kv.c.kv_heads * kv.c.page_tokens / kKvBlock;
@@ -351,6 +357,7 @@ __global__ __launch_bounds__(COPY) void k_kv_move(KvView kv, CompactWork w) {
 }
 
 __global__ __launch_bounds__(COPY) void k_kv_rename(KvView kv, CompactWork w) {
+  griddep_wait();
   const int64_t live = w.sizes[0], n = kv.c.slots * kv.c.max_pages;
   for (int64_t e = (int64_t)blockIdx.x * COPY + threadIdx.x; e < n; e += (int64_t)gridDim.x * COPY) {
     const int page = kv.c.table[e];
@@ -384,8 +391,8 @@ cudaError_t launch_kv_extend(const KvView& kv, const int32_t* slots, const int32
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   const int64_t parts = (int64_t)2 * kv.c.layers * kv.c.kv_heads;
-  k_kv_copy_parts<<<dim3((unsigned)n, (unsigned)std::min<int64_t>(parts, 65535)), COPY, 0, s>>>(kv, w);
-  return cudaGetLastError();
+  return launch_maybe_pdl(true, k_kv_copy_parts, dim3((unsigned)n, (unsigned)std::min<int64_t>(parts, 65535)),
+                          dim3(COPY), 0, s, kv, w);
 }
 
 size_t kv_compact_workspace(const KvView& kv) {
@@ -400,11 +407,10 @@ cudaError_t launch_kv_compact(const KvView& kv, int32_t* used, void* workspace, 
   k_kv_compact<<<1, ONE, 0, s>>>(kv, w, used);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
-  k_kv_move<<<sms * 8, COPY, 0, s>>>(kv, w);
-  if ((e = cudaGetLastError()) != cudaSuccess) return e;
+  if ((e = launch_maybe_pdl(true, k_kv_move, dim3(sms * 8), dim3(COPY), 0, s, kv, w)) != cudaSuccess) return e;
   const int64_t entries = kv.c.slots * kv.c.max_pages;
-  k_kv_rename<<<(unsigned)std::min<int64_t>((entries + COPY - 1) / COPY, (int64_t)sms * 8), COPY, 0, s>>>(kv, w);
-  return cudaGetLastError();
+  return launch_maybe_pdl(true, k_kv_rename, dim3((unsigned)std::min<int64_t>((entries + COPY - 1) / COPY, sms * 8)),
+                          dim3(COPY), 0, s, kv, w);
 }
 
 }  // namespace tq

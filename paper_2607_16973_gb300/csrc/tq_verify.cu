@@ -20,6 +20,7 @@
 #include <algorithm>
 
 #include "tq_kv.cuh"
+#include "tq_topk.cuh"
 
 namespace tq {
 namespace {
@@ -67,20 +68,62 @@ __device__ __forceinline__ uint64_t race_key(float w, int v) {
   return (uint64_t)__float_as_uint(w) << 32 | (uint32_t)~v;
 }
 
+// EACH neighbours of a row, from 16-byte loads where the row allows them.
+constexpr int EACH = 8;
+
+template <typename T>
+__device__ __forceinline__ void load_each(const T* __restrict__ p, float (&x)[EACH]) {
+  union {
+    uint4 v[EACH * sizeof(T) / 16];
+    T e[EACH];
+  } u;
+#pragma unroll
+  for (int c = 0; c < (int)(EACH * sizeof(T) / 16); ++c) u.v[c] = __ldcs(reinterpret_cast<const uint4*>(p) + c);
+#pragma unroll
+  for (int j = 0; j < EACH; ++j) x[j] = to_float(u.e[j]);
+}
+
+// The race over tokens [begin, end); begin is a multiple of EACH.  Every quotient
+// that could win is a correctly rounded division; one that is below the
+// thread's best by more than the product's rounding is not taken.
 template <typename T>
 __device__ uint64_t race(const T* __restrict__ p, const T* __restrict__ q, int without, const float* __restrict__ noise,
                          int begin, int end) {
   float best = 0.0f;
   int token = -1;
-  for (int v = begin + threadIdx.x; v < end; v += VERIFY) {
-    float w = to_float(p[v]);
-    if (q) w -= to_float(q[v]);
-    if (v == without) w = 0.0f;
-    if (!(w > 0.0f)) continue;
-    const float x = __fdiv_rn(w, noise[v]);
-    if (x > best) {
-      best = x;
-      token = v;
+  const bool wide = (((uintptr_t)p | (uintptr_t)q | (uintptr_t)noise) & 15u) == 0;
+  for (int base = begin; base < end; base += VERIFY * EACH) {
+    // aligned rows: a thread's tokens lie side by side, else VERIFY apart
+    const bool whole = base + VERIFY * EACH <= end && wide;
+    const int first = base + (int)threadIdx.x * (whole ? EACH : 1), stride = whole ? 1 : VERIFY;
+    float w[EACH], e[EACH];
+    if (whole) {
+      load_each(p + first, w);
+      load_each(noise + first, e);
+      if (q) {
+        float x[EACH];
+        load_each(q + first, x);
+#pragma unroll
+        for (int j = 0; j < EACH; ++j) w[j] -= x[j];
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < EACH; ++j) {
+        const int v = first + j * VERIFY;
+        w[j] = v < end ? to_float(p[v]) : 0.0f;
+        e[j] = v < end ? noise[v] : 1.0f;
+        if (q && v < end) w[j] -= to_float(q[v]);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < EACH; ++j) {
+      const int v = first + j * stride;
+      if (!(w[j] > 0.0f) || v == without || w[j] < best * e[j] * 0.999999f) continue;
+      const float x = __fdiv_rn(w[j], e[j]);
+      if (x > best) {
+        best = x;
+        token = v;
+      }
     }
   }
   return token < 0 ? 0 : race_key(best, token);
@@ -110,9 +153,10 @@ __global__ __launch_bounds__(VERIFY) void k_verify(const T* __restrict__ target,
                                                    int64_t n, int t, int vocab, uint64_t* __restrict__ keys) {
   __shared__ uint64_t shared[VERIFY / 32];
   const int64_t i = blockIdx.y;
+  griddep_launch_dependents();
   const Verdict r = judge(target, draft, drafts, draft_lens, uniforms, i, t, vocab);
   const bool rejected = r.accepted < r.drafts;
-  const int each = (vocab + gridDim.x - 1) / gridDim.x;
+  const int each = ((vocab + gridDim.x - 1) / gridDim.x + EACH - 1) / EACH * EACH;
   const int begin = blockIdx.x * each, end = min(vocab, begin + each);
   const T* q = rejected && draft ? draft + (i * t + r.accepted) * vocab : nullptr;
   uint64_t key = race(target + (i * (t + 1) + r.accepted) * vocab, q, rejected && !draft ? r.rejected : -1,
@@ -132,6 +176,7 @@ __global__ __launch_bounds__(VERIFY) void k_verify_finish(const T* __restrict__ 
   __shared__ uint64_t shared[2][VERIFY / 32];
   const int64_t i = blockIdx.x;
   const Verdict r = judge(target, draft, drafts, draft_lens, uniforms, i, t, vocab);
+  griddep_wait();  // (the verdict needs the call's inputs alone)
   uint64_t key = 0;
   for (int j = threadIdx.x; j < parts; j += VERIFY) key = max(key, keys[i * parts + j]);
   key = block_max(key, shared[0]);
@@ -161,10 +206,9 @@ cudaError_t verify(const void* target, const void* draft, const int32_t* drafts,
                                                           drafts, draft_lens, uniforms, noise, n, t, vocab, keys);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
-  k_verify_finish<T><<<(unsigned)n, VERIFY, 0, s>>>(static_cast<const T*>(target), static_cast<const T*>(draft), drafts,
-                                                    draft_lens, uniforms, noise, n, t, vocab, keys, parts, tokens,
-                                                    accepted);
-  return cudaGetLastError();
+  return launch_maybe_pdl(true, k_verify_finish<T>, dim3((unsigned)n), dim3(VERIFY), 0, s,
+                          static_cast<const T*>(target), static_cast<const T*>(draft), drafts, draft_lens, uniforms,
+                          noise, n, t, vocab, static_cast<const uint64_t*>(keys), parts, tokens, accepted);
 }
 
 }  // namespace

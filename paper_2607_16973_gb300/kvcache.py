@@ -19,28 +19,68 @@ call could not carry out.
 from __future__ import annotations
 
 import ctypes as C
-import math
+import functools
 
 from . import _dev_ptr, _on_stream, _stream_handle, _torch, _used_on
 from ._lib import KV_CODES, KvCacheStruct, check, load
 
 BLOCK = 16  # tokens that share a scale
 
+# A decoding step makes these calls once per layer on a few tokens, and their
+# host side is then what it waits for: the checks below take the short way where
+# everything is in order and leave it to _dev_ptr to say what is not.
 
+
+@functools.lru_cache(maxsize=1)
 def _types():
     torch = _torch()
     return {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 
 
+def _ptr(t, name: str, dtype) -> int:
+    if t.dtype is dtype and t.is_cuda and t.is_contiguous():
+        return t.data_ptr()
+    return _dev_ptr(t, name, dtype)
+
+
+@functools.lru_cache(maxsize=1)
+def _current_raw_stream():
+    """Handle of the current stream: without the Stream object that
+    torch.cuda.current_stream makes, where torch offers that."""
+    c = _torch()._C
+    raw, device = getattr(c, "_cuda_getCurrentRawStream", None), getattr(c, "_cuda_getDevice", None)
+    return (lambda: raw(device())) if raw and device else (lambda: _stream_handle(None))
+
+
+def _stream(stream) -> int:
+    return _current_raw_stream()() if stream is None else int(stream.cuda_stream)
+
+
+def _empty(shape, dtype, device, stream):
+    torch = _torch()
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with _on_stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _used(stream, *tensors) -> None:
+    if stream is not None:
+        for t in tensors:
+            _used_on(t, stream)
+
+
 def _rows(t, name: str, heads: int, dim: int, types):
     """Rows [tokens, heads, dim] with any strides but the last: (pointer, type,
     token stride, head stride)."""
-    ptr = _dev_ptr(t, name, types, contiguous=False)
+    if not t.is_cuda or t.dtype not in types:
+        _dev_ptr(t, name, types, contiguous=False)
     if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim:
         raise ValueError(f"{name} must be [tokens, {heads}, {dim}], got {tuple(t.shape)}")
-    if t.numel() and t.stride(2) != 1:
+    s0, s1, s2 = t.stride()
+    if s2 != 1 and t.numel():
         raise ValueError(f"{name}: the elements of a row must lie side by side")
-    return ptr, _types()[t.dtype], t.stride(0), t.stride(1)
+    return t.data_ptr(), _types()[t.dtype], s0, s1
 
 
 class KVCache:
@@ -98,25 +138,32 @@ class KVCache:
             _dev_ptr(v_scale, "v_scale", f32), _dev_ptr(table, "table", i32), _dev_ptr(lens, "lens", i32),
             _dev_ptr(refs, "refs", i32), _dev_ptr(self.status, "status"), pages, table.shape[0], table.shape[1],
             layers, kv_heads, head_dim, page_tokens, KV_CODES[codes])
+        self._handle = C.byref(self._c)
+        self._needs = {}  # workspace bytes by call and sizes
 
-    @property
-    def _handle(self):
-        return C.byref(self._c)
-
-    def _entries(self, a, b, names, stream, extra: int = 0):
+    def _entries(self, a, b, name_a: str, name_b: str, stream, extra: int = 0):
         """Two int32 arrays of as many entries (the second `extra` more)."""
         i32 = _torch().int32
-        pa, pb = _dev_ptr(a, names[0], i32), _dev_ptr(b, names[1], i32)
-        if a.dim() != 1 or b.dim() != 1 or b.numel() != a.numel() + extra:
-            raise ValueError(f"{names[0]} must be [n] and {names[1]} [n{' + 1' if extra else ''}]")
-        for t in (a, b):
-            _used_on(t, stream)
-        return pa, pb, a.numel()
+        pa, pb, n = _ptr(a, name_a, i32), _ptr(b, name_b, i32), a.numel()
+        if a.dim() != 1 or b.dim() != 1 or b.numel() != n + extra:
+            raise ValueError(f"{name_a} must be [n] and {name_b} [n{' + 1' if extra else ''}]")
+        _used(stream, a, b)
+        return pa, pb, n
 
-    def _workspace(self, workspace, need: int, stream):
+    def _need(self, fn: str, *sizes) -> int:
+        need = self._needs.get((fn, sizes))
+        if need is None:
+            out = C.c_size_t()
+            check(getattr(load(), fn)(self._handle, *sizes, C.byref(out)))
+            if len(self._needs) >= 4096:
+                self._needs.clear()
+            need = self._needs[fn, sizes] = max(out.value, 16)
+        return need
+
+    def _workspace(self, workspace, stream, fn: str, *sizes):
         if workspace is None:
-            with _on_stream(stream):
-                workspace = _torch().empty(max(need, 16), dtype=_torch().uint8, device=self.k.device)
+            workspace = _empty(self._need(fn, *sizes), _torch().uint8, self.k.device, stream)
+            return workspace, workspace.data_ptr(), workspace.numel()
         return workspace, _dev_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size()
 
     def append(self, layer: int, slots, starts, k, v, stream=None) -> None:
@@ -125,22 +172,19 @@ class KVCache:
         ([tokens, kv_heads, head_dim], bfloat16, float16 or float32, any strides
         but the last)."""
         c = self._c
-        ps, pt, n = self._entries(slots, starts, ("slots", "starts"), stream, 1)
+        ps, pt, n = self._entries(slots, starts, "slots", "starts", stream, 1)
         types = tuple(_types())
         kp, kt, k0, k1 = _rows(k, "k", c.kv_heads, c.head_dim, types)
         vp, vt, v0, v1 = _rows(v, "v", c.kv_heads, c.head_dim, types)
         if kt != vt or k.shape != v.shape:
             raise ValueError("k and v must have one type and shape")
-        for t in (k, v):
-            _used_on(t, stream)
+        _used(stream, k, v)
         check(load().tq_kv_append(self._handle, layer, ps, pt, n, kp, vp, kt, k.shape[0], k0, k1, v0, v1,
-                                  _stream_handle(stream)))
+                                  _stream(stream)))
 
     def attention_workspace(self, n: int, total: int, heads: int) -> int:
         """tq_kv_attend_workspace: device bytes for `total` queries of n sequences."""
-        need = C.c_size_t()
-        check(load().tq_kv_attend_workspace(self._handle, n, total, heads, C.byref(need)))
-        return need.value
+        return self._need("tq_kv_attend_workspace", n, total, heads)
 
     def attention(self, layer: int, slots, starts, q, scale: float | None = None, window: int = 0, out=None,
                   lse=None, return_lse: bool = False, workspace=None, stream=None):
@@ -152,67 +196,57 @@ class KVCache:
         `return_lse`."""
         torch = _torch()
         c = self._c
-        ps, pt, n = self._entries(slots, starts, ("slots", "starts"), stream, 1)
+        ps, pt, n = self._entries(slots, starts, "slots", "starts", stream, 1)
         if q.dim() != 3:
             raise ValueError(f"q must be [tokens, heads, {c.head_dim}]")
-        total, heads = q.shape[0], q.shape[1]
+        total, heads, dim = q.shape
         qp, qt, q0, q1 = _rows(q, "q", heads, c.head_dim, (torch.bfloat16, torch.float16))
-        _used_on(q, stream)
-        with _on_stream(stream):
-            if out is None:
-                out = torch.empty((total, heads, c.head_dim), dtype=q.dtype, device=q.device)
-            if lse is None and return_lse:
-                lse = torch.empty((total, heads), dtype=torch.float32, device=q.device)
-        if tuple(out.shape) != (total, heads, c.head_dim):
-            raise ValueError(f"out must be {(total, heads, c.head_dim)}")
-        if lse is not None and tuple(lse.shape) != (total, heads):
+        _used(stream, q)
+        if out is None:
+            out = _empty((total, heads, dim), q.dtype, q.device, stream)
+        elif tuple(out.shape) != (total, heads, dim):
+            raise ValueError(f"out must be {(total, heads, dim)}")
+        if lse is None:
+            if return_lse:
+                lse = _empty((total, heads), torch.float32, q.device, stream)
+        elif tuple(lse.shape) != (total, heads):
             raise ValueError(f"lse must be {(total, heads)}")
-        need = self.attention_workspace(n, total, heads) if workspace is None else 0
-        workspace, wp, wb = self._workspace(workspace, need, stream)
+        workspace, wp, wb = self._workspace(workspace, stream, "tq_kv_attend_workspace", n, total, heads)
         check(load().tq_kv_attend(self._handle, layer, ps, pt, n, qp, qt, total, heads, q0, q1,
-                                  1.0 / math.sqrt(c.head_dim) if scale is None else scale, window,
-                                  _dev_ptr(out, "out", q.dtype), _dev_ptr(lse, "lse", torch.float32) or None, wp, wb,
-                                  _stream_handle(stream)))
+                                  dim ** -0.5 if scale is None else scale, window, _ptr(out, "out", q.dtype),
+                                  None if lse is None else _ptr(lse, "lse", torch.float32), wp, wb, _stream(stream)))
         return (out, lse) if return_lse else out
 
     def fork(self, dst, src, stream=None) -> None:
         """tq_kv_fork: slots dst hold what slots src hold, in the same pages."""
-        pd, ps, n = self._entries(dst, src, ("dst", "src"), stream)
-        check(load().tq_kv_fork(self._handle, pd, ps, n, _stream_handle(stream)))
+        pd, ps, n = self._entries(dst, src, "dst", "src", stream)
+        check(load().tq_kv_fork(self._handle, pd, ps, n, _stream(stream)))
 
     def extend(self, slots, counts, workspace=None, stream=None) -> None:
         """tq_kv_extend: room for counts[i] more tokens in slots[i]; a shared last
         page that is part full is replaced by a copy."""
-        ps, pc, n = self._entries(slots, counts, ("slots", "counts"), stream)
-        need = C.c_size_t()
-        if workspace is None:
-            check(load().tq_kv_extend_workspace(self._handle, n, C.byref(need)))
-        workspace, wp, wb = self._workspace(workspace, need.value, stream)
-        check(load().tq_kv_extend(self._handle, ps, pc, n, wp, wb, _stream_handle(stream)))
+        ps, pc, n = self._entries(slots, counts, "slots", "counts", stream)
+        workspace, wp, wb = self._workspace(workspace, stream, "tq_kv_extend_workspace", n)
+        check(load().tq_kv_extend(self._handle, ps, pc, n, wp, wb, _stream(stream)))
 
     def truncate(self, slots, lens, stream=None) -> None:
         """tq_kv_truncate: slots[i] keeps its first lens[i] tokens (0: none)."""
-        ps, pl, n = self._entries(slots, lens, ("slots", "lens"), stream)
-        check(load().tq_kv_truncate(self._handle, ps, pl, n, _stream_handle(stream)))
+        ps, pl, n = self._entries(slots, lens, "slots", "lens", stream)
+        check(load().tq_kv_truncate(self._handle, ps, pl, n, _stream(stream)))
 
     def compact(self, workspace=None, stream=None):
         """tq_kv_compact: moves the pages in use to the front of the pool; returns
         how many there are (int32 [1] on the device)."""
-        torch = _torch()
-        need = C.c_size_t()
-        if workspace is None:
-            check(load().tq_kv_compact_workspace(self._handle, C.byref(need)))
-        workspace, wp, wb = self._workspace(workspace, need.value, stream)
-        with _on_stream(stream):
-            used = torch.empty(1, dtype=torch.int32, device=self.k.device)
-        check(load().tq_kv_compact(self._handle, _dev_ptr(used, "used"), wp, wb, _stream_handle(stream)))
+        workspace, wp, wb = self._workspace(workspace, stream, "tq_kv_compact_workspace")
+        used = _empty(1, _torch().int32, self.k.device, stream)
+        check(load().tq_kv_compact(self._handle, used.data_ptr(), wp, wb, _stream(stream)))
         return used
 
     def check(self, stream=None) -> None:
         """tq_kv_check: waits for the stream; raises TQError if a call since the
         last check found too few free pages (TQ_ENOMEM) or left entries out
         (TQ_EINVAL)."""
-        check(load().tq_kv_check(self._handle, _stream_handle(stream)))
+        check(load().tq_kv_check(self._handle, _stream(stream)))
 
 
 def verify_drafts(target_probs, drafts, uniforms, noise, draft_probs=None, draft_lens=None, tokens=None, accepted=None,
@@ -229,32 +263,37 @@ def verify_drafts(target_probs, drafts, uniforms, noise, draft_probs=None, draft
     types = _types()
     if target_probs.dim() != 3:
         raise ValueError("target_probs must be [n, t + 1, vocab]")
-    n, t, vocab = target_probs.shape[0], target_probs.shape[1] - 1, target_probs.shape[2]
-    shapes = ((drafts, "drafts", (n, t)), (uniforms, "uniforms", (n, t)), (noise, "noise", (n, vocab)),
-              (draft_probs, "draft_probs", (n, t, vocab)), (draft_lens, "draft_lens", (n,)),
-              (tokens, "tokens", (n, t + 1)), (accepted, "accepted", (n,)))
-    for x, name, shape in shapes:
-        if x is not None and tuple(x.shape) != shape:
+    n, t, vocab = target_probs.shape
+    t -= 1
+    dtype, i32, f32, dev = target_probs.dtype, torch.int32, torch.float32, target_probs.device
+
+    def ptr(x, name, kind, *shape):
+        if x is None:
+            return None
+        if x.shape != shape:
             raise ValueError(f"{name} must be {shape}, got {tuple(x.shape)}")
-    tp = _dev_ptr(target_probs, "target_probs", tuple(types))
-    dp = _dev_ptr(draft_probs, "draft_probs", target_probs.dtype)
-    for x in (target_probs, draft_probs, drafts, draft_lens, uniforms, noise):
-        if x is not None:
-            _used_on(x, stream)
-    dev, i32, f32 = target_probs.device, torch.int32, torch.float32
-    need = C.c_size_t()
-    with _on_stream(stream):
-        if tokens is None:
-            tokens = torch.empty((n, t + 1), dtype=i32, device=dev)
-        if accepted is None:
-            accepted = torch.empty(n, dtype=i32, device=dev)
-        if workspace is None:
-            check(load().tq_verify_drafts_workspace(n, vocab, C.byref(need)))
-            workspace = torch.empty(max(need.value, 16), dtype=torch.uint8, device=dev)
-    check(load().tq_verify_drafts(
-        tp, dp or None, types[target_probs.dtype], _dev_ptr(drafts, "drafts", i32),
-        _dev_ptr(draft_lens, "draft_lens", i32) or None, _dev_ptr(uniforms, "uniforms", f32),
-        _dev_ptr(noise, "noise", f32), n, t, vocab, _dev_ptr(tokens, "tokens", i32),
-        _dev_ptr(accepted, "accepted", i32), _dev_ptr(workspace, "workspace"),
-        workspace.numel() * workspace.element_size(), _stream_handle(stream)))
+        return _ptr(x, name, kind)
+
+    args = (target_probs.data_ptr(), ptr(draft_probs, "draft_probs", dtype, n, t, vocab), types.get(dtype),
+            ptr(drafts, "drafts", i32, n, t), ptr(draft_lens, "draft_lens", i32, n),
+            ptr(uniforms, "uniforms", f32, n, t), ptr(noise, "noise", f32, n, vocab), n, t, vocab)
+    if not target_probs.is_cuda or dtype not in types or not target_probs.is_contiguous():
+        _dev_ptr(target_probs, "target_probs", tuple(types))
+    _used(stream, target_probs, draft_probs, drafts, draft_lens, uniforms, noise)
+    if tokens is None:
+        tokens = _empty((n, t + 1), i32, dev, stream)
+    if accepted is None:
+        accepted = _empty(n, i32, dev, stream)
+    if workspace is None:
+        workspace = _empty(_verify_need(n, vocab), torch.uint8, dev, stream)
+    check(load().tq_verify_drafts(*args, ptr(tokens, "tokens", i32, n, t + 1), ptr(accepted, "accepted", i32, n),
+                                  _dev_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size(),
+                                  _stream(stream)))
     return tokens, accepted
+
+
+@functools.lru_cache(maxsize=4096)
+def _verify_need(n: int, vocab: int) -> int:
+    need = C.c_size_t()
+    check(load().tq_verify_drafts_workspace(n, vocab, C.byref(need)))
+    return max(need.value, 16)
