@@ -34,15 +34,53 @@ __device__ __forceinline__ float magnitude(uint32_t bits) {
   return to_float(x);
 }
 
-// Whether a quotient that is off by up to 2^-22 of itself might round to another
-// code than the exact one: within that of a half for int8 (4e-5 at 127), within
-// 4 steps of a middle for e4m3 (of 2^20 steps of a float32 between two codes), or
-// below e4m3's normal range.
+// Codes of a chunk by the definition: divided, NaN and everything at scale 0 to 0,
+// infinities to the ends.  A call, because it is rare and eight of it would not
+// stay in the instruction cache.
+template <typename T, int CODES>
+__device__ __noinline__ uint2 exact_codes(uint4 raw, float s) {
+  union {
+    uint4 u;
+    T e[16 / sizeof(T)];
+  } r;
+  r.u = raw;
+  float y[8] = {};
+#pragma unroll
+  for (int j = 0; j < (int)(16 / sizeof(T)); ++j) {
+    const float a = to_float(r.e[j]);
+    y[j] = s > 0.0f && a == a ? __fdiv_rn(a, s) : 0.0f;
+    y[j] = fminf(fmaxf(y[j], -kv_qmax<CODES>()), kv_qmax<CODES>());
+  }
+  return make_uint2(kv_pack4<CODES>(y[0], y[1], y[2], y[3]), kv_pack4<CODES>(y[4], y[5], y[6], y[7]));
+}
+
+// The largest finite magnitude of a chunk.
+template <typename T>
+__device__ __noinline__ float finite_top(uint4 raw) {
+  union {
+    uint4 u;
+    T e[16 / sizeof(T)];
+  } r;
+  r.u = raw;
+  float top = 0.0f;
+#pragma unroll
+  for (int j = 0; j < (int)(16 / sizeof(T)); ++j) {
+    const float a = fabsf(to_float(r.e[j]));
+    if (a < INFINITY) top = fmaxf(top, a);  // (not for NaN)
+  }
+  return top;
+}
+
+// kv_pack4 of four products.
 template <int CODES>
-__device__ __forceinline__ bool near_turn(float y) {
-  if (CODES == TQ_KV_INT8) return fabsf(y - rintf(y)) > 0.49996f;
-  const uint32_t low = __float_as_uint(y) & 0xFFFFFu;
-  return low - 0x7FFFCu <= 8u || (fabsf(y) < 0.015625f && y != 0.0f);
+__device__ __forceinline__ uint32_t pack_products(const float* x, float f) {
+  if (CODES == TQ_KV_INT8) {
+    const float m = 12582912.0f;  // (as in kv_pack4; the sum rounds the exact product)
+    const uint32_t ab = __byte_perm(__float_as_uint(fmaf(x[0], f, m)), __float_as_uint(fmaf(x[1], f, m)), 0x0040);
+    const uint32_t cd = __byte_perm(__float_as_uint(fmaf(x[2], f, m)), __float_as_uint(fmaf(x[3], f, m)), 0x0040);
+    return __byte_perm(ab, cd, 0x5410);
+  }
+  return kv_pack4<CODES>(x[0] * f, x[1] * f, x[2] * f, x[3] * f);
 }
 
 template <typename T, int D, int CODES, bool VEC>
@@ -114,12 +152,7 @@ __global__ __launch_bounds__(APPEND_WARPS * 32) void k_kv_append(KvView kv, int 
   if (!finite) {
     top = 0.0f;
 #pragma unroll
-    for (int c = 0; c < CHUNKS; ++c)
-#pragma unroll
-      for (int j = 0; j < E; ++j) {
-        const float a = fabsf(to_float(r[c].e[j]));
-        if (a < INFINITY) top = fmaxf(top, a);  // (not for NaN)
-      }
+    for (int c = 0; c < CHUNKS; ++c) top = fmaxf(top, finite_top<T>(r[c].u));
 #pragma unroll
     for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
   }
@@ -141,37 +174,28 @@ __global__ __launch_bounds__(APPEND_WARPS * 32) void k_kv_append(KvView kv, int 
   }
   __syncwarp();
   if (lane == 0) *scale = s;
-  // x / s as a product where that gives the same code: not for values that are
-  // not finite, scales whose reciprocal leaves the normal range, and quotients
-  // close to where the rounding turns
+  // x / s as a product where that gives the same code: products with factors just
+  // below and just above 1 / s (by 2^-21, more than what the reciprocal, the
+  // product and the division round) enclose the quotient, and rounding to codes
+  // keeps order, so where both give one code it is the quotient's.  Not for
+  // values that are not finite or scales whose reciprocal leaves the normal range.
   const bool fast = finite && s > 0x1p-100f && s < 0x1p100f;
   const float inv = fast ? __frcp_rn(s) : 0.0f;
+  const float below = inv * (1.0f - 0x1p-21f), above = inv * (1.0f + 0x1p-21f);
 #pragma unroll
   for (int c = 0; c < CHUNKS; ++c) {
     const int e = (c * 32 + lane) * E, row = e / D;
     if (row < lo || row >= hi) continue;
-    float y[E];
-    bool exact = !fast;
+    float a[E];
 #pragma unroll
-    for (int j = 0; j < E; ++j) {
-      y[j] = to_float(r[c].e[j]) * inv;
-      exact |= near_turn<CODES>(y[j]);
-    }
-    if (exact) {
-#pragma unroll
-      for (int j = 0; j < E; ++j) {
-        const float a = to_float(r[c].e[j]);
-        y[j] = s > 0.0f && a == a ? __fdiv_rn(a, s) : 0.0f;
-        y[j] = fminf(fmaxf(y[j], -kv_qmax<CODES>()), kv_qmax<CODES>());
-      }
-    }
-    uint32_t out[E / 4];
-#pragma unroll
-    for (int j = 0; j < E / 4; ++j) out[j] = kv_pack4<CODES>(y[4 * j], y[4 * j + 1], y[4 * j + 2], y[4 * j + 3]);
+    for (int j = 0; j < E; ++j) a[j] = to_float(r[c].e[j]);
+    uint2 out = make_uint2(pack_products<CODES>(a, below), pack_products<CODES>(a + (E - 4), below));
+    const uint2 up = make_uint2(pack_products<CODES>(a, above), pack_products<CODES>(a + (E - 4), above));
+    if (!fast || out.x != up.x || out.y != up.y) out = exact_codes<T, CODES>(r[c].u, s);
     if (E == 8)
-      *reinterpret_cast<uint2*>(codes + e) = make_uint2(out[0], out[E / 4 - 1]);
+      *reinterpret_cast<uint2*>(codes + e) = out;
     else
-      *reinterpret_cast<uint32_t*>(codes + e) = out[0];
+      *reinterpret_cast<uint32_t*>(codes + e) = out.x;
   }
 }
 

@@ -44,6 +44,7 @@ constexpr int WARPS = 4;
 constexpr int THREADS = WARPS * 32;
 constexpr int CHUNK = 1024;      // sequences whose units are kept in shared memory at a time
 constexpr int MIN_UNITS = 4;     // blocks that are worth a block of threads
+constexpr int ITEM_UNITS = 4;    // what an item costs beside its blocks (looking it up, its queries, its sums), in blocks
 // Weights are held as 2^(s - m) with the reference m LEAD below the largest score
 // that it was last set to, and moved again when a score passes that by LAZY:
 // they stay under 2^15, fp16's largest, and those down to 2^-24 of the largest
@@ -87,7 +88,8 @@ __device__ __forceinline__ float ex2(float x) {
 struct SeqWork {
   KvSeq s;
   int64_t tiles;
-  int first_block, blocks;  // blocks >= 1, so that a row that sees nothing is written too
+  int first_block, blocks;
+  int units;                // of each item: ITEM_UNITS, then one for each block
   bool ok;
 };
 
@@ -103,7 +105,8 @@ __device__ __forceinline__ SeqWork seq_work(const AttendArgs& a, int64_t i) {
   const int place = w.s.len - w.s.count;
   const int lo = a.window ? max(0, place - a.window + 1) : 0;
   w.first_block = lo / kKvBlock;
-  w.blocks = max(1, (w.s.len + kKvBlock - 1) / kKvBlock - w.first_block);
+  w.blocks = max(0, (w.s.len + kKvBlock - 1) / kKvBlock - w.first_block);
+  w.units = ITEM_UNITS + w.blocks;
   return w;
 }
 
@@ -111,7 +114,7 @@ template <int ROWS>
 __device__ __forceinline__ int64_t seq_units(const AttendArgs& a, int64_t i) {
   const SeqWork w = seq_work<ROWS>(a, i);
   if (!w.ok && blockIdx.x == 0) kv_status(a.kv, kKvBadEntry);
-  return w.tiles * a.kv.c.kv_heads * w.blocks;
+  return w.tiles * a.kv.c.kv_heads * w.units;
 }
 
 // The units of all sequences, found by a whole block: `before` holds the sums in
@@ -198,14 +201,11 @@ __device__ int64_t cut(const AttendArgs& a, Units& u, int64_t c, int64_t units, 
   if (x >= units) return units;
   int64_t before;
   const int64_t i = find_unit<ROWS>(a, u, x, before);
-  const int64_t blocks = seq_work<ROWS>(a, i).blocks, in = (x - before) % blocks;
-  return in < MIN_UNITS ? x - in : blocks - in < MIN_UNITS ? x - in + blocks : x;
+  const int64_t item = seq_work<ROWS>(a, i).units, in = (x - before) % item;
+  return in < ITEM_UNITS + MIN_UNITS ? x - in : item - in < MIN_UNITS ? x - in + item : x;
 }
 
-// Two pairs of fp16 values from the four codes of a word.  e4m3 codes come out
-// 2^-8 of their value: sign, exponent and mantissa are moved to their places in
-// fp16, whose exponents' bias is 8 larger; every code, the subnormal ones too,
-// is exact, and bytes that no token owns give finite values.
+// Two pairs of fp16 values from the four codes of a word: every code is exact.
 template <int CODES>
 __device__ __forceinline__ void to_half4(uint32_t w, uint32_t& lo, uint32_t& hi) {
   if (CODES == TQ_KV_INT8) {
@@ -219,13 +219,12 @@ __device__ __forceinline__ void to_half4(uint32_t w, uint32_t& lo, uint32_t& hi)
     x.h = __hsub2(x.h, bias);
     hi = x.r;
   } else {
-    const uint32_t a = __byte_perm(w, 0, 0x1404), b = __byte_perm(w, 0, 0x3424);
-    lo = (a & 0x80008000u) | ((a >> 1) & 0x3F803F80u);
-    hi = (b & 0x80008000u) | ((b >> 1) & 0x3F803F80u);
+    const __half2_raw a = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w & 0xFFFFu), __NV_E4M3);
+    const __half2_raw b = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w >> 16), __NV_E4M3);
+    lo = (uint32_t)a.y << 16 | a.x;
+    hi = (uint32_t)b.y << 16 | b.x;
   }
 }
-template <int CODES>
-constexpr float code_unit() { return CODES == TQ_KV_INT8 ? 1.0f : 256.0f; }
 
 __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                          uint32_t b1) {
@@ -279,17 +278,18 @@ __global__ __launch_bounds__(THREADS, D == 256 ? 2 : NT == 1 ? 4 : 3) void k_kv_
     int64_t before;
     const int64_t i = find_unit<ROWS>(a, units, u, before);
     const SeqWork w = seq_work<ROWS>(a, i);
-    const int64_t item = (u - before) / w.blocks;
-    const int b_first = (int)((u - before) % w.blocks);
-    const int b_last = (int)min((int64_t)w.blocks, b_first + (end - u));
-    u += b_last - b_first;
+    const int64_t item = (u - before) / w.units;
+    const int in = (int)((u - before) % w.units);
+    const int b_first = max(0, in - ITEM_UNITS);
+    const int b_last = (int)min((int64_t)w.blocks, in + (end - u) - ITEM_UNITS);
+    u += ITEM_UNITS + b_last - in;
     const int head = (int)(item % kv_heads);
     const int64_t row0 = item / kv_heads * ROWS, rows = (int64_t)w.s.count * a.group;
     if (b_first && threadIdx.x == 0) {
-      const int64_t begin = before + item * w.blocks;
-      const int first = (int)first_run(begin + MIN_UNITS, all, n_runs) - 1;
+      const int64_t begin = before + item * w.units;
+      const int first = (int)first_run(begin + ITEM_UNITS + MIN_UNITS, all, n_runs) - 1;
       if (first + 1 == (int)blockIdx.x)
-        a.splits[blockIdx.x] = {first, (int)last_run(begin + w.blocks - MIN_UNITS, all, n_runs), w.s.token, head, row0, rows};
+        a.splits[blockIdx.x] = {first, (int)last_run(begin + w.units - MIN_UNITS, all, n_runs), w.s.token, head, row0, rows};
     }
 
     // the queries, scaled by a power of two to fp16's middle: row n = g of each 8
@@ -325,7 +325,7 @@ __global__ __launch_bounds__(THREADS, D == 256 ? 2 : NT == 1 ? 4 : 3) void k_kv_
       // the largest element to [2^8, 2^9): both factors are powers of two within float32's normal range
       const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -110), 127);
       const float up = __uint_as_float((uint32_t)(127 + min(8 - e, 118)) << 23);
-      const float down = a.scale * LOG2E * code_unit<CODES>() / up;
+      const float down = a.scale * LOG2E / up;
 #pragma unroll
       for (int c = 0; c < KP; ++c)
 #pragma unroll
@@ -479,6 +479,17 @@ __global__ __launch_bounds__(THREADS, D == 256 ? 2 : NT == 1 ? 4 : 3) void k_kv_
               }
             }
         }
+        if (CODES == TQ_KV_E4M3 && !whole) {
+          // bytes that no token owns may be NaN, and 0 times that is not 0
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (b * kKvBlock + 2 * t + (r & 1) + (r >> 1) * 8 >= w.s.len) {
+#pragma unroll
+              for (int c = 0; c < VP; ++c)
+#pragma unroll
+                for (int x = 0; x < VW; ++x) vr[c][r][x] = 0;
+            }
+        }
         uint32_t pf[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -490,7 +501,6 @@ __global__ __launch_bounds__(THREADS, D == 256 ? 2 : NT == 1 ? 4 : 3) void k_kv_
           pf[nt][0] = transpose8x8(pack_half2(p0, p1));
           pf[nt][1] = transpose8x8(pack_half2(p2, p3));
         }
-        const float vf = v_scale * code_unit<CODES>();
 #pragma unroll
         for (int c = 0; c < VP; ++c)
 #pragma unroll
@@ -507,7 +517,7 @@ __global__ __launch_bounds__(THREADS, D == 256 ? 2 : NT == 1 ? 4 : 3) void k_kv_
                 float y[4] = {0.0f, 0.0f, 0.0f, 0.0f};
                 mma16816(y, a0, a1, a2, a3, pf[nt][0], pf[nt][1]);
 #pragma unroll
-                for (int z = 0; z < 4; ++z) o[nt][j][z] = fmaf(y[z], vf, o[nt][j][z]);
+                for (int z = 0; z < 4; ++z) o[nt][j][z] = fmaf(y[z], v_scale, o[nt][j][z]);
               }
             }
       }

@@ -21,7 +21,8 @@ namespace {
 constexpr int ONE = 1024;        // threads of the kernels that settle a call in one block
 constexpr int ROW = 256;         // threads per entry of fork and truncate
 constexpr int COPY = 256;        // threads of the copying kernels
-constexpr int COPY_BYTES = 16384;  // of a page that a block moves at a time
+constexpr int MOVE_BYTES = 32768;  // of a page that a block moves at a time
+constexpr int MOVE_PER_SM = 4;
 
 constexpr size_t align_up(size_t x) { return (x + 255) / 256 * 256; }
 
@@ -329,29 +330,50 @@ __global__ __launch_bounds__(ONE) void k_kv_compact(KvView kv, CompactWork w, in
   }
 }
 
-// Moves pages: pieces of COPY_BYTES of (page, layer, K or V), in turn over the grid.
-__global__ __launch_bounds__(COPY) void k_kv_move(KvView kv, CompactWork w) {
+// Moves pages: pieces of MOVE_BYTES of (page, layer, K or V), in turn over the
+// grid, each loaded whole before it is stored: 32 KB in flight per block, four
+// blocks per SM.  The pages of the next piece are looked up beside the copy.
+__global__ __launch_bounds__(COPY, MOVE_PER_SM) void k_kv_move(KvView kv, CompactWork w) {
   griddep_launch_dependents();
   griddep_wait();
   const int64_t moves = w.sizes[1];
-  const int64_t bytes = (int64_t)kv.c.kv_heads * kv.c.page_tokens * kv.c.head_dim;
-  const int64_t scales = (int64_t)kv.c.kv_heads * kv.c.page_tokens / kKvBlock;
-  const int64_t pieces = (bytes + COPY_BYTES - 1) / COPY_BYTES;
-  const int64_t per_page = pieces * 2 * kv.c.layers;
-  for (int64_t j = blockIdx.x; j < moves * per_page; j += gridDim.x) {
-    const int64_t i = j / per_page, r = j % per_page;
-    const int64_t piece = r % pieces;
+  const int bytes = kv.c.kv_heads * kv.c.page_tokens * kv.c.head_dim;
+  const int scales = kv.c.kv_heads * kv.c.page_tokens / kKvBlock;
+  const int pieces = (bytes + MOVE_BYTES - 1) / MOVE_BYTES;
+  const int per_page = pieces * 2 * kv.c.layers;
+  const int64_t all = moves * per_page;
+  int from = 0, to = 0;
+  if (blockIdx.x < all) {
+    from = w.from[blockIdx.x / per_page];
+    to = w.to[blockIdx.x / per_page];
+  }
+  for (int64_t j = blockIdx.x; j < all; j += gridDim.x) {
+    const int r = (int)(j % per_page), at = r % pieces * MOVE_BYTES;
     const bool is_v = r / pieces & 1;
-    const int layer = (int)(r / pieces / 2);
-    const int from = w.from[i], to = w.to[i];
+    const int layer = r / pieces / 2;
     uint8_t* codes = is_v ? kv.c.v : kv.c.k;
-    const int64_t at = piece * COPY_BYTES;
-    copy_codes(codes + kv.codes_at(layer, to, 0) + at, codes + kv.codes_at(layer, from, 0) + at,
-               min((int64_t)COPY_BYTES, bytes - at));
-    if (piece == 0) {
+    const uint4* a = reinterpret_cast<const uint4*>(codes + kv.codes_at(layer, from, 0) + at);
+    uint4* b = reinterpret_cast<uint4*>(codes + kv.codes_at(layer, to, 0) + at);
+    const int n = min(MOVE_BYTES, bytes - at) / 16;
+    uint4 x[MOVE_BYTES / 16 / COPY];
+#pragma unroll
+    for (int i = 0; i < MOVE_BYTES / 16 / COPY; ++i) {
+      const int e = i * COPY + threadIdx.x;
+      if (e < n) x[i] = __ldcs(a + e);
+    }
+    if (at == 0) {
       float* scale = is_v ? kv.c.v_scale : kv.c.k_scale;
-      for (int64_t e = threadIdx.x; e < scales; e += COPY)
+      for (int e = threadIdx.x; e < scales; e += COPY)
         scale[kv.scales_at(layer, to, 0) + e] = scale[kv.scales_at(layer, from, 0) + e];
+    }
+    if (j + gridDim.x < all) {
+      from = w.from[(j + gridDim.x) / per_page];
+      to = w.to[(j + gridDim.x) / per_page];
+    }
+#pragma unroll
+    for (int i = 0; i < MOVE_BYTES / 16 / COPY; ++i) {
+      const int e = i * COPY + threadIdx.x;
+      if (e < n) __stcs(b + e, x[i]);
     }
   }
 }
@@ -407,7 +429,7 @@ cudaError_t launch_kv_compact(const KvView& kv, int32_t* used, void* workspace, 
   k_kv_compact<<<1, ONE, 0, s>>>(kv, w, used);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
-  if ((e = launch_maybe_pdl(true, k_kv_move, dim3(sms * 8), dim3(COPY), 0, s, kv, w)) != cudaSuccess) return e;
+  if ((e = launch_maybe_pdl(true, k_kv_move, dim3(sms * MOVE_PER_SM), dim3(COPY), 0, s, kv, w)) != cudaSuccess) return e;
   const int64_t entries = kv.c.slots * kv.c.max_pages;
   return launch_maybe_pdl(true, k_kv_rename, dim3((unsigned)std::min<int64_t>((entries + COPY - 1) / COPY, sms * 8)),
                           dim3(COPY), 0, s, kv, w);
