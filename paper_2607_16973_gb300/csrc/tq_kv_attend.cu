@@ -50,6 +50,7 @@ constexpr int ITEM_UNITS = 4;    // what an item costs beside its blocks (lookin
 // they stay under 2^15, fp16's largest, and those down to 2^-24 of the largest
 // one keep all of fp16's bits.
 constexpr float LEAD = 10.0f, LAZY = 5.0f;
+constexpr int AHEAD = 3;         // blocks of a warp on their way to L2 beyond the one on its way to registers
 constexpr float LN2 = 0.6931471805599453f, LOG2E = 1.4426950408889634f;
 
 struct AttendArgs {
@@ -219,10 +220,9 @@ __device__ __forceinline__ void to_half4(uint32_t w, uint32_t& lo, uint32_t& hi)
     x.h = __hsub2(x.h, bias);
     hi = x.r;
   } else {
-    const __half2_raw a = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w & 0xFFFFu), __NV_E4M3);
-    const __half2_raw b = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w >> 16), __NV_E4M3);
-    lo = (uint32_t)a.y << 16 | a.x;
-    hi = (uint32_t)b.y << 16 | b.x;
+    asm("{\n .reg .b16 a, b;\n mov.b32 {a, b}, %2;\n cvt.rn.f16x2.e4m3x2 %0, a;\n cvt.rn.f16x2.e4m3x2 %1, b;\n}"
+        : "=r"(lo), "=r"(hi)
+        : "r"(w));
   }
 }
 
@@ -407,11 +407,23 @@ __global__ __launch_bounds__(THREADS, D == 256 ? 2 : NT == 1 ? 4 : 3) void k_kv_
           }
         }
     };
+    // a block's keys are 2 or 4 KB in one piece, its values too: half of the lanes
+    // fetch each, 128 bytes apart
+    auto fetch = [&](int64_t ln) {
+      const uint8_t* p = (lane < 16 ? kv.c.k : kv.c.v) + ln * (kKvBlock * D) + (lane & 15) * 128;
+#pragma unroll
+      for (int x = 0; x < kKvBlock * D; x += 2048)
+        if (x + (lane & 15) * 128 < kKvBlock * D) asm volatile("prefetch.global.L2 [%0];" ::"l"(p + x));
+    };
     const int steps = (blk_end - blk - warp + WARPS - 1) / WARPS;  // (<= 0: none)
     int64_t now = -1;
     if (steps > 0) {
       look_up(0);
       now = __shfl_sync(FULL, line, 0);
+      for (int x = 1; x <= AHEAD; ++x) {
+        const int64_t ln = __shfl_sync(FULL, line, x);
+        if (ln >= 0) fetch(ln);
+      }
       if (now >= 0) {
         load_k(now);
         load_v(now);
@@ -423,6 +435,9 @@ __global__ __launch_bounds__(THREADS, D == 256 ? 2 : NT == 1 ? 4 : 3) void k_kv_
       if (it + 1 < steps) {
         if (((it + 1) & 31) == 0) look_up(it + 1);
         next = __shfl_sync(FULL, line, (it + 1) & 31);
+        // (not past the 32 that are looked up, whose first ones are loaded without)
+        const int64_t ln = __shfl_sync(FULL, line, (it + 1 + AHEAD) & 31);
+        if (((it + 1) & 31) + AHEAD < 32 && ln >= 0) fetch(ln);
       }
       const int b = blk + warp + it * WARPS;
       float s[NT][4];
