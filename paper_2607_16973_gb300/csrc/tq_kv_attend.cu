@@ -25,186 +25,27 @@
 // The softmax keeps a reference m per row that only moves when a score passes
 // the one it was set to by LAZY: most blocks need no reduction over the warp.
 //
-// Work: (sequence, tile of rows, key head) items of 16-token blocks, laid end to
-// end and cut into equal runs, one for each block of threads, so that ragged
-// batches and single long sequences load every SM alike.  A run's ends are
-// written as partial sums (m, l, O) and joined, in a fixed order, by
-// k_kv_join.
-//
 // Bound: HBM, 2 (D + 1/4) bytes per token and key head.
 #include <algorithm>
 
-#include "tq_kv.cuh"
-#include "tq_topk.cuh"
+#include "tq_kv_attend.cuh"
 
 namespace tq {
 namespace {
 
 constexpr int WARPS = 4;
 constexpr int THREADS = WARPS * 32;
-constexpr int CHUNK = 1024;      // sequences whose units are kept in shared memory at a time
-constexpr int MIN_UNITS = 4;     // blocks that are worth a block of threads
-constexpr int ITEM_UNITS = 4;    // what an item costs beside its blocks (looking it up, its queries, its sums), in blocks
 // Weights are held as 2^(s - m) with the reference m LEAD below the largest score
 // that it was last set to, and moved again when a score passes that by LAZY:
 // they stay under 2^15, fp16's largest, and those down to 2^-24 of the largest
 // one keep all of fp16's bits.
 constexpr float LEAD = 10.0f, LAZY = 5.0f;
 constexpr int AHEAD = 3;         // blocks of a warp on their way to L2 beyond the one on its way to registers
-constexpr float LN2 = 0.6931471805599453f, LOG2E = 1.4426950408889634f;
 
-struct AttendArgs {
-  KvView kv;
-  int layer;
-  const int32_t *slots, *starts;
-  int64_t n, total;
-  KvRows q;
-  int heads, group;
-  float scale;
-  int window;
-  void* out;
-  float* lse;
-  float* parts;   // [2 * grid][rows * (D + 2)]: partial O, m, l
-  struct Split* splits;  // [grid]
-};
-
-// The item that a run continues, left for k_kv_join by the first run that does.
-struct Split {
-  int first, last;      // runs that have a part of it; first = -1: none to join
-  int token, head;      // first token of its sequence, its key head
-  int64_t row0, rows;   // first row of its tile, rows of its sequence
-};
-
-template <typename T> __device__ __forceinline__ T from_float(float x);
-template <> __device__ __forceinline__ __half from_float<__half>(float x) { return __float2half_rn(x); }
-template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
-
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-
-// What a sequence brings: its rows, and the blocks that any of them sees.
-struct SeqWork {
-  KvSeq s;
-  int64_t tiles;
-  int first_block, blocks;
-  int units;                // of each item: ITEM_UNITS, then one for each block
-  bool ok;
-};
-
-template <int ROWS>
-__device__ __forceinline__ SeqWork seq_work(const AttendArgs& a, int64_t i) {
-  SeqWork w;
-  w.ok = kv_seq(a.kv, a.slots, a.starts, i, a.total, true, w.s);
-  if (!w.ok) {
-    w.s.len = 0;
-    if (w.s.token < 0 || w.s.count < 0 || w.s.count > a.total || w.s.token > a.total - w.s.count) w.s.count = 0;
-  }
-  w.tiles = ((int64_t)w.s.count * a.group + ROWS - 1) / ROWS;
-  const int place = w.s.len - w.s.count;
-  const int lo = a.window ? max(0, place - a.window + 1) : 0;
-  w.first_block = lo / kKvBlock;
-  w.blocks = max(0, (w.s.len + kKvBlock - 1) / kKvBlock - w.first_block);
-  w.units = ITEM_UNITS + w.blocks;
-  return w;
-}
-
-template <int ROWS>
-__device__ __forceinline__ int64_t seq_units(const AttendArgs& a, int64_t i) {
-  const SeqWork w = seq_work<ROWS>(a, i);
-  if (!w.ok && blockIdx.x == 0) kv_status(a.kv, kKvBadEntry);
-  return w.tiles * a.kv.c.kv_heads * w.units;
-}
-
-// The units of all sequences, found by a whole block: `before` holds the sums in
-// front of sequences base .. base + CHUNK.
-struct Units {
-  int64_t before[CHUNK + 1];
-  int64_t warp_sums[WARPS];
-  int64_t base, total;
-};
-
-template <int ROWS>
-__device__ void load_chunk(const AttendArgs& a, Units& u, int64_t base, int64_t sum) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  for (int j0 = 0; j0 < CHUNK; j0 += THREADS) {
-    const int64_t i = base + j0 + threadIdx.x;
-    if (base + j0 >= a.n && j0) break;
-    const int64_t mine = i < a.n ? seq_units<ROWS>(a, i) : 0;
-    int64_t run = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int64_t y = __shfl_up_sync(FULL, run, o);
-      if (lane >= o) run += y;
-    }
-    if (lane == 31) u.warp_sums[warp] = run;
-    __syncthreads();
-    int64_t front = 0, all = 0;
-#pragma unroll
-    for (int w = 0; w < WARPS; ++w) {
-      if (w < warp) front += u.warp_sums[w];
-      all += u.warp_sums[w];
-    }
-    u.before[j0 + threadIdx.x] = sum + front + run - mine;
-    if (threadIdx.x == THREADS - 1) u.before[j0 + THREADS] = sum + all;
-    sum += all;
-    __syncthreads();
-  }
-  if (threadIdx.x == 0) {
-    u.base = base;
-    u.total = sum;
-  }
-  __syncthreads();
-}
-
-// Sets u up for the whole call (its total), the first chunk loaded last.
-template <int ROWS>
-__device__ int64_t load_units(const AttendArgs& a, Units& u) {
-  load_chunk<ROWS>(a, u, 0, 0);
-  if (a.n <= CHUNK) return u.total;
-  int64_t sum = u.total;
-  for (int64_t base = CHUNK; base < a.n; base += CHUNK) {
-    load_chunk<ROWS>(a, u, base, sum);
-    sum = u.total;
-  }
-  load_chunk<ROWS>(a, u, 0, 0);
-  return sum;
-}
-
-// The sequence that unit x falls into, and the sum in front of it; x does not go
-// back behind the chunk that is loaded.
-template <int ROWS>
-__device__ int64_t find_unit(const AttendArgs& a, Units& u, int64_t x, int64_t& before) {
-  while (x >= u.total) load_chunk<ROWS>(a, u, u.base + CHUNK, u.total);  // (uniform: x and u are the block's)
-  const int64_t count = min((int64_t)CHUNK, a.n - u.base);
-  const int64_t j = warp_last_not_above(count, x, [&](int64_t i) { return u.before[i]; });
-  before = u.before[j];
-  return u.base + j;
-}
-
-// Blocks of threads that share `units`, and the first unit of one of them.
-__device__ __forceinline__ int64_t runs(int64_t units, int64_t grid) {
-  return max((int64_t)1, min(grid, units / MIN_UNITS));
-}
-__device__ __forceinline__ int64_t run_start(int64_t c, int64_t units, int64_t n) { return c * units / n; }
-// The last run that starts at or in front of a unit, the first at or behind it.
-__device__ __forceinline__ int64_t last_run(int64_t unit, int64_t units, int64_t n) { return ((unit + 1) * n - 1) / units; }
-__device__ __forceinline__ int64_t first_run(int64_t unit, int64_t units, int64_t n) { return (unit * n + units - 1) / units; }
-
-// Where run c really starts: not within MIN_UNITS of an item's ends, but at that
-// end.  Items of less than 2 MIN_UNITS blocks are never cut, so that a short
-// sequence's result does not depend on the others of its batch.
-template <int ROWS>
-__device__ int64_t cut(const AttendArgs& a, Units& u, int64_t c, int64_t units, int64_t n) {
-  const int64_t x = run_start(c, units, n);
-  if (x >= units) return units;
-  int64_t before;
-  const int64_t i = find_unit<ROWS>(a, u, x, before);
-  const int64_t item = seq_work<ROWS>(a, i).units, in = (x - before) % item;
-  return in < ITEM_UNITS + MIN_UNITS ? x - in : item - in < MIN_UNITS ? x - in + item : x;
-}
+// Rows come in tiles of 8 or 16; a run is worth 4 blocks, and an item costs about as
+// much as 4 blocks beside its own (looking it up, its queries, its sums).
+template <int NT>
+using StreamCut = Cut<8 * NT, kKvBlock, 4, 4>;
 
 // Two pairs of fp16 values from the four codes of a word: every code is exact.
 template <int CODES>
@@ -254,7 +95,8 @@ struct Piece {  // what a lane loads of a row: K pieces of 16 bytes, V pieces of
 
 template <typename T, int D, int CODES, int NT>
 __global__ __launch_bounds__(THREADS, D == 256 ? 2 : NT == 1 ? 4 : 3) void k_kv_attend(AttendArgs a) {
-  constexpr int ROWS = 8 * NT;
+  using P = StreamCut<NT>;
+  constexpr int ROWS = P::ROWS;
   constexpr int KP = Piece<D>::K, VP = Piece<D>::V, VW = Piece<D>::VW;
   constexpr int MT = D / 16;  // m-tiles of O^T
   __shared__ Units units;
@@ -263,34 +105,16 @@ __global__ __launch_bounds__(THREADS, D == 256 ? 2 : NT == 1 ? 4 : 3) void k_kv_
 
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
   const KvView& kv = a.kv;
-  const int kv_heads = kv.c.kv_heads;
   griddep_launch_dependents();
-  const int64_t all = load_units<ROWS>(a, units);
-  const int64_t n_runs = runs(all, gridDim.x);
-  if (threadIdx.x == 0) a.splits[blockIdx.x].first = -1;
-  if (blockIdx.x >= n_runs) return;
-  int64_t u = cut<ROWS>(a, units, blockIdx.x, all, n_runs);
-  const int64_t chunk = units.base, chunk_sum = units.before[0];
-  const int64_t end = cut<ROWS>(a, units, blockIdx.x + 1, all, n_runs);
-  if (units.base != chunk) load_chunk<ROWS>(a, units, chunk, chunk_sum);  // (uniform)
+  int64_t all, n_runs, u, end;
+  if (!my_run<P>(a, units, all, n_runs, u, end)) return;
 
   while (u < end) {
-    int64_t before;
-    const int64_t i = find_unit<ROWS>(a, units, u, before);
-    const SeqWork w = seq_work<ROWS>(a, i);
-    const int64_t item = (u - before) / w.units;
-    const int in = (int)((u - before) % w.units);
-    const int b_first = max(0, in - ITEM_UNITS);
-    const int b_last = (int)min((int64_t)w.blocks, in + (end - u) - ITEM_UNITS);
-    u += ITEM_UNITS + b_last - in;
-    const int head = (int)(item % kv_heads);
-    const int64_t row0 = item / kv_heads * ROWS, rows = (int64_t)w.s.count * a.group;
-    if (b_first && threadIdx.x == 0) {
-      const int64_t begin = before + item * w.units;
-      const int first = (int)first_run(begin + ITEM_UNITS + MIN_UNITS, all, n_runs) - 1;
-      if (first + 1 == (int)blockIdx.x)
-        a.splits[blockIdx.x] = {first, (int)last_run(begin + w.units - MIN_UNITS, all, n_runs), w.s.token, head, row0, rows};
-    }
+    const Segment seg = next_segment<P>(a, units, all, n_runs, u, end);
+    const KvSeq& sq = seg.it.s;
+    const Span& span = seg.it.span;
+    const int head = seg.it.head;
+    const int64_t row0 = seg.row0, rows = seg.rows;
 
     // the queries, scaled by a power of two to fp16's middle: row n = g of each 8
     uint32_t qf[NT][KP * 4][2];
@@ -300,7 +124,7 @@ __global__ __launch_bounds__(THREADS, D == 256 ? 2 : NT == 1 ? 4 : 3) void k_kv_
     for (int nt = 0; nt < NT; ++nt) {
       const int64_t row = row0 + nt * 8 + g;
       const bool real = row < rows;
-      const int64_t token = w.s.token + row / a.group;
+      const int64_t token = sq.token + row / a.group;
       const T* p = static_cast<const T*>(a.q.p) + token * a.q.token_stride +
                    (int64_t)(head * a.group + (int)(row % a.group)) * a.q.head_stride + 16 * t;
       union { uint4 v[2]; T e[16]; } x[KP];
@@ -338,19 +162,13 @@ __global__ __launch_bounds__(THREADS, D == 256 ? 2 : NT == 1 ? 4 : 3) void k_kv_
       for (int h = 0; h < 2; ++h) {
         unscale[nt][h] = __shfl_sync(FULL, down, (2 * t + h) * 4);
         const int64_t r = row0 + nt * 8 + 2 * t + h;
-        place[nt][h] = r < rows ? w.s.len - w.s.count + (int)(r / a.group) : -1;
+        place[nt][h] = r < rows ? sq.len - sq.count + (int)(r / a.group) : -1;
       }
     }
-    // the blocks of this run that some row of the tile sees
-    const int64_t last_row = min(rows, row0 + ROWS) - 1;
-    const int place_hi = w.s.len - w.s.count + (int)(last_row / a.group);
-    const int place_lo = w.s.len - w.s.count + (int)(row0 / a.group);
-    int blk = w.first_block + b_first, blk_end = w.first_block + b_last;
-    if (a.window) blk = max(blk, max(0, place_lo - a.window + 1) / kKvBlock);
-    blk_end = min(blk_end, place_hi < 0 ? 0 : place_hi / kKvBlock + 1);
+    const int blk = span.first + seg.b_first, blk_end = span.first + seg.b_last;
     // blocks that every row of the tile sees whole
-    const int whole_from = a.window ? max(0, place_hi - a.window + kKvBlock) / kKvBlock : 0;
-    const int whole_to = place_lo >= 0 ? (place_lo + 1) / kKvBlock : 0;
+    const int whole_from = a.window ? max(0, span.place_hi - a.window + kKvBlock) / kKvBlock : 0;
+    const int whole_to = span.place_lo >= 0 ? (span.place_lo + 1) / kKvBlock : 0;
 
     float o[NT][MT][4], m[NT][2], l[NT][2];
 #pragma unroll
@@ -363,7 +181,7 @@ __global__ __launch_bounds__(THREADS, D == 256 ? 2 : NT == 1 ? 4 : 3) void k_kv_
 
     // This warp's blocks: blk + warp, + WARPS, ...; lane l looks up the page and the
     // scales of the l-th of 32 of them.
-    const int32_t* table = kv.c.table + w.s.slot * kv.c.max_pages;
+    const int32_t* table = kv.c.table + sq.slot * kv.c.max_pages;
     int64_t line = -1;      // first row (token) of lane's block in the pool, in units of 16 tokens
     float ks = 0.0f, vs = 0.0f;
     auto look_up = [&](int it) {
@@ -498,7 +316,7 @@ __global__ __launch_bounds__(THREADS, D == 256 ? 2 : NT == 1 ? 4 : 3) void k_kv_
           // bytes that no token owns may be NaN, and 0 times that is not 0
 #pragma unroll
           for (int r = 0; r < 4; ++r)
-            if (b * kKvBlock + 2 * t + (r & 1) + (r >> 1) * 8 >= w.s.len) {
+            if (b * kKvBlock + 2 * t + (r & 1) + (r >> 1) * 8 >= sq.len) {
 #pragma unroll
               for (int c = 0; c < VP; ++c)
 #pragma unroll
@@ -563,8 +381,7 @@ __global__ __launch_bounds__(THREADS, D == 256 ? 2 : NT == 1 ? 4 : 3) void k_kv_
       }
     __syncthreads();
     // joined; whole items go to the output, the others to the partial sums
-    const bool is_whole = b_first == 0 && b_last == w.blocks;
-    float* part = a.parts + ((int64_t)blockIdx.x * 2 + (b_first == 0)) * (ROWS * (D + 2));
+    float* part = part_of<D, ROWS>(a, seg);
     for (int row = threadIdx.x / 32; row < ROWS; row += WARPS) {
       if (row0 + row >= rows) break;
       float top = -INFINITY, sum = 0.0f, f[WARPS];
@@ -575,8 +392,7 @@ __global__ __launch_bounds__(THREADS, D == 256 ? 2 : NT == 1 ? 4 : 3) void k_kv_
         f[x] = top == -INFINITY ? 0.0f : ex2(sh_m[x][row] - top);
         sum += f[x] * sh_l[x][row];
       }
-      const int64_t r = row0 + row;
-      const int64_t at = (w.s.token + r / a.group) * a.heads + head * a.group + r % a.group;
+      const int64_t at = out_row(a, sq.token, head, row0 + row);
       const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
       for (int d = lane * 2; d < D; d += 64) {
         float y0 = 0.0f, y1 = 0.0f;
@@ -586,7 +402,7 @@ __global__ __launch_bounds__(THREADS, D == 256 ? 2 : NT == 1 ? 4 : 3) void k_kv_
           y0 += f[x] * z.x;
           y1 += f[x] * z.y;
         }
-        if (is_whole) {
+        if (seg.whole) {
           T* out = static_cast<T*>(a.out) + at * D + d;
           out[0] = from_float<T>(y0 * inv);
           out[1] = from_float<T>(y1 * inv);
@@ -595,11 +411,11 @@ __global__ __launch_bounds__(THREADS, D == 256 ? 2 : NT == 1 ? 4 : 3) void k_kv_
         }
       }
       if (lane == 0) {
-        if (!is_whole) {
+        if (!seg.whole) {
           part[ROWS * D + row] = top;
           part[ROWS * (D + 1) + row] = sum;
         } else if (a.lse) {
-          a.lse[at] = sum > 0.0f ? top * LN2 + logf(sum) : -INFINITY;
+          a.lse[at] = lse_of(top, sum);
         }
       }
     }
@@ -607,109 +423,53 @@ __global__ __launch_bounds__(THREADS, D == 256 ? 2 : NT == 1 ? 4 : 3) void k_kv_
   }
 }
 
-// Joins the items that several runs share: a block per run that continues one,
-// and row.
-template <typename T, int D, int ROWS>
-__global__ __launch_bounds__(THREADS) void k_kv_join(AttendArgs a) {
-  constexpr int LANES = D / 4, GROUPS = THREADS / LANES;  // a thread sums 4 elements over every GROUPS-th part
-  __shared__ float4 sh_o[GROUPS][LANES];
-  __shared__ float sh_l[GROUPS];
-  griddep_wait();
-  const Split sp = a.splits[blockIdx.x];
-  const int row = blockIdx.y;
-  const int64_t r = sp.row0 + row;
-  if (sp.first < 0 || r >= sp.rows) return;
-  const int first = sp.first, last = sp.last;
-  const int group = threadIdx.x / LANES, at = threadIdx.x % LANES;
-  auto part = [&](int x) { return a.parts + ((int64_t)x * 2 + (x == first)) * (ROWS * (D + 2)); };
-  float top = -INFINITY;
-  for (int x = first + (threadIdx.x & 31); x <= last; x += 32) top = fmaxf(top, part(x)[ROWS * D + row]);
-#pragma unroll
-  for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(FULL, top, o));
-  float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  float sum = 0.0f;
-  if (top > -INFINITY) {
-#pragma unroll 4
-    for (int x = first + group; x <= last; x += GROUPS) {
-      const float* p = part(x);
-      const float f = ex2(p[ROWS * D + row] - top);
-      const float4 z = *reinterpret_cast<const float4*>(p + row * D + 4 * at);
-      sum += f * p[ROWS * (D + 1) + row];
-      y.x += f * z.x, y.y += f * z.y, y.z += f * z.z, y.w += f * z.w;
-    }
-  }
-  sh_o[group][at] = y;
-  if (at == 0) sh_l[group] = sum;
-  __syncthreads();
-  if (group) return;
-#pragma unroll
-  for (int x = 1; x < GROUPS; ++x) {
-    const float4 z = sh_o[x][at];
-    y.x += z.x, y.y += z.y, y.z += z.z, y.w += z.w;
-    sum += sh_l[x];
-  }
-  const int64_t o = (sp.token + r / a.group) * a.heads + sp.head * a.group + r % a.group;
-  const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
-  T* out = static_cast<T*>(a.out) + o * D + 4 * at;
-  out[0] = from_float<T>(y.x * inv), out[1] = from_float<T>(y.y * inv);
-  out[2] = from_float<T>(y.z * inv), out[3] = from_float<T>(y.w * inv);
-  if (a.lse && at == 0) a.lse[o] = sum > 0.0f ? top * LN2 + logf(sum) : -INFINITY;
-}
-
-// Workspace: Split [grid] | partial sums.
-size_t split_bytes(int grid) { return ((size_t)grid * sizeof(Split) + 255) / 256 * 256; }
-
 constexpr int per_sm(int dim, int nt) { return dim == 256 ? 2 : nt == 1 ? 4 : 3; }
 
-// Rows of a tile: 16 where the sequences bring more than 8 on average and the
+// Tiles of 16 rows where the sequences bring more than 8 on average and the
 // accumulators of 16 fit (head_dim up to 128).
 int row_tiles_of(const KvView& kv, int64_t n, int64_t total, int heads) {
-  const int64_t rows = (total + n - 1) / n * (heads / kv.c.kv_heads);
+  const int64_t rows = n ? (total + n - 1) / n * (heads / kv.c.kv_heads) : 0;
   return rows > 8 && kv.c.head_dim <= 128 ? 2 : 1;
 }
 
 template <typename T, int D, int NT>
-cudaError_t attend(AttendArgs a, cudaStream_t s) {
+cudaError_t attend(AttendArgs a, void* workspace, cudaStream_t s) {
   const int grid = device_sm_count() * per_sm(D, NT);
-  a.splits = reinterpret_cast<Split*>(a.parts);
-  a.parts += split_bytes(grid) / sizeof(float);
+  take_workspace(a, grid, workspace);
   (a.kv.c.codes == TQ_KV_INT8 ? k_kv_attend<T, D, TQ_KV_INT8, NT> : k_kv_attend<T, D, TQ_KV_E4M3, NT>)<<<grid, THREADS, 0, s>>>(a);
-  cudaError_t e = cudaGetLastError();
+  const cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
-  return launch_maybe_pdl(true, k_kv_join<T, D, 8 * NT>, dim3(grid, 8 * NT), dim3(THREADS), 0, s, a);
+  return launch_join<T, D, 8 * NT>(a, grid, s);
 }
 
 template <typename T>
-cudaError_t attend_for(const AttendArgs& a, int nt, cudaStream_t s) {
+cudaError_t attend_for(const AttendArgs& a, int nt, void* workspace, cudaStream_t s) {
   switch (a.kv.c.head_dim) {
     case 64:
-      return nt == 1 ? attend<T, 64, 1>(a, s) : attend<T, 64, 2>(a, s);
+      return (nt == 1 ? attend<T, 64, 1> : attend<T, 64, 2>)(a, workspace, s);
     case 128:
-      return nt == 1 ? attend<T, 128, 1>(a, s) : attend<T, 128, 2>(a, s);
+      return (nt == 1 ? attend<T, 128, 1> : attend<T, 128, 2>)(a, workspace, s);
     default:
-      return attend<T, 256, 1>(a, s);
+      return attend<T, 256, 1>(a, workspace, s);
   }
 }
 
 }  // namespace
 
-size_t kv_attend_workspace(const KvView& kv, int64_t, int64_t, int) {
-  const int dim = kv.c.head_dim;
-  size_t need = 0;
-  for (int nt = 1; nt <= 2; ++nt) {
-    const int grid = device_sm_count() * per_sm(dim, nt);
-    need = std::max(need, split_bytes(grid) + (size_t)grid * 2 * 8 * nt * (dim + 2) * sizeof(float));
-  }
-  return need;
+size_t kv_attend_workspace(const KvView& kv, int64_t n, int64_t total, int heads) {
+  if (kv_tile_supported(kv, n, total, heads)) return kv_tile_workspace(kv);
+  const int nt = row_tiles_of(kv, n, total, heads);
+  return attend_workspace(device_sm_count() * per_sm(kv.c.head_dim, nt), 8 * nt, kv.c.head_dim);
 }
 
 cudaError_t launch_kv_attend(const KvView& kv, int layer, const int32_t* slots, const int32_t* starts, int64_t n,
                              const KvRows& q, int type, int64_t total, int heads, float scale, int window, void* out,
                              float* lse, void* workspace, cudaStream_t s) {
-  const AttendArgs a = {kv, layer, slots, starts, n, total, q, heads, heads / kv.c.kv_heads, scale, window, out, lse,
-                        static_cast<float*>(workspace), nullptr};
+  AttendArgs a = {kv, layer, slots, starts, n, total, q, heads, heads / kv.c.kv_heads, scale, window, out, lse,
+                  nullptr, nullptr};
+  if (kv_tile_supported(kv, n, total, heads)) return launch_kv_tile(a, type, workspace, s);
   const int nt = row_tiles_of(kv, n, total, heads);
-  return type == TQ_BF16 ? attend_for<__nv_bfloat16>(a, nt, s) : attend_for<__half>(a, nt, s);
+  return type == TQ_BF16 ? attend_for<__nv_bfloat16>(a, nt, workspace, s) : attend_for<__half>(a, nt, workspace, s);
 }
 
 }  // namespace tq

@@ -104,13 +104,6 @@ __host__ __device__ constexpr uint32_t tm_idesc(int N) {
   return (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(TM_M >> 4) << 24);
 }
 
-// warp_wait whose usual case, a phase already complete, is one poll per lane.
-__device__ __forceinline__ bool all_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int* err,
-                                         int where) {
-  if (__all_sync(FULL, mbar_try_wait(bar, parity))) return true;
-  return warp_wait(bar, parity, abort_flag, err, where);
-}
-
 __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
