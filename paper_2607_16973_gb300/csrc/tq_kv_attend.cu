@@ -100,21 +100,20 @@ __global__ __launch_bounds__(THREADS, D == 256 ? 2 : NT == 1 ? 4 : 3) void k_kv_
   constexpr int KP = Piece<D>::K, VP = Piece<D>::V, VW = Piece<D>::VW;
   constexpr int MT = D / 16;  // m-tiles of O^T
   __shared__ Units units;
+  __shared__ Run run;
   __shared__ float sh_o[WARPS][ROWS][D + 4];
   __shared__ float sh_m[WARPS][ROWS], sh_l[WARPS][ROWS];
 
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
   const KvView& kv = a.kv;
   griddep_launch_dependents();
-  int64_t all, n_runs, u, end;
-  if (!my_run<P>(a, units, all, n_runs, u, end)) return;
+  if (!my_run<P>(a, units, run)) return;
 
-  while (u < end) {
-    const Segment seg = next_segment<P>(a, units, all, n_runs, u, end);
-    const KvSeq& sq = seg.it.s;
-    const Span& span = seg.it.span;
-    const int head = seg.it.head;
-    const int64_t row0 = seg.row0, rows = seg.rows;
+  while (run.u < run.end) {
+    next_segment<P>(a, units, run);
+    const KvSeq sq = run.seg.it.s;
+    const Span span = run.seg.it.span;
+    const int head = run.seg.it.head, row0 = run.seg.row0, rows = run.seg.rows;
 
     // the queries, scaled by a power of two to fp16's middle: row n = g of each 8
     uint32_t qf[NT][KP * 4][2];
@@ -122,11 +121,11 @@ __global__ __launch_bounds__(THREADS, D == 256 ? 2 : NT == 1 ? 4 : 3) void k_kv_
     int place[NT][2];             // last token that they see; -1: none
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      const int64_t row = row0 + nt * 8 + g;
+      const int row = row0 + nt * 8 + g;
       const bool real = row < rows;
       const int64_t token = sq.token + row / a.group;
       const T* p = static_cast<const T*>(a.q.p) + token * a.q.token_stride +
-                   (int64_t)(head * a.group + (int)(row % a.group)) * a.q.head_stride + 16 * t;
+                   (int64_t)(head * a.group + row % a.group) * a.q.head_stride + 16 * t;
       union { uint4 v[2]; T e[16]; } x[KP];
       float top = 0.0f;
 #pragma unroll
@@ -161,11 +160,11 @@ __global__ __launch_bounds__(THREADS, D == 256 ? 2 : NT == 1 ? 4 : 3) void k_kv_
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         unscale[nt][h] = __shfl_sync(FULL, down, (2 * t + h) * 4);
-        const int64_t r = row0 + nt * 8 + 2 * t + h;
-        place[nt][h] = r < rows ? sq.len - sq.count + (int)(r / a.group) : -1;
+        const int r = row0 + nt * 8 + 2 * t + h;
+        place[nt][h] = r < rows ? sq.len - sq.count + r / a.group : -1;
       }
     }
-    const int blk = span.first + seg.b_first, blk_end = span.first + seg.b_last;
+    const int blk = span.first + run.seg.b_first, blk_end = span.first + run.seg.b_last;
     // blocks that every row of the tile sees whole
     const int whole_from = a.window ? max(0, span.place_hi - a.window + kKvBlock) / kKvBlock : 0;
     const int whole_to = span.place_lo >= 0 ? (span.place_lo + 1) / kKvBlock : 0;
@@ -182,7 +181,7 @@ __global__ __launch_bounds__(THREADS, D == 256 ? 2 : NT == 1 ? 4 : 3) void k_kv_
     // This warp's blocks: blk + warp, + WARPS, ...; lane l looks up the page and the
     // scales of the l-th of 32 of them.
     const int32_t* table = kv.c.table + sq.slot * kv.c.max_pages;
-    int64_t line = -1;      // first row (token) of lane's block in the pool, in units of 16 tokens
+    int line = -1;  // lane's block in the pool (they are of 1 KB at least: 2^31 of them are more than any memory)
     float ks = 0.0f, vs = 0.0f;
     auto look_up = [&](int it) {
       const int b = blk + warp + (it + lane) * WARPS;
@@ -191,7 +190,7 @@ __global__ __launch_bounds__(THREADS, D == 256 ? 2 : NT == 1 ? 4 : 3) void k_kv_
         const int64_t tok = (int64_t)b * kKvBlock;
         const int page = table[tok >> kv.page_shift];
         if (page >= 0 && page < kv.c.pages) {
-          line = kv.scales_at(a.layer, page, head) + ((tok & (kv.c.page_tokens - 1)) / kKvBlock);
+          line = (int)(kv.scales_at(a.layer, page, head) + ((tok & (kv.c.page_tokens - 1)) / kKvBlock));
           ks = __ldg(kv.c.k_scale + line);
           vs = __ldg(kv.c.v_scale + line);
         } else {
@@ -201,16 +200,16 @@ __global__ __launch_bounds__(THREADS, D == 256 ? 2 : NT == 1 ? 4 : 3) void k_kv_
     };
     uint4 kr[KP][2];
     uint32_t vr[VP][4][VW];
-    auto load_k = [&](int64_t ln) {
-      const uint8_t* p = kv.c.k + ln * (kKvBlock * D) + g * D + 16 * t;
+    auto load_k = [&](int ln) {
+      const uint8_t* p = kv.c.k + (int64_t)ln * (kKvBlock * D) + g * D + 16 * t;
 #pragma unroll
       for (int c = 0; c < KP; ++c) {
         kr[c][0] = __ldg(reinterpret_cast<const uint4*>(p + 64 * c));
         kr[c][1] = __ldg(reinterpret_cast<const uint4*>(p + 64 * c + 8 * D));
       }
     };
-    auto load_v = [&](int64_t ln) {
-      const uint8_t* p = kv.c.v + ln * (kKvBlock * D) + 2 * t * D + (D == 64 ? 8 : 16) * g;
+    auto load_v = [&](int ln) {
+      const uint8_t* p = kv.c.v + (int64_t)ln * (kKvBlock * D) + 2 * t * D + (D == 64 ? 8 : 16) * g;
 #pragma unroll
       for (int c = 0; c < VP; ++c)
 #pragma unroll
@@ -227,19 +226,19 @@ __global__ __launch_bounds__(THREADS, D == 256 ? 2 : NT == 1 ? 4 : 3) void k_kv_
     };
     // a block's keys are 2 or 4 KB in one piece, its values too: half of the lanes
     // fetch each, 128 bytes apart
-    auto fetch = [&](int64_t ln) {
-      const uint8_t* p = (lane < 16 ? kv.c.k : kv.c.v) + ln * (kKvBlock * D) + (lane & 15) * 128;
+    auto fetch = [&](int ln) {
+      const uint8_t* p = (lane < 16 ? kv.c.k : kv.c.v) + (int64_t)ln * (kKvBlock * D) + (lane & 15) * 128;
 #pragma unroll
       for (int x = 0; x < kKvBlock * D; x += 2048)
         if (x + (lane & 15) * 128 < kKvBlock * D) asm volatile("prefetch.global.L2 [%0];" ::"l"(p + x));
     };
     const int steps = (blk_end - blk - warp + WARPS - 1) / WARPS;  // (<= 0: none)
-    int64_t now = -1;
+    int now = -1;
     if (steps > 0) {
       look_up(0);
       now = __shfl_sync(FULL, line, 0);
       for (int x = 1; x <= AHEAD; ++x) {
-        const int64_t ln = __shfl_sync(FULL, line, x);
+        const int ln = __shfl_sync(FULL, line, x);
         if (ln >= 0) fetch(ln);
       }
       if (now >= 0) {
@@ -249,12 +248,12 @@ __global__ __launch_bounds__(THREADS, D == 256 ? 2 : NT == 1 ? 4 : 3) void k_kv_
     }
     for (int it = 0; it < steps; ++it) {
       const float k_scale = __shfl_sync(FULL, ks, it & 31), v_scale = __shfl_sync(FULL, vs, it & 31);
-      int64_t next = -1;
+      int next = -1;
       if (it + 1 < steps) {
         if (((it + 1) & 31) == 0) look_up(it + 1);
         next = __shfl_sync(FULL, line, (it + 1) & 31);
         // (not past the 32 that are looked up, whose first ones are loaded without)
-        const int64_t ln = __shfl_sync(FULL, line, (it + 1 + AHEAD) & 31);
+        const int ln = __shfl_sync(FULL, line, (it + 1 + AHEAD) & 31);
         if (((it + 1) & 31) + AHEAD < 32 && ln >= 0) fetch(ln);
       }
       const int b = blk + warp + it * WARPS;
@@ -381,9 +380,10 @@ __global__ __launch_bounds__(THREADS, D == 256 ? 2 : NT == 1 ? 4 : 3) void k_kv_
       }
     __syncthreads();
     // joined; whole items go to the output, the others to the partial sums
-    float* part = part_of<D, ROWS>(a, seg);
+    const Segment& done = run.seg;
+    float* part = part_of<D, ROWS>(a, done);
     for (int row = threadIdx.x / 32; row < ROWS; row += WARPS) {
-      if (row0 + row >= rows) break;
+      if (done.row0 + row >= done.rows) break;
       float top = -INFINITY, sum = 0.0f, f[WARPS];
 #pragma unroll
       for (int x = 0; x < WARPS; ++x) top = fmaxf(top, sh_m[x][row]);
@@ -392,7 +392,7 @@ __global__ __launch_bounds__(THREADS, D == 256 ? 2 : NT == 1 ? 4 : 3) void k_kv_
         f[x] = top == -INFINITY ? 0.0f : ex2(sh_m[x][row] - top);
         sum += f[x] * sh_l[x][row];
       }
-      const int64_t at = out_row(a, sq.token, head, row0 + row);
+      const int64_t at = out_row(a, done.it.s.token, done.it.head, done.row0 + row);
       const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
       for (int d = lane * 2; d < D; d += 64) {
         float y0 = 0.0f, y1 = 0.0f;
@@ -402,7 +402,7 @@ __global__ __launch_bounds__(THREADS, D == 256 ? 2 : NT == 1 ? 4 : 3) void k_kv_
           y0 += f[x] * z.x;
           y1 += f[x] * z.y;
         }
-        if (seg.whole) {
+        if (done.whole) {
           T* out = static_cast<T*>(a.out) + at * D + d;
           out[0] = from_float<T>(y0 * inv);
           out[1] = from_float<T>(y1 * inv);
@@ -411,7 +411,7 @@ __global__ __launch_bounds__(THREADS, D == 256 ? 2 : NT == 1 ? 4 : 3) void k_kv_
         }
       }
       if (lane == 0) {
-        if (!seg.whole) {
+        if (!done.whole) {
           part[ROWS * D + row] = top;
           part[ROWS * (D + 1) + row] = sum;
         } else if (a.lse) {
@@ -419,6 +419,8 @@ __global__ __launch_bounds__(THREADS, D == 256 ? 2 : NT == 1 ? 4 : 3) void k_kv_
         }
       }
     }
+    __syncthreads();
+    if (threadIdx.x == 0) run.u = done.next;
     __syncthreads();
   }
 }
@@ -465,7 +467,7 @@ size_t kv_attend_workspace(const KvView& kv, int64_t n, int64_t total, int heads
 cudaError_t launch_kv_attend(const KvView& kv, int layer, const int32_t* slots, const int32_t* starts, int64_t n,
                              const KvRows& q, int type, int64_t total, int heads, float scale, int window, void* out,
                              float* lse, void* workspace, cudaStream_t s) {
-  AttendArgs a = {kv, layer, slots, starts, n, total, q, heads, heads / kv.c.kv_heads, scale, window, out, lse,
+  AttendArgs a = {kv, layer, slots, starts, n, total, q, false, heads, heads / kv.c.kv_heads, scale, window, out, lse,
                   nullptr, nullptr};
   if (kv_tile_supported(kv, n, total, heads)) return launch_kv_tile(a, type, workspace, s);
   const int nt = row_tiles_of(kv, n, total, heads);

@@ -22,6 +22,7 @@ struct AttendArgs {
   const int32_t *slots, *starts;
   int64_t n, total;
   KvRows q;
+  bool q_wide;           // every row of q starts on a 16-byte boundary
   int heads, group;
   float scale;
   int window;
@@ -35,7 +36,7 @@ struct AttendArgs {
 struct Split {
   int first, last;      // runs that have a part of it; first = -1: none to join
   int token, head;      // first token of its sequence, its key head
-  int64_t row0, rows;   // first row of its tile, rows of its sequence
+  int row0, rows;       // first row of its tile, rows of its sequence
 };
 
 // The tensor-core tiles (tq_kv_tile.cu).
@@ -73,14 +74,21 @@ struct Span {
 };
 
 template <class P>
-__device__ __forceinline__ Span tile_span(const AttendArgs& a, const KvSeq& s, int64_t tile) {
+__device__ __forceinline__ Span tile_span(const AttendArgs& a, const KvSeq& s, int tile) {
   Span w;
-  const int64_t last = min((int64_t)s.count * a.group, (tile + 1) * P::ROWS) - 1;
-  w.place_lo = s.len - s.count + (int)(tile * P::ROWS / a.group);
-  w.place_hi = s.len - s.count + (int)(last / a.group);
+  const unsigned group = (unsigned)a.group, row0 = (unsigned)tile * P::ROWS;
+  const unsigned last = min((unsigned)s.count * group, row0 + P::ROWS) - 1;
+  w.place_lo = s.len - s.count + (int)(row0 / group);
+  w.place_hi = s.len - s.count + (int)(last / group);
   w.first = a.window ? max(0, w.place_lo - a.window + 1) / P::BLOCK : 0;
   w.blocks = w.place_hi < 0 ? 0 : max(0, w.place_hi / P::BLOCK + 1 - w.first);
   return w;
+}
+
+// (rows of a sequence fit in 31 bits: the call's queries times heads do)
+template <class P>
+__device__ __forceinline__ int tiles_of(const AttendArgs& a, const KvSeq& s) {
+  return (int)(((unsigned)s.count * (unsigned)a.group + P::ROWS - 1) / P::ROWS);
 }
 
 // Sums of the sequences' units, found by a whole block: before[i] is what lies
@@ -108,8 +116,8 @@ __device__ void load_chunk(const AttendArgs& a, Units& u, int64_t base, int64_t 
           if (s.token < 0 || s.count < 0 || s.count > a.total || s.token > a.total - s.count) s.count = 0;
         }
         u.seq[j] = s;
-        const int64_t tiles = ((int64_t)s.count * a.group + P::ROWS - 1) / P::ROWS;
-        for (int64_t t = 0; t < tiles; ++t) mine += P::ITEM + tile_span<P>(a, s, t).blocks;
+        const int tiles = tiles_of<P>(a, s);
+        for (int t = 0; t < tiles; ++t) mine += P::ITEM + tile_span<P>(a, s, t).blocks;
         mine *= a.kv.c.kv_heads;
       }
       run = mine;
@@ -152,32 +160,51 @@ __device__ int64_t load_units(const AttendArgs& a, Units& u) {
   return sum;
 }
 
-// The item that unit x falls into; x does not go back behind the chunk that is
-// loaded.
+// The item that unit x falls into, found by a warp; the chunk with x is loaded.
 struct Item {
   KvSeq s;
   Span span;
-  int64_t begin, tile;  // its first unit
-  int head, units;
+  int64_t begin;  // its first unit
+  int tile, head, units;
 };
 
 template <class P>
-__device__ Item find_item(const AttendArgs& a, Units& u, int64_t x) {
-  while (x >= u.total) load_chunk<P>(a, u, u.base + CHUNK, u.total);  // (uniform: x and u are the block's)
+__device__ Item find_item(const AttendArgs& a, const Units& u, int64_t x) {
+  const int lane = threadIdx.x & 31;
   const int64_t i = warp_last_not_above(min((int64_t)CHUNK, a.n - u.base), x, [&](int64_t j) { return u.before[j]; });
   Item it;
   it.s = u.seq[i];
+  const int tiles = tiles_of<P>(a, it.s);
   int64_t in = x - u.before[i];
-  for (it.tile = 0;; ++it.tile) {
-    it.span = tile_span<P>(a, it.s, it.tile);
-    it.units = P::ITEM + it.span.blocks;
-    const int64_t all = (int64_t)it.units * a.kv.c.kv_heads;
-    if (in < all) break;
-    in -= all;
+  for (int base = 0;; base += 32) {  // a tile per lane
+    const int64_t mine = base + lane < tiles ? (int64_t)(P::ITEM + tile_span<P>(a, it.s, base + lane).blocks) * a.kv.c.kv_heads : 0;
+    int64_t upto = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t y = __shfl_up_sync(FULL, upto, o);
+      if (lane >= o) upto += y;
+    }
+    const unsigned past = __ballot_sync(FULL, upto > in);
+    if (past || base + 32 >= tiles) {
+      const int at = past ? __ffs(past) - 1 : 0;
+      in -= __shfl_sync(FULL, upto - mine, at);
+      it.tile = base + at;
+      break;
+    }
+    in -= __shfl_sync(FULL, upto, 31);
   }
+  it.span = tile_span<P>(a, it.s, it.tile);
+  it.units = P::ITEM + it.span.blocks;
   it.head = (int)(in / it.units);
   it.begin = x - in % it.units;
   return it;
+}
+
+// Loads the chunk that unit x falls into; x does not go back behind the one that is
+// loaded.  By the whole block.
+template <class P>
+__device__ __forceinline__ void chunk_of(const AttendArgs& a, Units& u, int64_t x) {
+  while (x >= u.total) load_chunk<P>(a, u, u.base + CHUNK, u.total);  // (uniform: x and u are the block's)
 }
 
 // Runs that share `units`; where run c starts if nothing is in the way; the last
@@ -197,55 +224,77 @@ template <class P>
 __device__ int64_t run_cut(const AttendArgs& a, Units& u, int64_t c, int64_t units, int64_t n) {
   const int64_t x = run_start(c, units, n);
   if (x >= units) return units;
+  chunk_of<P>(a, u, x);
   const Item it = find_item<P>(a, u, x);
   const int64_t in = x - it.begin;
   return in < P::ITEM + P::MIN ? it.begin : it.units - in < P::MIN ? it.begin + it.units : x;
 }
 
-// This block's run [u, end): false if it has none.  Leaves the chunk of its start
-// loaded, and its entry of `splits` empty.
-template <class P>
-__device__ bool my_run(const AttendArgs& a, Units& units, int64_t& all, int64_t& n_runs, int64_t& u, int64_t& end) {
-  all = load_units<P>(a, units);
-  n_runs = runs<P>(all, gridDim.x);
-  if (threadIdx.x == 0) a.splits[blockIdx.x].first = -1;
-  if (blockIdx.x >= n_runs) return false;
-  u = run_cut<P>(a, units, blockIdx.x, all, n_runs);
-  const int64_t chunk = units.base, sum = units.before[0];
-  end = run_cut<P>(a, units, blockIdx.x + 1, all, n_runs);
-  if (units.base != chunk) load_chunk<P>(a, units, chunk, sum);  // (uniform)
-  return u < end;
-}
-
-// Takes the next segment of the run: blocks [b_first, b_last) of an item, those of
-// a whole item if both are its ends.  Notes an item that this run is the first to
-// continue.
+// A segment of a run: blocks [b_first, b_last) of an item, a whole item if both are
+// its ends.
 struct Segment {
   Item it;
   int b_first, b_last;
   bool whole;
-  int64_t row0, rows;
+  int row0, rows;
+  int64_t next;  // the unit behind it
 };
 
+// A block's run [u, end), in shared memory: what is only needed between segments
+// takes no registers within them.
+struct Run {
+  int64_t all, n_runs, u, end;
+  Segment seg;
+};
+
+// Sets this block's run up: false if it has none.  Leaves the chunk of its start
+// loaded, and its entry of `splits` empty.
 template <class P>
-__device__ __forceinline__ Segment next_segment(const AttendArgs& a, Units& units, int64_t all, int64_t n_runs, int64_t& u,
-                                                int64_t end) {
-  Segment g;
-  g.it = find_item<P>(a, units, u);
-  const int in = (int)(u - g.it.begin);
-  g.b_first = max(0, in - P::ITEM);
-  g.b_last = (int)min((int64_t)g.it.span.blocks, in + (end - u) - P::ITEM);
-  g.whole = g.b_first == 0 && g.b_last == g.it.span.blocks;
-  g.row0 = g.it.tile * P::ROWS;
-  g.rows = (int64_t)g.it.s.count * a.group;
-  u += P::ITEM + g.b_last - in;
-  if (g.b_first && threadIdx.x == 0) {
-    const int first = (int)first_run(g.it.begin + P::ITEM + P::MIN, all, n_runs) - 1;
-    if (first + 1 == (int)blockIdx.x)
-      a.splits[blockIdx.x] = {first,    (int)last_run(g.it.begin + g.it.units - P::MIN, all, n_runs),
-                              g.it.s.token, g.it.head, g.row0, g.rows};
+__device__ bool my_run(const AttendArgs& a, Units& units, Run& run) {
+  const int64_t all = load_units<P>(a, units), n_runs = runs<P>(all, gridDim.x);
+  if (threadIdx.x == 0) a.splits[blockIdx.x].first = -1;
+  if (blockIdx.x >= n_runs) return false;
+  const int64_t u = run_cut<P>(a, units, blockIdx.x, all, n_runs);
+  const int64_t chunk = units.base, sum = units.before[0];
+  const int64_t end = run_cut<P>(a, units, blockIdx.x + 1, all, n_runs);
+  if (units.base != chunk) load_chunk<P>(a, units, chunk, sum);  // (uniform)
+  if (threadIdx.x == 0) {
+    run.all = all;
+    run.n_runs = n_runs;
+    run.u = u;
+    run.end = end;
   }
-  return g;
+  __syncthreads();
+  return u < end;
+}
+
+// Finds the next segment of the run, in run.seg; the caller moves run.u on, behind
+// a barrier.  Notes an item that this run is the first to continue.
+template <class P>
+__device__ __forceinline__ void next_segment(const AttendArgs& a, Units& units, Run& run) {
+  chunk_of<P>(a, units, run.u);
+  if (threadIdx.x < 32) {
+    const int64_t u = run.u;
+    Segment g;
+    g.it = find_item<P>(a, units, u);
+    const int in = (int)(u - g.it.begin);
+    g.b_first = max(0, in - P::ITEM);
+    g.b_last = (int)min((int64_t)g.it.span.blocks, in + (run.end - u) - P::ITEM);
+    g.whole = g.b_first == 0 && g.b_last == g.it.span.blocks;
+    g.row0 = g.it.tile * P::ROWS;
+    g.rows = g.it.s.count * a.group;
+    g.next = u + P::ITEM + g.b_last - in;
+    if (threadIdx.x == 0) {
+      run.seg = g;
+      if (g.b_first) {
+        const int first = (int)first_run(g.it.begin + P::ITEM + P::MIN, run.all, run.n_runs) - 1;
+        if (first + 1 == (int)blockIdx.x)
+          a.splits[blockIdx.x] = {first,         (int)last_run(g.it.begin + g.it.units - P::MIN, run.all, run.n_runs),
+                                  g.it.s.token, g.it.head, g.row0, g.rows};
+      }
+    }
+  }
+  __syncthreads();
 }
 
 // Where this segment's partial sums go: a run has one that continues an item at
@@ -255,8 +304,8 @@ __device__ __forceinline__ float* part_of(const AttendArgs& a, const Segment& g)
   return a.parts + ((int64_t)blockIdx.x * 2 + (g.b_first == 0)) * (ROWS * (D + 2));
 }
 // Output row (token, head) of row r of a sequence.
-__device__ __forceinline__ int64_t out_row(const AttendArgs& a, int token, int head, int64_t r) {
-  return (token + r / a.group) * a.heads + head * a.group + r % a.group;
+__device__ __forceinline__ int64_t out_row(const AttendArgs& a, int token, int head, int r) {
+  return (int64_t)(token + r / a.group) * a.heads + head * a.group + r % a.group;
 }
 __device__ __forceinline__ float lse_of(float m, float l) { return l > 0.0f ? m * LN2 + logf(l) : -INFINITY; }
 
@@ -278,7 +327,7 @@ __global__ __launch_bounds__(join_warps(D) * 32) void k_kv_join(AttendArgs a) {
   const int row0 = blockIdx.y * 8;
   if (sp.first < 0 || sp.row0 + row0 >= sp.rows) return;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int live = (int)min((int64_t)8, sp.rows - sp.row0 - row0);
+  const int live = min(8, sp.rows - sp.row0 - row0);
   auto part = [&](int x) { return a.parts + ((int64_t)x * 2 + (x == sp.first)) * (ROWS * (D + 2)); };
   float o[8][E], m[8], l[8];
 #pragma unroll

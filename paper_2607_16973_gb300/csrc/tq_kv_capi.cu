@@ -118,7 +118,7 @@ static tq_status check_attend(const char* fn, const tq::KvView& kv, int64_t n, i
   TRY(check_entries(fn, kv, n));
   if (heads < 1 || heads % kv.c.kv_heads)
     return fail(TQ_EINVAL, "%s: heads=%d is not a multiple of kv_heads=%d", fn, heads, kv.c.kv_heads);
-  if (total < 0 || total > INT32_MAX - 1 || heads > INT32_MAX / 64 || total * heads > (int64_t)INT32_MAX * 4)
+  if (total < 0 || total > INT32_MAX - 1 || total * heads > INT32_MAX)
     return fail(TQ_EINVAL, "%s: total=%lld queries of %d heads are too many", fn, (long long)total, heads);
   return TQ_OK;
 }

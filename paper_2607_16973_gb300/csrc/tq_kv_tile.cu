@@ -10,20 +10,21 @@
 // between the blocks' scales; the softmax's own sum is taken of the same numbers,
 // per block, divided by g.  (g below 2^-100 counts as 2^-100.)
 //
-// One CTA per SM, 13 warps:
+// One CTA per SM, 12 warps (168 registers each):
 //   0-7   softmax: warps 0-3 the first 128 rows, 4-7 the others; a thread per row.
-//         S is read from tensor memory twice, for the maximum and for the
-//         weights, 16 columns (one block of tokens, one scale) at a time; P goes
-//         back over the columns of S as the A operand of the second product.
+//         S is read from tensor memory 64 columns at a time (four blocks of
+//         tokens), half of it twice; P goes back over the columns of S as the A
+//         operand of the second product.
 //         The reference m only moves when a weight passes it by 2^15; then the row's
 //         O is scaled in tensor memory (LEAD, LAZY: as in tq_kv_attend.cu).
+//         The first warp of each four issues their MMAs: P V once all four have
+//         written P, then, when that product is complete (S and P share columns),
+//         the scores of the next tokens.  While one row tile's softmax runs, the
+//         other's products do.
 //   8-11  converters: codes from HBM to registers (the next half tile's loads
 //         go out before the present one is converted), to keys [token][d] and
 //         values transposed to [d][token] in fp16, both K-major with a 128-byte
 //         swizzle, two stages each.
-//   12    issues the MMAs.  While one 128 rows' softmax runs, the other's products
-//         do: S and P of a row tile share their columns, so S of the next tokens
-//         waits for the product that reads P.
 //
 // Tensor memory (512 columns): S/P of the two row tiles, 128 each, O of the two.
 //
@@ -38,10 +39,11 @@
 namespace tq {
 namespace {
 
-constexpr int SOFT = 8, CONV = 4, ISSUE = SOFT + CONV;  // warps
-constexpr int TILE_THREADS = (ISSUE + 1) * 32;
+constexpr int SOFT = 8, CONV = 4;  // warps
+constexpr int TILE_THREADS = (SOFT + CONV) * 32;
 constexpr int TOKENS = 128;
 constexpr float LEAD = 10.0f, LAZY = 5.0f;
+constexpr int AHEAD = 3;       // tiles on their way to L2 (less than four: see the converters' look-ups)
 constexpr int SCALE_RING = 4;  // tiles whose scales are held (two being converted, two in the softmax)
 
 // A run is worth a tile of tokens; an item costs about as much as two beside its own.
@@ -56,10 +58,12 @@ struct TileSmem {
 
 struct TileShared {  // behind the operands
   Units units;
+  Run run;
   // of a tile's blocks: K's scale, log2 of V's, 1 / V's; a block without tokens, or
   // one that cannot be read, has 0, -inf, 0
   float scales[SCALE_RING][3][8];
-  uint64_t q_full, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_full[2], fin;
+  float unscale[256];  // factor of a row's scores, in log2 units
+  uint64_t q_full[2], k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_full[2], fin;
   uint32_t tmem;
   int abort_flag, err;
 };
@@ -77,9 +81,22 @@ __device__ __forceinline__ void mma_f16_ss(uint32_t d, uint64_t a, uint64_t b, u
       ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate));
 }
 
-__device__ __forceinline__ void tmem_put8(uint32_t at, const uint32_t (&r)[8]) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
-               ::"r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+__device__ __forceinline__ void tmem_put32(uint32_t at, const uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+      "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
+      "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
+      ::"r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
+        "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
+        "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+      : "memory");
+}
+// Four floats of shared memory that another warp has written, read here and now.
+__device__ __forceinline__ void lds4(const float* p, float (&x)[4]) {
+  asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];"
+               : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3])
+               : "r"(smem_u32(p))
                : "memory");
 }
 __device__ __forceinline__ void tmem_put16(uint32_t at, const uint32_t (&r)[16]) {
@@ -89,6 +106,12 @@ __device__ __forceinline__ void tmem_put16(uint32_t at, const uint32_t (&r)[16])
       ::"r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
         "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
+}
+// Ties registers of a load to the wait in front of this (see tmem_wait16).
+__device__ __forceinline__ void tmem_hold16(uint32_t (&r)[16]) {
+  asm volatile(""
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                 "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]));
 }
 __device__ __forceinline__ void tmem_wait_put() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
@@ -131,13 +154,13 @@ __global__ __launch_bounds__(TILE_THREADS, 1) void k_kv_tile(AttendArgs a) {
 
   griddep_launch_dependents();
   if (threadIdx.x == 0) {
-    mbar_init(&sh.q_full, SOFT);
-    mbar_init(&sh.fin, 1);
+    mbar_init(&sh.fin, 2);
     for (int i = 0; i < 2; ++i) {
       mbar_init(sh.k_full + i, CONV);
       mbar_init(sh.v_full + i, CONV);
-      mbar_init(sh.k_empty + i, 1);
-      mbar_init(sh.v_empty + i, 1);
+      mbar_init(sh.q_full + i, SOFT / 2);
+      mbar_init(sh.k_empty + i, 2);  // (both row tiles' products; one's twice where it is alone)
+      mbar_init(sh.v_empty + i, 2);
       mbar_init(sh.s_full + i, 1);
       mbar_init(sh.p_full + i, SOFT / 2);
       mbar_init(sh.o_full + i, 1);
@@ -146,10 +169,9 @@ __global__ __launch_bounds__(TILE_THREADS, 1) void k_kv_tile(AttendArgs a) {
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   __syncthreads();
-  int64_t all, n_runs, u, end;
-  if (!my_run<P>(a, sh.units, all, n_runs, u, end)) return;  // (the whole block)
+  if (!my_run<P>(a, sh.units, sh.run)) return;  // (the whole block)
 
-  if (warp == ISSUE) {
+  if (warp == SOFT) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&sh.tmem)));
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
   }
@@ -162,160 +184,249 @@ __global__ __launch_bounds__(TILE_THREADS, 1) void k_kv_tile(AttendArgs a) {
 
   // Tiles done by this CTA, and by its second row tile: their barriers' phases.
   int done = 0, done2 = 0, segments = 0;
-  while (u < end) {
-    const Segment seg = next_segment<P>(a, sh.units, all, n_runs, u, end);
-    const KvSeq& sq = seg.it.s;
-    const Span& span = seg.it.span;
+  while (sh.run.u < sh.run.end) {
+    next_segment<P>(a, sh.units, sh.run);
+    const Segment& seg = sh.run.seg;
+    const KvSeq sq = seg.it.s;
     const int head = seg.it.head;
-    const int tiles = seg.b_last - seg.b_first, first = span.first + seg.b_first;  // tiles of tokens
+    const int tiles = seg.b_last - seg.b_first, first = seg.it.span.first + seg.b_first;  // tiles of tokens
     const bool two = seg.rows - seg.row0 > 128;
 
     if (warp < SOFT) {
       // ------------------------------------------------------------ softmax
       const int w = warp >> 2, row = (warp & 3) * 32 + lane;
-      const int64_t r = seg.row0 + w * 128 + row;
+      const int r = seg.row0 + w * 128 + row;
       const bool real = r < seg.rows;
-      float unscale = 0.0f;
       if (w == 0 || two) {
-        // the row of queries, scaled so that its largest element lies in [2^8, 2^9)
-        const T* p = static_cast<const T*>(a.q.p) + (sq.token + r / a.group) * a.q.token_stride +
-                     (int64_t)(head * a.group + (int)(r % a.group)) * a.q.head_stride;
-        const bool wide = ((uintptr_t)p & 15) == 0;
-        union {
+        // The warp's 32 rows of queries, D / 8 lanes to a row, each row scaled so that
+        // its largest element lies in [2^8, 2^9).
+        constexpr int LANES = D / 8, STEP = 32 / LANES;
+        const int c = lane % LANES;
+        union Chunk {
           uint4 v;
           T e[8];
-        } x;
-        auto load = [&](int c) {
-          x.v = make_uint4(0, 0, 0, 0);
-          if (!real) return;
-          if (wide) {
-            x.v = __ldg(reinterpret_cast<const uint4*>(p + 8 * c));
-          } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x.e[e] = p[8 * c + e];
-          }
         };
-        float top = 0.0f;
+        auto put_row = [&](int y, const Chunk& in) {
+          float top = 0.0f;
 #pragma unroll
-        for (int c = 0; c < D / 8; ++c) {
-          load(c);
+          for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(to_float(in.e[e])));
 #pragma unroll
-          for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(to_float(x.e[e])));
-        }
-        const int e2 = min(max((int)(__float_as_uint(top) >> 23) - 127, -110), 127);
-        const float up = __uint_as_float((uint32_t)(127 + min(8 - e2, 118)) << 23);
-        unscale = fabsf(a.scale) * LOG2E / up;  // (>= 0: the scale's sign goes with the queries)
-        const float f = a.scale < 0.0f ? -up : up;
-#pragma unroll
-        for (int c = 0; c < D / 8; ++c) {
-          load(c);
+          for (int o = LANES / 2; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(FULL, top, o));
+          const int e2 = min(max((int)(__float_as_uint(top) >> 23) - 127, -110), 127);
+          const float up = __uint_as_float((uint32_t)(127 + min(8 - e2, 118)) << 23);
+          const float f = a.scale < 0.0f ? -up : up;  // (the scale's sign goes with the queries)
           uint32_t h[4];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const __half2 y = __floats2half2_rn(to_float(x.e[2 * e]) * f, to_float(x.e[2 * e + 1]) * f);
-            h[e] = *reinterpret_cast<const uint32_t*>(&y);
-          }
-          *reinterpret_cast<uint4*>(sm + M::q + w * M::Q + (c >> 3) * 16384 + sw128_offset(row, c & 7)) =
+          for (int e = 0; e < 4; ++e) h[e] = pack_fp16(to_float(in.e[2 * e]) * f, to_float(in.e[2 * e + 1]) * f);
+          *reinterpret_cast<uint4*>(sm + M::q + w * M::Q + (c >> 3) * 16384 + sw128_offset(y, c & 7)) =
               make_uint4(h[0], h[1], h[2], h[3]);
+          if (c == 0) sh.unscale[w * 128 + y] = fabsf(a.scale) * LOG2E / up;
+        };
+        int y = (warp & 3) * 32 + lane / LANES;
+        int token = (seg.row0 + w * 128 + y) / a.group, member = (seg.row0 + w * 128 + y) % a.group;
+        auto step = [&]() {  // to the lane's next row; returns the present one's address
+          const T* p = static_cast<const T*>(a.q.p) + (int64_t)(sq.token + token) * a.q.token_stride +
+                       (int64_t)(head * a.group + member) * a.q.head_stride + 8 * c;
+          for (member += STEP; member >= a.group; member -= a.group) ++token;
+          return p;
+        };
+        const int ys = seg.rows - seg.row0 - w * 128;  // (rows from ys on do not exist)
+        if (a.q_wide) {
+#pragma unroll 1
+          for (int half = 0; half < 2; ++half) {  // 16 rows on their way at a time
+            Chunk in[16 / STEP];
+#pragma unroll
+            for (int x = 0; x < 16 / STEP; ++x) {
+              const T* p = step();
+              in[x].v = make_uint4(0, 0, 0, 0);
+              if (y + x * STEP < ys) in[x].v = __ldg(reinterpret_cast<const uint4*>(p));
+            }
+#pragma unroll
+            for (int x = 0; x < 16 / STEP; ++x, y += STEP) put_row(y, in[x]);
+          }
+        } else {
+#pragma unroll 1
+          for (int x = 0; x < 32; x += STEP, y += STEP) {
+            const T* p = step();
+            Chunk in;
+            in.v = make_uint4(0, 0, 0, 0);
+            if (y < ys) {
+#pragma unroll
+              for (int e = 0; e < 8; ++e) in.e[e] = p[e];
+            }
+            put_row(y, in);
+          }
         }
         fence_proxy_async();
       }
       __syncwarp();
-      if (lane == 0) mbar_arrive(&sh.q_full);
+      if (lane == 0) mbar_arrive(sh.q_full + w);
 
       if (w == 0 || two) {
-        const int place = real ? sq.len - sq.count + (int)(r / a.group) : -1;
+        const float unscale = sh.unscale[w * 128 + row];  // (written by this warp)
+        const int place = real ? sq.len - sq.count + r / a.group : -1;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t ts = tmem + lanes + (uint32_t)(w * TOKENS), to = tmem + lanes + (uint32_t)(2 * TOKENS + w * D);
         int phase = w ? done2 : done;
         float m = -INFINITY, l = 0.0f;
+        // what the first warp issues for the four
+        const bool issuer = (warp & 3) == 0;
+        const uint32_t tm = __shfl_sync(FULL, tmem, 0);
+        const uint64_t qd = sw128_desc(__shfl_sync(FULL, smem_u32(sm + M::q), 0)) + (uint64_t)(w * (M::Q >> 4));
+        const uint64_t k0 = sw128_desc(__shfl_sync(FULL, smem_u32(sm + M::k), 0));
+        const uint64_t v0 = sw128_desc(__shfl_sync(FULL, smem_u32(sm + M::v), 0));
+        auto scores = [&](int n) {  // of tile n of this CTA
+          if (elect_one()) {
+            const uint64_t kd = k0 + (uint64_t)((n & 1) * (M::K >> 4));
+#pragma unroll
+            for (int kk = 0; kk < D / 16; ++kk) {
+              const uint64_t off = (uint64_t)((kk >> 2) * (16384 >> 4) + (kk & 3) * 2);
+              mma_f16_ss(tm + (uint32_t)(w * TOKENS), qd + off, kd + off, tile_idesc(TOKENS), kk ? 1u : 0u);
+            }
+            mma_commit(sh.s_full + w);
+            mma_commit(sh.k_empty + (n & 1));
+            if (!two) mma_commit(sh.k_empty + (n & 1));
+          }
+          __syncwarp();
+        };
+        auto values = [&](int n, bool more) {
+          if (elect_one()) {
+            const uint64_t vd = v0 + (uint64_t)((n & 1) * (M::K >> 4));
+#pragma unroll
+            for (int kk = 0; kk < TOKENS / 16; ++kk)
+              mma_f16_ta(tm + (uint32_t)(2 * TOKENS + w * D), tm + (uint32_t)(w * TOKENS + kk * 8),
+                         vd + (uint64_t)((kk >> 2) * (D * 128 >> 4) + (kk & 3) * 2), tile_idesc(D), kk || more ? 1u : 0u);
+            mma_commit(sh.o_full + w);
+            mma_commit(sh.v_empty + (n & 1));
+            if (!two) mma_commit(sh.v_empty + (n & 1));
+          }
+          __syncwarp();
+        };
         bool ok = true;
-        for (int j = 0; j < tiles; ++j, ++phase) {
+        if (issuer && tiles) {
+          ok = all_wait(sh.q_full + w, segments & 1, abort_flag, err, 6) &&
+               all_wait(sh.k_full + (done & 1), (done >> 1) & 1, abort_flag, err, 7);
+          if (ok) {
+            tc_fence_after();
+            scores(done);
+          }
+        }
+        for (int j = 0; ok && j < tiles; ++j, ++phase) {
           if (!(ok = all_wait(sh.s_full + w, phase & 1, abort_flag, err, 1))) break;
           tc_fence_after();
-          const volatile float(*sc)[8] = sh.scales[(done + j) % SCALE_RING];
+          if (__any_sync(FULL, real)) {  // (else P of these lanes is whatever S was: nobody reads their O)
+          const float(*sc)[8] = sh.scales[(done + j) % SCALE_RING];
           const int t0 = (first + j) * TOKENS;
-          // columns [lo, hi) are seen; the warp looks at each only where some row does not see them all
+          // columns [lo, hi) are seen; they are looked at only where some row does not see them all
           const int hi = place - t0 + 1, lo = a.window ? place - a.window + 1 - t0 : 0;
           const bool edge = __any_sync(FULL, real && (hi < TOKENS || lo > 0));
-          float top = -INFINITY;
-          uint32_t r0[16], r1[16];
-          auto block_top = [&](int c, const uint32_t(&x)[16]) {
-            const float f = sc[0][c] * unscale;  // (>= 0)
-            float y = -INFINITY;
+          // Half of S at a time (64 columns, 4 blocks): the second half's maximum, the
+          // first half's, its weights, and the second half read again for its.  P goes
+          // over columns of the first half.
+          uint32_t x[4][16];
+          auto load = [&](int half) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) tmem_ld16_issue(ts + half * 64 + 16 * c, x[c]);
+            tmem_wait16(x[0]);
+#pragma unroll
+            for (int c = 1; c < 4; ++c) tmem_hold16(x[c]);
             if (edge) {
 #pragma unroll
-              for (int i = 0; i < 16; ++i)
-                if (16 * c + i < hi && 16 * c + i >= lo) y = fmaxf(y, __uint_as_float(x[i]) * f);
-            } else {
+              for (int c = 0; c < 4; ++c)
 #pragma unroll
-              for (int i = 0; i < 16; ++i) y = fmaxf(y, __uint_as_float(x[i]));
-              y *= f;
+                for (int i = 0; i < 16; ++i) {
+                  const int at = half * 64 + 16 * c + i;
+                  if (at >= hi || at < lo) x[c][i] = 0xFF800000u;  // -inf
+                }
             }
-            top = fmaxf(top, y + sc[1][c]);
           };
-          tmem_ld16_issue(ts, r0);
+          float f[4], add[4];  // of the half's blocks
+          auto factors = [&](int half) {
+            lds4(sc[0] + half * 4, f);
+            lds4(sc[1] + half * 4, add);
+            // positive even for a zero scale (whose scores are 0), so that -inf stays
 #pragma unroll
-          for (int c = 0; c < 8; c += 2) {
-            tmem_wait16(r0);
-            tmem_ld16_issue(ts + 16 * (c + 1), r1);
-            block_top(c, r0);
-            tmem_wait16(r1);
-            tmem_ld16_issue(ts + 16 * ((c + 2) & 7), r0);  // (at the end the first block again, for the weights)
-            block_top(c + 1, r1);
+            for (int c = 0; c < 4; ++c) f[c] = fmaxf(f[c] * unscale, 1e-30f);
+          };
+          float top = -INFINITY;
+#pragma unroll 1
+          for (int half = 1; half >= 0; --half) {
+            factors(half);
+            load(half);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              float y[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) y[i] = __uint_as_float(x[c][i]);
+#pragma unroll
+              for (int i = 4; i < 16; ++i) y[i & 3] = fmaxf(y[i & 3], __uint_as_float(x[c][i]));
+              top = fmaxf(top, fmaf(fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])), f[c], add[c]));
+            }
           }
           if (__any_sync(FULL, top > m + (LEAD + LAZY))) {
             const float to_m = fmaxf(m, top - LEAD), keep = to_m > m ? ex2(m - to_m) : 1.0f;
             m = to_m;
             l *= keep;
             if (j) {  // O so far, once its product is complete
-              tmem_wait16(r0);
               if (!(ok = all_wait(sh.o_full + w, (phase - 1) & 1, abort_flag, err, 2))) break;
               tc_fence_after();
-#pragma unroll
+#pragma unroll 1
               for (int c = 0; c < D; c += 16) {
-                tmem_ld16_issue(to + c, r0);
-                tmem_wait16(r0);
+                uint32_t y[16];
+                tmem_ld16_issue(to + c, y);
+                tmem_wait16(y);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) r0[i] = __float_as_uint(__uint_as_float(r0[i]) * keep);
-                tmem_put16(to + c, r0);
+                for (int i = 0; i < 16; ++i) y[i] = __float_as_uint(__uint_as_float(y[i]) * keep);
+                tmem_put16(to + c, y);
               }
-              tmem_wait_put();
-              tmem_ld16_issue(ts, r0);
             }
           }
           const float ref = m == -INFINITY ? 0.0f : m;
-          auto weights = [&](int c, const uint32_t(&x)[16]) {
-            const float f = sc[0][c] * unscale, add = sc[1][c] - ref;
-            float sum = 0.0f;
-            uint32_t out[8];
-#pragma unroll
-            for (int i = 0; i < 16; i += 2) {
-              float p0 = ex2(fmaf(__uint_as_float(x[i]), f, add)), p1 = ex2(fmaf(__uint_as_float(x[i + 1]), f, add));
-              if (edge) {
-                const int at = 16 * c + i;
-                if (at >= hi || at < lo) p0 = 0.0f;
-                if (at + 1 >= hi || at + 1 < lo) p1 = 0.0f;
-              }
-              sum += p0 + p1;
-              out[i / 2] = pack_fp16(p0, p1);
+#pragma unroll 1
+          for (int half = 0; half < 2; ++half) {
+            float inv[4];
+            lds4(sc[2] + half * 4, inv);
+            if (half) {
+              factors(1);
+              load(1);
             }
-            l = fmaf(sum, sc[2][c], l);
-            tmem_put8(ts + 8 * c, out);  // (columns of S that have been read)
-          };
+            uint32_t out[32];
 #pragma unroll
-          for (int c = 0; c < 8; c += 2) {
-            tmem_wait16(r0);
-            tmem_ld16_issue(ts + 16 * (c + 1), r1);
-            weights(c, r0);
-            tmem_wait16(r1);
-            if (c + 2 < 8) tmem_ld16_issue(ts + 16 * (c + 2), r0);
-            weights(c + 1, r1);
+            for (int c = 0; c < 4; ++c) {
+              const float to = add[c] - ref;
+              float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+              for (int i = 0; i < 16; i += 2) {
+                const float p0 = ex2(fmaf(__uint_as_float(x[c][i]), f[c], to));
+                const float p1 = ex2(fmaf(__uint_as_float(x[c][i + 1]), f[c], to));
+                sum[i & 2] += p0;
+                sum[(i & 2) + 1] += p1;
+                out[c * 8 + i / 2] = pack_fp16(p0, p1);
+              }
+              l = fmaf((sum[0] + sum[1]) + (sum[2] + sum[3]), inv[c], l);
+            }
+            tmem_put32(ts + half * 32, out);
           }
           tmem_wait_put();
+          }
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(sh.p_full + w);
+          if (issuer) {
+            const int n = done + j, next = (n + 1) & 1;
+            if (!(ok = all_wait(sh.v_full + (n & 1), (n >> 1) & 1, abort_flag, err, 8) &&
+                       all_wait(sh.p_full + w, phase & 1, abort_flag, err, 9)))
+              break;
+            tc_fence_after();
+            values(n, j > 0);
+            if (j + 1 < tiles) {  // the next scores overwrite P: its product has to be complete
+              if (!(ok = all_wait(sh.k_full + next, ((n + 1) >> 1) & 1, abort_flag, err, 10) &&
+                         all_wait(sh.o_full + w, phase & 1, abort_flag, err, 11)))
+                break;
+              tc_fence_after();
+              scores(n + 1);
+            }
+          }
         }
         if (ok && tiles && (ok = all_wait(sh.o_full + w, (phase - 1) & 1, abort_flag, err, 3))) tc_fence_after();
         if (ok && __any_sync(FULL, real)) {
@@ -357,53 +468,66 @@ __global__ __launch_bounds__(TILE_THREADS, 1) void k_kv_tile(AttendArgs a) {
           }
         }
       }
-    } else if (warp < ISSUE) {
+    } else {
       // --------------------------------------------------------- converters
       const int cw = warp - SOFT;
       const int32_t* table = kv.c.table + sq.slot * kv.c.max_pages;
-      // lane b < 8 looks up block b of a tile: its 16 rows in the pool and its scales
-      int64_t line = -1, line_next = -1;
-      float ks = 0.0f, vs = 0.0f, ks_next = 0.0f, vs_next = 0.0f;
+      // Lane l looks up the l-th of the 32 blocks of four tiles: its place in the pool
+      // and its scales; the next four tiles' are looked up while these are converted.
+      struct Lines {
+        int line;  // (blocks are of 1 KB at least: 2^31 of them are more than any memory)
+        float ks, vs;
+      } now, ahead;
       auto look_up = [&](int j) {
-        line_next = -1;
-        ks_next = vs_next = 0.0f;
+        Lines x = {-1, 0.0f, 0.0f};
         const int64_t tok = (int64_t)(first + j) * TOKENS + lane * kKvBlock;
-        if (lane < 8 && j < tiles && tok < sq.len) {
+        if (j + (lane >> 3) < tiles && tok < sq.len) {
           const int page = table[tok >> kv.page_shift];
           if (page >= 0 && page < kv.c.pages) {
-            line_next = kv.scales_at(a.layer, page, head) + ((tok & (kv.c.page_tokens - 1)) / kKvBlock);
-            ks_next = __ldg(kv.c.k_scale + line_next);
-            vs_next = __ldg(kv.c.v_scale + line_next);
+            x.line = (int)(kv.scales_at(a.layer, page, head) + ((tok & (kv.c.page_tokens - 1)) / kKvBlock));
+            x.ks = __ldg(kv.c.k_scale + x.line);
+            x.vs = __ldg(kv.c.v_scale + x.line);
           } else {
             kv_status(kv, kKvBadEntry);
           }
+        }
+        return x;
+      };
+      // A tile's codes on their way to L2: a warp takes half of each of the 8 blocks of K
+      // or V, four lanes a block.
+      auto fetch = [&](int j, int line) {
+        const int ln = __shfl_sync(FULL, line, (j & 3) * 8 + (lane >> 2));
+        if (ln >= 0) {
+          const uint8_t* p = (cw & 1 ? kv.c.v : kv.c.k) + (int64_t)ln * (kKvBlock * D) + ((cw >> 1) * 4 + (lane & 3)) * (D * 2);
+#pragma unroll
+          for (int y = 0; y < D * 2; y += 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(p + y));
         }
       };
       // keys: warp cw takes tokens 32 cw ..; lane: 16-byte piece (lane & 3) of each 64 bytes, token lane >> 2 of 8
       constexpr int KN = D / 64 * 4;
       uint4 kr[KN];
-      auto load_k = [&]() {
+      auto load_k = [&](int j, int line) {
 #pragma unroll
         for (int i = 0; i < KN; ++i) {
           const int tok = cw * 32 + (i & 3) * 8 + (lane >> 2);
-          const int64_t ln = __shfl_sync(FULL, line, tok >> 4);
+          const int64_t ln = __shfl_sync(FULL, line, (j & 3) * 8 + (tok >> 4));
           kr[i] = make_uint4(0, 0, 0, 0);
           if (ln >= 0)
-            kr[i] = __ldg(reinterpret_cast<const uint4*>(kv.c.k + (ln * kKvBlock + (tok & 15)) * D + (i >> 2) * 64 + (lane & 3) * 16));
+            kr[i] = __ldg(reinterpret_cast<const uint4*>(kv.c.k + ((int64_t)ln * kKvBlock + (tok & 15)) * D + (i >> 2) * 64 + (lane & 3) * 16));
         }
       };
       // values: 64 tokens x 64 elements a warp (half of them at head_dim 64: 64 x 32); lane: 8 tokens (lane & 7), VB elements
       constexpr int VB = D / 8;  // bytes of a lane's row: 16 or 8
       const int half = cw >> 1, v_octet = lane & 7, v_el = (cw & 1) * (D / 2) + (lane >> 3) * VB;
       uint32_t vr[8][VB / 4];
-      auto load_v = [&](int j) {
+      auto load_v = [&](int j, int line) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const int tok = half * 64 + v_octet * 8 + i;
-          int64_t ln = __shfl_sync(FULL, line, tok >> 4);
+          int64_t ln = __shfl_sync(FULL, line, (j & 3) * 8 + (tok >> 4));
           // bytes that no token owns may be NaN, and 0 times that is not 0
           if ((first + j) * TOKENS + tok >= sq.len) ln = -1;
-          const uint8_t* p = kv.c.v + (ln * kKvBlock + (tok & 15)) * D + v_el;
+          const uint8_t* p = kv.c.v + ((int64_t)ln * kKvBlock + (tok & 15)) * D + v_el;
 #pragma unroll
           for (int x = 0; x < VB / 4; ++x) vr[i][x] = 0;
           if (ln >= 0) {
@@ -417,20 +541,22 @@ __global__ __launch_bounds__(TILE_THREADS, 1) void k_kv_tile(AttendArgs a) {
           }
         }
       };
-      look_up(0);
-      line = line_next, ks = ks_next, vs = vs_next;
-      if (tiles) load_k();
+      now = look_up(0);
+      ahead = look_up(4);
+      if (tiles) load_k(0, now.line);
+      for (int j = 1; j < AHEAD; ++j) fetch(j, now.line);
       for (int j = 0; j < tiles; ++j) {
         const int n = done + j, st = n & 1;
-        load_v(j);
-        look_up(j + 1);
+        load_v(j, now.line);
+        fetch(j + AHEAD, (j & 3) + AHEAD < 4 ? now.line : ahead.line);
         if (n >= 2 && !all_wait(sh.k_empty + st, ((n >> 1) - 1) & 1, abort_flag, err, 4)) break;
-        if (cw == 0 && lane < 8) {
+        if (cw == 0 && lane >> 3 == (j & 3)) {
           // (the softmax of the tile that had this place in the ring is over: S two tiles on waited for it)
-          const float g = fmaxf(vs, 0x1p-100f);
-          sh.scales[n % SCALE_RING][0][lane] = ks;
-          sh.scales[n % SCALE_RING][1][lane] = line >= 0 ? log2f(g) : -INFINITY;
-          sh.scales[n % SCALE_RING][2][lane] = line >= 0 ? 1.0f / g : 0.0f;
+          const float g = fmaxf(now.vs, 0x1p-100f);
+          float* sc = &sh.scales[n % SCALE_RING][0][lane & 7];
+          sc[0] = now.ks;
+          sc[8] = now.line >= 0 ? log2f(g) : -INFINITY;
+          sc[16] = now.line >= 0 ? 1.0f / g : 0.0f;
         }
         unsigned char* sk = sm + M::k + st * M::K;
 #pragma unroll
@@ -447,8 +573,11 @@ __global__ __launch_bounds__(TILE_THREADS, 1) void k_kv_tile(AttendArgs a) {
         fence_proxy_async();
         __syncwarp();
         if (lane == 0) mbar_arrive(sh.k_full + st);
-        line = line_next, ks = ks_next, vs = vs_next;
-        if (j + 1 < tiles) load_k();
+        if ((j & 3) == 3) {
+          now = ahead;
+          ahead = look_up(j + 5);
+        }
+        if (j + 1 < tiles) load_k(j + 1, now.line);
         if (n >= 2 && !all_wait(sh.v_empty + st, ((n >> 1) - 1) & 1, abort_flag, err, 5)) break;
         unsigned char* sv = sm + M::v + st * M::K + half * (D * 128);
 #pragma unroll
@@ -467,77 +596,6 @@ __global__ __launch_bounds__(TILE_THREADS, 1) void k_kv_tile(AttendArgs a) {
         __syncwarp();
         if (lane == 0) mbar_arrive(sh.v_full + st);
       }
-    } else {
-      // --------------------------------------------------------- MMA issuer
-      const uint32_t tm = __shfl_sync(FULL, tmem, 0);
-      const uint64_t q0 = sw128_desc(__shfl_sync(FULL, smem_u32(sm + M::q), 0));
-      const uint64_t k0 = sw128_desc(__shfl_sync(FULL, smem_u32(sm + M::k), 0));
-      const uint64_t v0 = sw128_desc(__shfl_sync(FULL, smem_u32(sm + M::v), 0));
-      // S of row tile w and tile n of this CTA
-      auto scores = [&](int w, int n) {
-        if (elect_one()) {
-          const uint64_t qd = q0 + (uint64_t)(w * (M::Q >> 4)), kd = k0 + (uint64_t)((n & 1) * (M::K >> 4));
-#pragma unroll
-          for (int kk = 0; kk < D / 16; ++kk) {
-            const uint64_t off = (uint64_t)((kk >> 2) * (16384 >> 4) + (kk & 3) * 2);
-            mma_f16_ss(tm + (uint32_t)(w * TOKENS), qd + off, kd + off, tile_idesc(TOKENS), kk ? 1u : 0u);
-          }
-          mma_commit(sh.s_full + w);
-        }
-        __syncwarp();
-      };
-      auto values = [&](int w, int n, bool more) {
-        if (elect_one()) {
-          const uint64_t vd = v0 + (uint64_t)((n & 1) * (M::K >> 4));
-#pragma unroll
-          for (int kk = 0; kk < TOKENS / 16; ++kk)
-            mma_f16_ta(tm + (uint32_t)(2 * TOKENS + w * D), tm + (uint32_t)(w * TOKENS + kk * 8),
-                       vd + (uint64_t)((kk >> 2) * (D * 128 >> 4) + (kk & 3) * 2), tile_idesc(D), kk || more ? 1u : 0u);
-          mma_commit(sh.o_full + w);
-        }
-        __syncwarp();
-      };
-      auto release = [&](uint64_t* bar) {
-        if (elect_one()) mma_commit(bar);
-        __syncwarp();
-      };
-      bool ok = all_wait(&sh.q_full, segments & 1, abort_flag, err, 6);
-      if (ok && tiles) {
-        ok = all_wait(sh.k_full + (done & 1), (done >> 1) & 1, abort_flag, err, 7);
-        if (ok) {
-          tc_fence_after();
-          scores(0, done);
-          if (two) scores(1, done);
-          release(sh.k_empty + (done & 1));
-        }
-        for (int j = 0; ok && j < tiles; ++j) {
-          const int n = done + j;
-          if (!(ok = all_wait(sh.v_full + (n & 1), (n >> 1) & 1, abort_flag, err, 8) &&
-                     all_wait(sh.p_full, n & 1, abort_flag, err, 9)))
-            break;
-          tc_fence_after();
-          values(0, n, j > 0);
-          if (two) {
-            if (!(ok = all_wait(sh.p_full + 1, (done2 + j) & 1, abort_flag, err, 10))) break;
-            tc_fence_after();
-            values(1, n, j > 0);
-          }
-          release(sh.v_empty + (n & 1));
-          if (j + 1 == tiles) break;
-          // the next scores overwrite P: its product has to be complete
-          if (!(ok = all_wait(sh.k_full + ((n + 1) & 1), ((n + 1) >> 1) & 1, abort_flag, err, 11) &&
-                     all_wait(sh.o_full, n & 1, abort_flag, err, 12)))
-            break;
-          tc_fence_after();
-          scores(0, n + 1);
-          if (two) {
-            if (!(ok = all_wait(sh.o_full + 1, (done2 + j) & 1, abort_flag, err, 13))) break;
-            tc_fence_after();
-            scores(1, n + 1);
-          }
-          release(sh.k_empty + ((n + 1) & 1));
-        }
-      }
     }
     done += tiles;
     if (two) done2 += tiles;
@@ -546,8 +604,10 @@ __global__ __launch_bounds__(TILE_THREADS, 1) void k_kv_tile(AttendArgs a) {
     __syncthreads();
     tc_fence_after();
     if (*abort_flag) break;  // (uniform behind the barrier)
+    if (threadIdx.x == 0) sh.run.u = sh.run.seg.next;
+    __syncthreads();
   }
-  if (warp == ISSUE) {
+  if (warp == 0 || warp == SOFT / 2) {
     if (elect_one()) {  // never leave with MMAs in flight
       mma_commit(&sh.fin);
       mbar_wait_drain(&sh.fin, 0);
@@ -558,7 +618,7 @@ __global__ __launch_bounds__(TILE_THREADS, 1) void k_kv_tile(AttendArgs a) {
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (warp == ISSUE) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+  if (warp == SOFT) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
 }
 
 template <typename T, int D, int CODES>
@@ -593,6 +653,7 @@ size_t kv_tile_workspace(const KvView& kv) {
 cudaError_t launch_kv_tile(AttendArgs a, int type, void* workspace, cudaStream_t s) {
   const int grid = device_sm_count();
   take_workspace(a, grid, workspace);
+  a.q_wide = aligned16(a.q.p) && a.q.token_stride % 8 == 0 && a.q.head_stride % 8 == 0;
   return type == TQ_BF16 ? tile_for<__nv_bfloat16>(a, grid, s) : tile_for<__half>(a, grid, s);
 }
 
