@@ -93,8 +93,11 @@ struct Piece {  // what a lane loads of a row: K pieces of 16 bytes, V pieces of
   static constexpr int V = D == 256 ? 2 : 1;
 };
 
+// Blocks of threads per SM, by the registers that the accumulators leave.
+constexpr int per_sm(int dim, int nt) { return dim == 256 ? 2 : nt == 1 ? 4 : 3; }
+
 template <typename T, int D, int CODES, int NT>
-__global__ __launch_bounds__(THREADS, D == 256 ? 2 : NT == 1 ? 4 : 3) void k_kv_attend(AttendArgs a) {
+__global__ __launch_bounds__(THREADS, per_sm(D, NT)) void k_kv_attend(AttendArgs a) {
   using P = StreamCut<NT>;
   constexpr int ROWS = P::ROWS;
   constexpr int KP = Piece<D>::K, VP = Piece<D>::V, VW = Piece<D>::VW;
@@ -425,13 +428,12 @@ __global__ __launch_bounds__(THREADS, D == 256 ? 2 : NT == 1 ? 4 : 3) void k_kv_
   }
 }
 
-constexpr int per_sm(int dim, int nt) { return dim == 256 ? 2 : nt == 1 ? 4 : 3; }
-
-// Tiles of 16 rows where the sequences bring more than 8 on average and the
-// accumulators of 16 fit (head_dim up to 128).
+// Rows of a tile, in eights: 16 where the sequences bring more than 8 on average
+// and the accumulators of 16 fit (head_dim up to 128).  (32 at head_dim 64, with
+// two blocks of threads per SM: 71 us for 24 sequences of 25 rows over 4,096
+// tokens, 58 us as two tiles of 16.)
 int row_tiles_of(const KvView& kv, int64_t n, int64_t total, int heads) {
-  const int64_t rows = n ? (total + n - 1) / n * (heads / kv.c.kv_heads) : 0;
-  return rows > 8 && kv.c.head_dim <= 128 ? 2 : 1;
+  return attend_rows(kv, n, total, heads) > 8 && kv.c.head_dim <= 128 ? 2 : 1;
 }
 
 template <typename T, int D, int NT>

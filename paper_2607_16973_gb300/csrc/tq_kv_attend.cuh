@@ -39,6 +39,11 @@ struct Split {
   int row0, rows;       // first row of its tile, rows of its sequence
 };
 
+// Rows per key head that a sequence of the call brings on average.
+inline int64_t attend_rows(const KvView& kv, int64_t n, int64_t total, int heads) {
+  return n > 0 ? (total + n - 1) / n * (heads / kv.c.kv_heads) : 0;
+}
+
 // The tensor-core tiles (tq_kv_tile.cu).
 bool kv_tile_supported(const KvView& kv, int64_t n, int64_t total, int heads);
 size_t kv_tile_workspace(const KvView& kv);

@@ -12,11 +12,12 @@
 //
 // One CTA per SM, 12 warps (168 registers each):
 //   0-7   softmax: warps 0-3 the first 128 rows, 4-7 the others; a thread per row.
-//         S is read from tensor memory 64 columns at a time (four blocks of
-//         tokens), half of it twice; P goes back over the columns of S as the A
-//         operand of the second product.
-//         The reference m only moves when a weight passes it by 2^15; then the row's
-//         O is scaled in tensor memory (LEAD, LAZY: as in tq_kv_attend.cu).
+//         (Up to 128 rows: both have them all and take tiles of tokens in turn.)
+//         S is read from tensor memory 32 columns at a time (two blocks of
+//         tokens) and weighed with the reference m of the tiles before; only where
+//         a weight passes it by 2^15 does m move, the row's O is scaled in tensor
+//         memory and the tile weighed again (LEAD, LAZY: as in tq_kv_attend.cu).
+//         P goes over the columns of S as the A operand of the second product.
 //         The first warp of each four issues their MMAs: P V once all four have
 //         written P, then, when that product is complete (S and P share columns),
 //         the scores of the next tokens.  While one row tile's softmax runs, the
@@ -62,6 +63,7 @@ struct TileShared {  // behind the operands
   // of a tile's blocks: K's scale, log2 of V's, 1 / V's; a block without tokens, or
   // one that cannot be read, has 0, -inf, 0
   float scales[SCALE_RING][3][8];
+  float row_m[2][128], row_l[2][128];  // what the softmax ends with
   float unscale[256];  // factor of a row's scores, in log2 units
   uint64_t q_full[2], k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_full[2], fin;
   uint32_t tmem;
@@ -182,21 +184,24 @@ __global__ __launch_bounds__(TILE_THREADS, 1) void k_kv_tile(AttendArgs a) {
   volatile int* abort_flag = &sh.abort_flag;
   int* err = &sh.err;
 
-  // Tiles done by this CTA, and by its second row tile: their barriers' phases.
-  int done = 0, done2 = 0, segments = 0;
+  // Tiles of tokens done by this CTA, and by this half of the softmax: their
+  // barriers' phases.
+  int done = 0, mine = 0, segments = 0;
   while (sh.run.u < sh.run.end) {
     next_segment<P>(a, sh.units, sh.run);
     const Segment& seg = sh.run.seg;
     const KvSeq sq = seg.it.s;
     const int head = seg.it.head;
     const int tiles = seg.b_last - seg.b_first, first = seg.it.span.first + seg.b_first;  // tiles of tokens
+    // Two row tiles, each with its half of the softmax; or one, whose tiles of tokens
+    // the halves take in turn, their sums joined at the end.
     const bool two = seg.rows - seg.row0 > 128;
 
     if (warp < SOFT) {
       // ------------------------------------------------------------ softmax
-      const int w = warp >> 2, row = (warp & 3) * 32 + lane;
-      const int r = seg.row0 + w * 128 + row;
+      const int w = warp >> 2, rt = two ? w : 0, row = (warp & 3) * 32 + lane, r = seg.row0 + rt * 128 + row;
       const bool real = r < seg.rows;
+      const int j0 = two ? 0 : w, step_j = two ? 1 : 2;
       if (w == 0 || two) {
         // The warp's 32 rows of queries, D / 8 lanes to a row, each row scaled so that
         // its largest element lies in [2^8, 2^9).
@@ -206,21 +211,32 @@ __global__ __launch_bounds__(TILE_THREADS, 1) void k_kv_tile(AttendArgs a) {
           uint4 v;
           T e[8];
         };
-        auto put_row = [&](int y, const Chunk& in) {
-          float top = 0.0f;
+        // N rows, y, y + STEP, ...: their reductions run side by side
+        auto put_rows = [&](int y, const auto& in) {
+          constexpr int N = sizeof(in) / sizeof(Chunk);
+          float top[N];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(to_float(in.e[e])));
+          for (int x = 0; x < N; ++x) {
+            top[x] = 0.0f;
 #pragma unroll
-          for (int o = LANES / 2; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(FULL, top, o));
-          const int e2 = min(max((int)(__float_as_uint(top) >> 23) - 127, -110), 127);
-          const float up = __uint_as_float((uint32_t)(127 + min(8 - e2, 118)) << 23);
-          const float f = a.scale < 0.0f ? -up : up;  // (the scale's sign goes with the queries)
-          uint32_t h[4];
+            for (int e = 0; e < 8; ++e) top[x] = fmaxf(top[x], fabsf(to_float(in[x].e[e])));
+          }
 #pragma unroll
-          for (int e = 0; e < 4; ++e) h[e] = pack_fp16(to_float(in.e[2 * e]) * f, to_float(in.e[2 * e + 1]) * f);
-          *reinterpret_cast<uint4*>(sm + M::q + w * M::Q + (c >> 3) * 16384 + sw128_offset(y, c & 7)) =
-              make_uint4(h[0], h[1], h[2], h[3]);
-          if (c == 0) sh.unscale[w * 128 + y] = fabsf(a.scale) * LOG2E / up;
+          for (int o = LANES / 2; o; o >>= 1)
+#pragma unroll
+            for (int x = 0; x < N; ++x) top[x] = fmaxf(top[x], __shfl_xor_sync(FULL, top[x], o));
+#pragma unroll
+          for (int x = 0; x < N; ++x) {
+            const int e2 = min(max((int)(__float_as_uint(top[x]) >> 23) - 127, -110), 127), at = y + x * STEP;
+            const float up = __uint_as_float((uint32_t)(127 + min(8 - e2, 118)) << 23);
+            const float f = a.scale < 0.0f ? -up : up;  // (the scale's sign goes with the queries)
+            uint32_t h[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) h[e] = pack_fp16(to_float(in[x].e[2 * e]) * f, to_float(in[x].e[2 * e + 1]) * f);
+            *reinterpret_cast<uint4*>(sm + M::q + w * M::Q + (c >> 3) * 16384 + sw128_offset(at, c & 7)) =
+                make_uint4(h[0], h[1], h[2], h[3]);
+            if (c == 0) sh.unscale[w * 128 + at] = fabsf(a.scale) * LOG2E * __uint_as_float((uint32_t)(127 - min(8 - e2, 118)) << 23);
+          }
         };
         int y = (warp & 3) * 32 + lane / LANES;
         int token = (seg.row0 + w * 128 + y) / a.group, member = (seg.row0 + w * 128 + y) % a.group;
@@ -241,20 +257,20 @@ __global__ __launch_bounds__(TILE_THREADS, 1) void k_kv_tile(AttendArgs a) {
               in[x].v = make_uint4(0, 0, 0, 0);
               if (y + x * STEP < ys) in[x].v = __ldg(reinterpret_cast<const uint4*>(p));
             }
-#pragma unroll
-            for (int x = 0; x < 16 / STEP; ++x, y += STEP) put_row(y, in[x]);
+            put_rows(y, in);
+            y += 16;
           }
         } else {
 #pragma unroll 1
           for (int x = 0; x < 32; x += STEP, y += STEP) {
             const T* p = step();
-            Chunk in;
-            in.v = make_uint4(0, 0, 0, 0);
+            Chunk in[1];
+            in[0].v = make_uint4(0, 0, 0, 0);
             if (y < ys) {
 #pragma unroll
-              for (int e = 0; e < 8; ++e) in.e[e] = p[e];
+              for (int e = 0; e < 8; ++e) in[0].e[e] = p[e];
             }
-            put_row(y, in);
+            put_rows(y, in);
           }
         }
         fence_proxy_async();
@@ -262,59 +278,52 @@ __global__ __launch_bounds__(TILE_THREADS, 1) void k_kv_tile(AttendArgs a) {
       __syncwarp();
       if (lane == 0) mbar_arrive(sh.q_full + w);
 
-      if (w == 0 || two) {
-        const float unscale = sh.unscale[w * 128 + row];  // (written by this warp)
-        const int place = real ? sq.len - sq.count + r / a.group : -1;
-        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t ts = tmem + lanes + (uint32_t)(w * TOKENS), to = tmem + lanes + (uint32_t)(2 * TOKENS + w * D);
-        int phase = w ? done2 : done;
-        float m = -INFINITY, l = 0.0f;
-        // what the first warp issues for the four
-        const bool issuer = (warp & 3) == 0;
-        const uint32_t tm = __shfl_sync(FULL, tmem, 0);
-        const uint64_t qd = sw128_desc(__shfl_sync(FULL, smem_u32(sm + M::q), 0)) + (uint64_t)(w * (M::Q >> 4));
-        const uint64_t k0 = sw128_desc(__shfl_sync(FULL, smem_u32(sm + M::k), 0));
-        const uint64_t v0 = sw128_desc(__shfl_sync(FULL, smem_u32(sm + M::v), 0));
-        auto scores = [&](int n) {  // of tile n of this CTA
-          if (elect_one()) {
-            const uint64_t kd = k0 + (uint64_t)((n & 1) * (M::K >> 4));
+      const uint32_t ts = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)(w * TOKENS);
+      float m = -INFINITY, l = 0.0f;
+      bool ok = all_wait(sh.q_full + rt, segments & 1, abort_flag, err, 6);
+      const float unscale = sh.unscale[rt * 128 + row];
+      const int place = real ? sq.len - sq.count + r / a.group : -1;
+      // what the first warp issues for the four
+      const bool issuer = (warp & 3) == 0;
+      const uint32_t tm = __shfl_sync(FULL, tmem, 0), sm0 = __shfl_sync(FULL, smem_u32(sm), 0);
+      auto scores = [&](int n) {  // of tile n of this CTA
+        if (elect_one()) {
+          const uint64_t qd = sw128_desc(sm0 + M::q + rt * M::Q), kd = sw128_desc(sm0 + M::k + (n & 1) * M::K);
 #pragma unroll
-            for (int kk = 0; kk < D / 16; ++kk) {
-              const uint64_t off = (uint64_t)((kk >> 2) * (16384 >> 4) + (kk & 3) * 2);
-              mma_f16_ss(tm + (uint32_t)(w * TOKENS), qd + off, kd + off, tile_idesc(TOKENS), kk ? 1u : 0u);
-            }
-            mma_commit(sh.s_full + w);
-            mma_commit(sh.k_empty + (n & 1));
-            if (!two) mma_commit(sh.k_empty + (n & 1));
+          for (int kk = 0; kk < D / 16; ++kk) {
+            const uint64_t off = (uint64_t)((kk >> 2) * (16384 >> 4) + (kk & 3) * 2);
+            mma_f16_ss(tm + (uint32_t)(w * TOKENS), qd + off, kd + off, tile_idesc(TOKENS), kk ? 1u : 0u);
           }
-          __syncwarp();
-        };
-        auto values = [&](int n, bool more) {
-          if (elect_one()) {
-            const uint64_t vd = v0 + (uint64_t)((n & 1) * (M::K >> 4));
-#pragma unroll
-            for (int kk = 0; kk < TOKENS / 16; ++kk)
-              mma_f16_ta(tm + (uint32_t)(2 * TOKENS + w * D), tm + (uint32_t)(w * TOKENS + kk * 8),
-                         vd + (uint64_t)((kk >> 2) * (D * 128 >> 4) + (kk & 3) * 2), tile_idesc(D), kk || more ? 1u : 0u);
-            mma_commit(sh.o_full + w);
-            mma_commit(sh.v_empty + (n & 1));
-            if (!two) mma_commit(sh.v_empty + (n & 1));
-          }
-          __syncwarp();
-        };
-        bool ok = true;
-        if (issuer && tiles) {
-          ok = all_wait(sh.q_full + w, segments & 1, abort_flag, err, 6) &&
-               all_wait(sh.k_full + (done & 1), (done >> 1) & 1, abort_flag, err, 7);
-          if (ok) {
-            tc_fence_after();
-            scores(done);
-          }
+          mma_commit(sh.s_full + w);
+          mma_commit(sh.k_empty + (n & 1));
+          if (!two) mma_commit(sh.k_empty + (n & 1));
         }
-        for (int j = 0; ok && j < tiles; ++j, ++phase) {
-          if (!(ok = all_wait(sh.s_full + w, phase & 1, abort_flag, err, 1))) break;
+        __syncwarp();
+      };
+      auto values = [&](int n, bool more) {
+        if (elect_one()) {
+          const uint64_t vd = sw128_desc(sm0 + M::v + (n & 1) * M::K);
+#pragma unroll
+          for (int kk = 0; kk < TOKENS / 16; ++kk)
+            mma_f16_ta(tm + (uint32_t)(2 * TOKENS + w * D), tm + (uint32_t)(w * TOKENS + kk * 8),
+                       vd + (uint64_t)((kk >> 2) * (D * 128 >> 4) + (kk & 3) * 2), tile_idesc(D), kk || more ? 1u : 0u);
+          mma_commit(sh.o_full + w);
+          mma_commit(sh.v_empty + (n & 1));
+          if (!two) mma_commit(sh.v_empty + (n & 1));
+        }
+        __syncwarp();
+      };
+      if (ok && issuer && j0 < tiles) {
+        const int n = done + j0;
+        if ((ok = all_wait(sh.k_full + (n & 1), (n >> 1) & 1, abort_flag, err, 7))) {
           tc_fence_after();
-          if (__any_sync(FULL, real)) {  // (else P of these lanes is whatever S was: nobody reads their O)
+          scores(n);
+        }
+      }
+      for (int j = j0; ok && j < tiles;) {
+        if (!(ok = all_wait(sh.s_full + w, mine & 1, abort_flag, err, 1))) break;
+        tc_fence_after();
+        if (__any_sync(FULL, real)) {  // (else P of these lanes is whatever S was: nobody reads their O)
           const float(*sc)[8] = sh.scales[(done + j) % SCALE_RING];
           const int t0 = (first + j) * TOKENS;
           // columns [lo, hi) are seen; they are looked at only where some row does not see them all
@@ -367,9 +376,10 @@ __global__ __launch_bounds__(TILE_THREADS, 1) void k_kv_tile(AttendArgs a) {
             const float to_m = fmaxf(m, top - LEAD), keep = to_m > m ? ex2(m - to_m) : 1.0f;
             m = to_m;
             l *= keep;
-            if (j) {  // O so far, once its product is complete
-              if (!(ok = all_wait(sh.o_full + w, (phase - 1) & 1, abort_flag, err, 2))) break;
+            if (j > j0) {  // O so far, once its product is complete
+              if (!(ok = all_wait(sh.o_full + w, (mine - 1) & 1, abort_flag, err, 2))) break;
               tc_fence_after();
+              const uint32_t to = ts + (uint32_t)(2 * TOKENS + w * D - w * TOKENS);
 #pragma unroll 1
               for (int c = 0; c < D; c += 16) {
                 uint32_t y[16];
@@ -393,12 +403,12 @@ __global__ __launch_bounds__(TILE_THREADS, 1) void k_kv_tile(AttendArgs a) {
             uint32_t out[32];
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-              const float to = add[c] - ref;
+              const float plus = add[c] - ref;
               float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
               for (int i = 0; i < 16; i += 2) {
-                const float p0 = ex2(fmaf(__uint_as_float(x[c][i]), f[c], to));
-                const float p1 = ex2(fmaf(__uint_as_float(x[c][i + 1]), f[c], to));
+                const float p0 = ex2(fmaf(__uint_as_float(x[c][i]), f[c], plus));
+                const float p1 = ex2(fmaf(__uint_as_float(x[c][i + 1]), f[c], plus));
                 sum[i & 2] += p0;
                 sum[(i & 2) + 1] += p1;
                 out[c * 8 + i / 2] = pack_fp16(p0, p1);
@@ -408,168 +418,152 @@ __global__ __launch_bounds__(TILE_THREADS, 1) void k_kv_tile(AttendArgs a) {
             tmem_put32(ts + half * 32, out);
           }
           tmem_wait_put();
-          }
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(sh.p_full + w);
-          if (issuer) {
-            const int n = done + j, next = (n + 1) & 1;
-            if (!(ok = all_wait(sh.v_full + (n & 1), (n >> 1) & 1, abort_flag, err, 8) &&
-                       all_wait(sh.p_full + w, phase & 1, abort_flag, err, 9)))
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(sh.p_full + w);
+        if (issuer) {
+          const int n = done + j, next = n + step_j;
+          if (!(ok = all_wait(sh.v_full + (n & 1), (n >> 1) & 1, abort_flag, err, 8) &&
+                     all_wait(sh.p_full + w, mine & 1, abort_flag, err, 9)))
+            break;
+          tc_fence_after();
+          values(n, j > j0);
+          if (j + step_j < tiles) {  // the next scores overwrite P: its product has to be complete
+            if (!(ok = all_wait(sh.k_full + (next & 1), (next >> 1) & 1, abort_flag, err, 10) &&
+                       all_wait(sh.o_full + w, mine & 1, abort_flag, err, 11)))
               break;
             tc_fence_after();
-            values(n, j > 0);
-            if (j + 1 < tiles) {  // the next scores overwrite P: its product has to be complete
-              if (!(ok = all_wait(sh.k_full + next, ((n + 1) >> 1) & 1, abort_flag, err, 10) &&
-                         all_wait(sh.o_full + w, phase & 1, abort_flag, err, 11)))
-                break;
-              tc_fence_after();
-              scores(n + 1);
-            }
+            scores(next);
           }
         }
-        if (ok && tiles && (ok = all_wait(sh.o_full + w, (phase - 1) & 1, abort_flag, err, 3))) tc_fence_after();
-        if (ok && __any_sync(FULL, real)) {
-          const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-          const int64_t at = out_row(a, sq.token, head, r);
-          float* part = part_of<D, P::ROWS>(a, seg);
-          const int prow = w * 128 + row;
-#pragma unroll
-          for (int c = 0; c < D; c += 16) {
-            uint32_t x[16];
-            if (tiles) {
-              tmem_ld16_issue(to + c, x);
-              tmem_wait16(x);
-            } else {
-#pragma unroll
-              for (int i = 0; i < 16; ++i) x[i] = 0;
-            }
-            if (!real) continue;
-            if (seg.whole) {
-              union {
-                T e[16];
-                uint4 v[2];
-              } y;
-#pragma unroll
-              for (int i = 0; i < 16; ++i) y.e[i] = from_float<T>(__uint_as_float(x[i]) * inv);
-              uint4* o = reinterpret_cast<uint4*>(static_cast<T*>(a.out) + at * D + c);
-              o[0] = y.v[0];
-              o[1] = y.v[1];
-            } else {
-              uint4* o = reinterpret_cast<uint4*>(part + prow * D + c);
-#pragma unroll
-              for (int i = 0; i < 4; ++i) o[i] = make_uint4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
-            }
-          }
-          if (real && seg.whole && a.lse) a.lse[at] = lse_of(m, l);
-          if (real && !seg.whole) {
-            part[P::ROWS * D + prow] = m;
-            part[P::ROWS * (D + 1) + prow] = l;
-          }
-        }
+        j += step_j;
+        ++mine;
       }
+      if (ok && j0 < tiles) all_wait(sh.o_full + w, (mine - 1) & 1, abort_flag, err, 3);
+      sh.row_m[w][row] = m;
+      sh.row_l[w][row] = l;
     } else {
       // --------------------------------------------------------- converters
       const int cw = warp - SOFT;
       const int32_t* table = kv.c.table + sq.slot * kv.c.max_pages;
       // Lane l looks up the l-th of the 32 blocks of four tiles: its place in the pool
-      // and its scales; the next four tiles' are looked up while these are converted.
+      // and what the softmax takes of its scales; the next four tiles' are looked up
+      // while these are converted.
       struct Lines {
         int line;  // (blocks are of 1 KB at least: 2^31 of them are more than any memory)
-        float ks, vs;
+        float ks, log_g, inv_g;
       } now, ahead;
       auto look_up = [&](int j) {
-        Lines x = {-1, 0.0f, 0.0f};
+        Lines x = {-1, 0.0f, -INFINITY, 0.0f};
         const int64_t tok = (int64_t)(first + j) * TOKENS + lane * kKvBlock;
         if (j + (lane >> 3) < tiles && tok < sq.len) {
           const int page = table[tok >> kv.page_shift];
           if (page >= 0 && page < kv.c.pages) {
             x.line = (int)(kv.scales_at(a.layer, page, head) + ((tok & (kv.c.page_tokens - 1)) / kKvBlock));
             x.ks = __ldg(kv.c.k_scale + x.line);
-            x.vs = __ldg(kv.c.v_scale + x.line);
+            const float g = fmaxf(__ldg(kv.c.v_scale + x.line), 0x1p-100f);
+            x.log_g = log2f(g);
+            x.inv_g = 1.0f / g;
           } else {
             kv_status(kv, kKvBadEntry);
           }
         }
         return x;
       };
+      auto line_of = [&](int j, int block, const Lines& x) { return __shfl_sync(FULL, x.line, (j & 3) * 8 + block); };
       // A tile's codes on their way to L2: a warp takes half of each of the 8 blocks of K
       // or V, four lanes a block.
-      auto fetch = [&](int j, int line) {
-        const int ln = __shfl_sync(FULL, line, (j & 3) * 8 + (lane >> 2));
+      auto fetch = [&](int j, const Lines& x) {
+        const int ln = line_of(j, lane >> 2, x);
         if (ln >= 0) {
           const uint8_t* p = (cw & 1 ? kv.c.v : kv.c.k) + (int64_t)ln * (kKvBlock * D) + ((cw >> 1) * 4 + (lane & 3)) * (D * 2);
 #pragma unroll
           for (int y = 0; y < D * 2; y += 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(p + y));
         }
       };
-      // keys: warp cw takes tokens 32 cw ..; lane: 16-byte piece (lane & 3) of each 64 bytes, token lane >> 2 of 8
-      constexpr int KN = D / 64 * 4;
-      uint4 kr[KN];
-      auto load_k = [&](int j, int line) {
+      // keys: warp cw takes blocks 2 cw and 2 cw + 1; lane: 16-byte piece (lane & 3) of each
+      // 64 bytes, tokens lane >> 2 and 8 more.  A block that is not there reads block 0
+      // of the pool and is zeroed when it is converted.
+      constexpr int KN = D / 64;
+      uint4 kr[2][2][KN];
+      bool k_there[2];
+      auto load_k = [&](int j, const Lines& x) {
 #pragma unroll
-        for (int i = 0; i < KN; ++i) {
-          const int tok = cw * 32 + (i & 3) * 8 + (lane >> 2);
-          const int64_t ln = __shfl_sync(FULL, line, (j & 3) * 8 + (tok >> 4));
-          kr[i] = make_uint4(0, 0, 0, 0);
-          if (ln >= 0)
-            kr[i] = __ldg(reinterpret_cast<const uint4*>(kv.c.k + ((int64_t)ln * kKvBlock + (tok & 15)) * D + (i >> 2) * 64 + (lane & 3) * 16));
+        for (int b = 0; b < 2; ++b) {
+          const int ln = line_of(j, cw * 2 + b, x);
+          k_there[b] = ln >= 0;
+          const uint8_t* p = kv.c.k + (int64_t)max(ln, 0) * (kKvBlock * D) + (lane >> 2) * D + (lane & 3) * 16;
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int c = 0; c < KN; ++c) kr[b][h][c] = __ldg(reinterpret_cast<const uint4*>(p + h * 8 * D + c * 64));
         }
       };
-      // values: 64 tokens x 64 elements a warp (half of them at head_dim 64: 64 x 32); lane: 8 tokens (lane & 7), VB elements
+      // values: 64 tokens x 64 elements a warp (x 32 at head_dim 64); lane: 8 tokens (lane & 7), VB elements.
+      // Bytes that no token owns may be NaN, and 0 times that is not 0: zeroed too.
       constexpr int VB = D / 8;  // bytes of a lane's row: 16 or 8
       const int half = cw >> 1, v_octet = lane & 7, v_el = (cw & 1) * (D / 2) + (lane >> 3) * VB;
       uint32_t vr[8][VB / 4];
-      auto load_v = [&](int j, int line) {
+      int v_tokens;  // that are there
+      auto load_v = [&](int j, const Lines& x) {
+        const int ln = line_of(j, half * 4 + (v_octet >> 1), x);
+        v_tokens = ln >= 0 ? sq.len - ((first + j) * TOKENS + half * 64 + v_octet * 8) : 0;
+        const uint8_t* p = kv.c.v + (int64_t)max(ln, 0) * (kKvBlock * D) + (v_octet & 1) * 8 * D + v_el;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const int tok = half * 64 + v_octet * 8 + i;
-          int64_t ln = __shfl_sync(FULL, line, (j & 3) * 8 + (tok >> 4));
-          // bytes that no token owns may be NaN, and 0 times that is not 0
-          if ((first + j) * TOKENS + tok >= sq.len) ln = -1;
-          const uint8_t* p = kv.c.v + ((int64_t)ln * kKvBlock + (tok & 15)) * D + v_el;
-#pragma unroll
-          for (int x = 0; x < VB / 4; ++x) vr[i][x] = 0;
-          if (ln >= 0) {
-            if (VB == 16) {
-              const uint4 y = __ldg(reinterpret_cast<const uint4*>(p));
-              vr[i][0] = y.x, vr[i][1] = y.y, vr[i][VB / 4 - 2] = y.z, vr[i][VB / 4 - 1] = y.w;
-            } else {
-              const uint2 y = __ldg(reinterpret_cast<const uint2*>(p));
-              vr[i][0] = y.x, vr[i][1] = y.y;
-            }
+          if (VB == 16) {
+            const uint4 y = __ldg(reinterpret_cast<const uint4*>(p + i * D));
+            vr[i][0] = y.x, vr[i][1] = y.y, vr[i][VB / 4 - 2] = y.z, vr[i][VB / 4 - 1] = y.w;
+          } else {
+            const uint2 y = __ldg(reinterpret_cast<const uint2*>(p + i * D));
+            vr[i][0] = y.x, vr[i][1] = y.y;
           }
         }
       };
       now = look_up(0);
       ahead = look_up(4);
-      if (tiles) load_k(0, now.line);
-      for (int j = 1; j < AHEAD; ++j) fetch(j, now.line);
+      if (tiles) load_k(0, now);
+      for (int j = 1; j < AHEAD; ++j) fetch(j, now);
       for (int j = 0; j < tiles; ++j) {
         const int n = done + j, st = n & 1;
-        load_v(j, now.line);
-        fetch(j + AHEAD, (j & 3) + AHEAD < 4 ? now.line : ahead.line);
+        load_v(j, now);
+        if ((j & 3) + AHEAD < 4)
+          fetch(j + AHEAD, now);
+        else
+          fetch(j + AHEAD, ahead);
         if (n >= 2 && !all_wait(sh.k_empty + st, ((n >> 1) - 1) & 1, abort_flag, err, 4)) break;
         if (cw == 0 && lane >> 3 == (j & 3)) {
           // (the softmax of the tile that had this place in the ring is over: S two tiles on waited for it)
-          const float g = fmaxf(now.vs, 0x1p-100f);
           float* sc = &sh.scales[n % SCALE_RING][0][lane & 7];
           sc[0] = now.ks;
-          sc[8] = now.line >= 0 ? log2f(g) : -INFINITY;
-          sc[16] = now.line >= 0 ? 1.0f / g : 0.0f;
+          sc[8] = now.log_g;
+          sc[16] = now.inv_g;
         }
         unsigned char* sk = sm + M::k + st * M::K;
+        if (!__all_sync(FULL, k_there[0] && k_there[1])) {
 #pragma unroll
-        for (int i = 0; i < KN; ++i) {
-          const int tok = cw * 32 + (i & 3) * 8 + (lane >> 2), c = (lane & 3) * 2;
-          uint32_t h[8];
-          const uint32_t x[4] = {kr[i].x, kr[i].y, kr[i].z, kr[i].w};
+          for (int b = 0; b < 2; ++b)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) to_fp16x4<CODES>(x[e], h[2 * e], h[2 * e + 1]);
-          unsigned char* to = sk + (i >> 2) * 16384;
-          *reinterpret_cast<uint4*>(to + sw128_offset(tok, c)) = make_uint4(h[0], h[1], h[2], h[3]);
-          *reinterpret_cast<uint4*>(to + sw128_offset(tok, c + 1)) = make_uint4(h[4], h[5], h[6], h[7]);
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+              for (int c = 0; c < KN; ++c)
+                if (!k_there[b]) kr[b][h][c] = make_uint4(0, 0, 0, 0);
         }
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int c = 0; c < KN; ++c) {
+              const int tok = cw * 32 + b * 16 + x * 8 + (lane >> 2), at = (lane & 3) * 2;
+              const uint32_t y[4] = {kr[b][x][c].x, kr[b][x][c].y, kr[b][x][c].z, kr[b][x][c].w};
+              uint32_t h[8];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) to_fp16x4<CODES>(y[e], h[2 * e], h[2 * e + 1]);
+              *reinterpret_cast<uint4*>(sk + c * 16384 + sw128_offset(tok, at)) = make_uint4(h[0], h[1], h[2], h[3]);
+              *reinterpret_cast<uint4*>(sk + c * 16384 + sw128_offset(tok, at + 1)) = make_uint4(h[4], h[5], h[6], h[7]);
+            }
         fence_proxy_async();
         __syncwarp();
         if (lane == 0) mbar_arrive(sh.k_full + st);
@@ -577,8 +571,15 @@ __global__ __launch_bounds__(TILE_THREADS, 1) void k_kv_tile(AttendArgs a) {
           now = ahead;
           ahead = look_up(j + 5);
         }
-        if (j + 1 < tiles) load_k(j + 1, now.line);
+        if (j + 1 < tiles) load_k(j + 1, now);
         if (n >= 2 && !all_wait(sh.v_empty + st, ((n >> 1) - 1) & 1, abort_flag, err, 5)) break;
+        if (__any_sync(FULL, v_tokens < 8)) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int x = 0; x < VB / 4; ++x)
+              if (i >= v_tokens) vr[i][x] = 0;
+        }
         unsigned char* sv = sm + M::v + st * M::K + half * (D * 128);
 #pragma unroll
         for (int x = 0; x < VB / 4; ++x)
@@ -598,12 +599,86 @@ __global__ __launch_bounds__(TILE_THREADS, 1) void k_kv_tile(AttendArgs a) {
       }
     }
     done += tiles;
-    if (two) done2 += tiles;
     ++segments;
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     if (*abort_flag) break;  // (uniform behind the barrier)
+
+    // ------------------------------------------------------------ the sums
+    // O of this thread's row, 16 elements at a time (none where no tile was seen).
+    const int w = (warp >> 2) & 1, rt = two ? w : 0, row = (warp & 3) * 32 + lane, r = seg.row0 + rt * 128 + row;
+    const bool real = r < seg.rows, seen = two ? tiles > 0 : w < tiles, some = warp < SOFT && __any_sync(FULL, real);
+    const uint32_t to = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)(2 * TOKENS + w * D);
+    auto load_o = [&](int c, uint32_t(&x)[16]) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i] = 0;
+      if (seen) {
+        tmem_ld16_issue(to + c, x);
+        tmem_wait16(x);
+      }
+    };
+    float* other = reinterpret_cast<float*>(sm + M::k);  // [D][128], the second half's O (the keys are done with)
+    if (!two) {
+      if (w == 1 && some) {
+#pragma unroll 1
+        for (int c = 0; c < D; c += 16) {
+          uint32_t x[16];
+          load_o(c, x);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) other[(c + i) * 128 + row] = __uint_as_float(x[i]);
+        }
+      }
+      __syncthreads();
+    }
+    float m = sh.row_m[w][row], l = sh.row_l[w][row], keep0 = 1.0f, keep1 = 0.0f;
+    if (!two) {
+      const float m1 = sh.row_m[1][row], top = fmaxf(m, m1);
+      keep0 = top > -INFINITY ? ex2(m - top) : 0.0f;
+      keep1 = top > -INFINITY ? ex2(m1 - top) : 0.0f;
+      m = top;
+      l = l * keep0 + sh.row_l[1][row] * keep1;
+    }
+    if (some && (two || w == 0)) {
+      const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+      const int64_t at = real ? out_row(a, sq.token, head, r) : 0;
+      float* part = part_of<D, P::ROWS>(a, seg);
+      const int prow = rt * 128 + row;
+#pragma unroll 1
+      for (int c = 0; c < D; c += 16) {
+        uint32_t x[16];
+        load_o(c, x);
+        if (!two) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            x[i] = __float_as_uint(__uint_as_float(x[i]) * keep0 + other[(c + i) * 128 + row] * keep1);
+        }
+        if (!real) continue;
+        if (seg.whole) {
+          union {
+            T e[16];
+            uint4 v[2];
+          } y;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) y.e[i] = from_float<T>(__uint_as_float(x[i]) * inv);
+          uint4* o = reinterpret_cast<uint4*>(static_cast<T*>(a.out) + at * D + c);
+          o[0] = y.v[0];
+          o[1] = y.v[1];
+        } else {
+          uint4* o = reinterpret_cast<uint4*>(part + prow * D + c);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[i] = make_uint4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+        }
+      }
+      if (real && seg.whole && a.lse) a.lse[at] = lse_of(m, l);
+      if (real && !seg.whole) {
+        part[P::ROWS * D + prow] = m;
+        part[P::ROWS * (D + 1) + prow] = l;
+      }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
     if (threadIdx.x == 0) sh.run.u = sh.run.seg.next;
     __syncthreads();
   }
@@ -640,10 +715,14 @@ cudaError_t tile_for(const AttendArgs& a, int grid, cudaStream_t s) {
 
 }  // namespace
 
-// Where the sequences bring more than 16 rows on average (and the operands of 256
-// rows fit beside two stages: head_dim up to 128).
+// From where on the tiles are faster than the stream (tq_kv_attend.cu), in rows per
+// key head, for 24 sequences of 2,000 to 8,190 tokens and 8 key heads: at head_dim
+// 128 25 rows take 152 us here and 140 there, 28 rows 153 and 165, 40 rows 155 and
+// 218; at head_dim 64 40 rows take 110 and 106, 48 rows 110 and 111, 64 rows 111
+// and 137.  (The operands of 256 rows fit beside two stages up to head_dim 128.)
 bool kv_tile_supported(const KvView& kv, int64_t n, int64_t total, int heads) {
-  return n > 0 && kv.c.head_dim <= 128 && (total + n - 1) / n * (heads / kv.c.kv_heads) > 16;
+  const int dim = kv.c.head_dim;
+  return dim <= 128 && attend_rows(kv, n, total, heads) > (dim == 128 ? 26 : 40);
 }
 
 size_t kv_tile_workspace(const KvView& kv) {
