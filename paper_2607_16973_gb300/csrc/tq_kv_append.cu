@@ -84,7 +84,7 @@ __device__ __forceinline__ uint32_t pack_products(const float* x, float f) {
 }
 
 template <typename T, int D, int CODES, bool VEC>
-__global__ __launch_bounds__(APPEND_WARPS * 32) void k_kv_append(KvView kv, int layer,
+__global__ __launch_bounds__(APPEND_WARPS * 32, kKvBlock * D * sizeof(T) <= 4096 ? 4 : 1) void k_kv_append(KvView kv, int layer,
                                                                  const int32_t* __restrict__ slots,
                                                                  const int32_t* __restrict__ starts, int64_t n,
                                                                  KvRows k, KvRows v, int64_t total, int64_t work) {

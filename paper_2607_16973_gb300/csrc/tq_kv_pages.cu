@@ -251,40 +251,36 @@ __global__ __launch_bounds__(ONE) void k_kv_extend(KvView kv, const int32_t* __r
   for (int64_t i = threadIdx.x; i < n; i += ONE) kv.c.lens[slots[i]] += counts[i];
 }
 
-__device__ __forceinline__ void copy_codes(uint8_t* __restrict__ to, const uint8_t* __restrict__ from, int64_t bytes) {
-  const uint4* a = reinterpret_cast<const uint4*>(from);
-  uint4* b = reinterpret_cast<uint4*>(to);
-  const int64_t n = bytes / 16;
-  for (int64_t i = threadIdx.x; i < n; i += COPY * 4) {
-    uint4 r[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (i + j * COPY < n) r[j] = a[i + j * COPY];
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (i + j * COPY < n) b[i + j * COPY] = r[j];
-  }
-}
-
 // Copies the used blocks of the pages that tq_kv_extend replaced: a block of
-// threads per entry, layer, head, and K or V.
+// threads per entry, layer, and K or V, which has all heads' pieces of a column
+// of threads on their way together.
 __global__ __launch_bounds__(COPY) void k_kv_copy_parts(KvView kv, ExtendWork w) {
   const int64_t i = blockIdx.x;
   griddep_wait();
   const int from = w.from[i];
   if (from < 0) return;
   const int to = w.to[i], blocks = w.blocks[i];
-  const int heads = kv.c.kv_heads;
-  for (int64_t j = blockIdx.y; j < (int64_t)2 * kv.c.layers * heads; j += gridDim.y) {
-    const int head = (int)(j % heads);
-    const bool is_v = j / heads & 1;
-    const int layer = (int)(j / (2 * heads));
+  const int heads = kv.c.kv_heads, pieces = blocks * kv.c.head_dim;  // of 16 bytes, of a head
+  const int64_t head_pieces = (int64_t)kv.c.page_tokens * kv.c.head_dim / 16;
+  for (int64_t j = blockIdx.y; j < (int64_t)2 * kv.c.layers; j += gridDim.y) {
+    const bool is_v = j & 1;
+    const int layer = (int)(j >> 1);
     uint8_t* codes = is_v ? kv.c.v : kv.c.k;
+    const uint4* a = reinterpret_cast<const uint4*>(codes + kv.codes_at(layer, from, 0));
+    uint4* b = reinterpret_cast<uint4*>(codes + kv.codes_at(layer, to, 0));
+    for (int e = threadIdx.x; e < pieces; e += COPY)
+      for (int h = 0; h < heads; h += 8) {
+        uint4 x[8];
+#pragma unroll
+        for (int y = 0; y < 8; ++y)
+          if (h + y < heads) x[y] = a[(h + y) * head_pieces + e];
+#pragma unroll
+        for (int y = 0; y < 8; ++y)
+          if (h + y < heads) b[(h + y) * head_pieces + e] = x[y];
+      }
     float* scale = is_v ? kv.c.v_scale : kv.c.k_scale;
-    copy_codes(codes + kv.codes_at(layer, to, head), codes + kv.codes_at(layer, from, head),
-               (int64_t)blocks * kKvBlock * kv.c.head_dim);
-    if (threadIdx.x < blocks)
-      scale[kv.scales_at(layer, to, head) + threadIdx.x] = scale[kv.scales_at(layer, from, head) + threadIdx.x];
+    for (int e = threadIdx.x; e < heads * blocks; e += COPY)
+      scale[kv.scales_at(layer, to, e / blocks) + e % blocks] = scale[kv.scales_at(layer, from, e / blocks) + e % blocks];
   }
 }
 
@@ -412,7 +408,7 @@ cudaError_t launch_kv_extend(const KvView& kv, const int32_t* slots, const int32
   k_kv_extend<<<1, ONE, 0, s>>>(kv, slots, counts, n, w);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
-  const int64_t parts = (int64_t)2 * kv.c.layers * kv.c.kv_heads;
+  const int64_t parts = (int64_t)2 * kv.c.layers;
   return launch_maybe_pdl(true, k_kv_copy_parts, dim3((unsigned)n, (unsigned)std::min<int64_t>(parts, 65535)),
                           dim3(COPY), 0, s, kv, w);
 }

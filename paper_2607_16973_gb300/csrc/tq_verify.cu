@@ -27,6 +27,7 @@ namespace {
 
 constexpr int VERIFY = 256;
 constexpr int VERIFY_MIN = 2048;  // vocabulary entries that are worth a block
+constexpr int PER_SM = 16;        // blocks of a call per SM, twice what fits: the shorter ones even out
 
 struct Verdict {
   int accepted;   // drafts accepted
@@ -154,10 +155,13 @@ __global__ __launch_bounds__(VERIFY) void k_verify(const T* __restrict__ target,
   __shared__ uint64_t shared[VERIFY / 32];
   const int64_t i = blockIdx.y;
   griddep_launch_dependents();
-  const Verdict r = judge(target, draft, drafts, draft_lens, uniforms, i, t, vocab);
-  const bool rejected = r.accepted < r.drafts;
   const int each = ((vocab + gridDim.x - 1) / gridDim.x + EACH - 1) / EACH * EACH;
   const int begin = blockIdx.x * each, end = min(vocab, begin + each);
+  // which row of the probabilities it is follows from the verdict; the noise is known before
+  if (begin + (int)threadIdx.x * 32 < end)
+    asm volatile("prefetch.global.L2 [%0];" ::"l"(noise + i * vocab + begin + threadIdx.x * 32));
+  const Verdict r = judge(target, draft, drafts, draft_lens, uniforms, i, t, vocab);
+  const bool rejected = r.accepted < r.drafts;
   const T* q = rejected && draft ? draft + (i * t + r.accepted) * vocab : nullptr;
   uint64_t key = race(target + (i * (t + 1) + r.accepted) * vocab, q, rejected && !draft ? r.rejected : -1,
                       noise + i * vocab, begin, end);
@@ -193,7 +197,7 @@ __global__ __launch_bounds__(VERIFY) void k_verify_finish(const T* __restrict__ 
 // than VERIFY_MIN entries.
 int verify_parts(int64_t n, int64_t vocab) {
   const int64_t most = (vocab + VERIFY_MIN - 1) / VERIFY_MIN;
-  return (int)std::max<int64_t>(1, std::min<int64_t>(most, (int64_t)device_sm_count() * 8 / n));
+  return (int)std::max<int64_t>(1, std::min<int64_t>(most, (int64_t)device_sm_count() * PER_SM / n));
 }
 
 template <typename T>
@@ -215,7 +219,7 @@ cudaError_t verify(const void* target, const void* draft, const int32_t* drafts,
 
 // Enough for every smaller batch too, which may be split further.
 size_t verify_workspace(int64_t n, int64_t vocab) {
-  return (size_t)std::max<int64_t>(n, (int64_t)device_sm_count() * 8) * sizeof(uint64_t);
+  return (size_t)std::max<int64_t>(n, (int64_t)device_sm_count() * PER_SM) * sizeof(uint64_t);
 }
 
 cudaError_t launch_verify(const void* target, const void* draft, int type, const int32_t* drafts,
