@@ -40,7 +40,8 @@ constexpr int THREADS = WARPS * 32;
 // they stay under 2^15, fp16's largest, and those down to 2^-24 of the largest
 // one keep all of fp16's bits.
 constexpr float LEAD = 10.0f, LAZY = 5.0f;
-constexpr int AHEAD = 3;         // blocks of a warp on their way to L2 beyond the one on its way to registers
+constexpr int AHEAD = 1;         // blocks of a warp on their way to L2 beyond the one on its way to registers (none: 102 us
+                                 // for 200,001 tokens, 1: 84, 2: 85, 4: 98, 10: 123, what is on its way then fills L2)
 
 // Rows come in tiles of 8 or 16; a run is worth 4 blocks, and an item costs about as
 // much as 4 blocks beside its own (looking it up, its queries, its sums).
@@ -181,25 +182,29 @@ __global__ __launch_bounds__(THREADS, per_sm(D, NT)) void k_kv_attend(AttendArgs
       l[nt][0] = l[nt][1] = 0.0f;
     }
 
-    // This warp's blocks: blk + warp, + WARPS, ...; lane l looks up the page and the
-    // scales of the l-th of 32 of them.
+    // This warp's blocks: blk + warp, + WARPS, ...; lane l looks up the place and the
+    // scales of the l-th of 32 of them, 32 to 64 blocks before they are scored.
     const int32_t* table = kv.c.table + sq.slot * kv.c.max_pages;
-    int line = -1;  // lane's block in the pool (they are of 1 KB at least: 2^31 of them are more than any memory)
-    float ks = 0.0f, vs = 0.0f;
+    // (line: a block's place in the pool; they are of 1 KB at least, and 2^31 of them more than any memory)
+    struct Lines {
+      int line;
+      float ks, vs;
+    };
     auto look_up = [&](int it) {
+      Lines x = {-1, 0.0f, 0.0f};
       const int b = blk + warp + (it + lane) * WARPS;
-      line = -1;
       if (b < blk_end) {
         const int64_t tok = (int64_t)b * kKvBlock;
         const int page = table[tok >> kv.page_shift];
         if (page >= 0 && page < kv.c.pages) {
-          line = (int)(kv.scales_at(a.layer, page, head) + ((tok & (kv.c.page_tokens - 1)) / kKvBlock));
-          ks = __ldg(kv.c.k_scale + line);
-          vs = __ldg(kv.c.v_scale + line);
+          x.line = (int)(kv.scales_at(a.layer, page, head) + ((tok & (kv.c.page_tokens - 1)) / kKvBlock));
+          x.ks = __ldg(kv.c.k_scale + x.line);
+          x.vs = __ldg(kv.c.v_scale + x.line);
         } else {
           kv_status(kv, kKvBadEntry);
         }
       }
+      return x;
     };
     uint4 kr[KP][2];
     uint32_t vr[VP][4][VW];
@@ -236,29 +241,28 @@ __global__ __launch_bounds__(THREADS, per_sm(D, NT)) void k_kv_attend(AttendArgs
         if (x + (lane & 15) * 128 < kKvBlock * D) asm volatile("prefetch.global.L2 [%0];" ::"l"(p + x));
     };
     const int steps = (blk_end - blk - warp + WARPS - 1) / WARPS;  // (<= 0: none)
-    int now = -1;
-    if (steps > 0) {
-      look_up(0);
-      now = __shfl_sync(FULL, line, 0);
-      for (int x = 1; x <= AHEAD; ++x) {
-        const int ln = __shfl_sync(FULL, line, x);
-        if (ln >= 0) fetch(ln);
-      }
-      if (now >= 0) {
-        load_k(now);
-        load_v(now);
-      }
+    // the 32 blocks that lanes stand for now, and the 32 behind them
+    Lines batch = look_up(0), after = look_up(32);
+    int now = __shfl_sync(FULL, batch.line, 0);
+    if (now >= 0) {
+      load_k(now);
+      load_v(now);
+    }
+    for (int x = 1; x <= AHEAD; ++x) {
+      const int ln = __shfl_sync(FULL, batch.line, x);
+      if (ln >= 0) fetch(ln);
     }
     for (int it = 0; it < steps; ++it) {
-      const float k_scale = __shfl_sync(FULL, ks, it & 31), v_scale = __shfl_sync(FULL, vs, it & 31);
-      int next = -1;
-      if (it + 1 < steps) {
-        if (((it + 1) & 31) == 0) look_up(it + 1);
-        next = __shfl_sync(FULL, line, (it + 1) & 31);
-        // (not past the 32 that are looked up, whose first ones are loaded without)
-        const int ln = __shfl_sync(FULL, line, (it + 1 + AHEAD) & 31);
-        if (((it + 1) & 31) + AHEAD < 32 && ln >= 0) fetch(ln);
+      const float k_scale = __shfl_sync(FULL, batch.ks, it & 31), v_scale = __shfl_sync(FULL, batch.vs, it & 31);
+      if (((it + 1) & 31) == 0) {
+        batch = after;
+        after = look_up(it + 33);
       }
+      // (the blocks behind the last have no line)
+      const int next = __shfl_sync(FULL, batch.line, (it + 1) & 31);
+      const int far = ((it + 1) & 31) + AHEAD;
+      const int ln = __shfl_sync(FULL, far < 32 ? batch.line : after.line, far & 31);
+      if (ln >= 0) fetch(ln);
       const int b = blk + warp + it * WARPS;
       float s[NT][4];
       if (now >= 0) {
