@@ -72,15 +72,17 @@ def _used(stream, *tensors) -> None:
 
 def _rows(t, name: str, heads: int, dim: int, types):
     """Rows [tokens, heads, dim] with any strides but the last: (pointer, type,
-    token stride, head stride)."""
-    if not t.is_cuda or t.dtype not in types:
-        _dev_ptr(t, name, types, contiguous=False)
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim:
-        raise ValueError(f"{name} must be [tokens, {heads}, {dim}], got {tuple(t.shape)}")
+    token stride, head stride, tokens)."""
+    kind = types.get(t.dtype)
+    if kind is None or not t.is_cuda:
+        _dev_ptr(t, name, tuple(types), contiguous=False)
+    shape = t.shape
+    if len(shape) != 3 or shape[1] != heads or shape[2] != dim:
+        raise ValueError(f"{name} must be [tokens, {heads}, {dim}], got {tuple(shape)}")
     s0, s1, s2 = t.stride()
     if s2 != 1 and t.numel():
         raise ValueError(f"{name}: the elements of a row must lie side by side")
-    return t.data_ptr(), _types()[t.dtype], s0, s1
+    return t.data_ptr(), kind, s0, s1, shape[0]
 
 
 class KVCache:
@@ -140,21 +142,25 @@ class KVCache:
             layers, kv_heads, head_dim, page_tokens, KV_CODES[codes])
         self._handle = C.byref(self._c)
         self._needs = {}  # workspace bytes by call and sizes
+        self._heads, self._dim, self._device = kv_heads, head_dim, k.device
+        self._lib, self._i32, self._f32, self._u8 = load(), i32, f32, u8
+        self._query_types = {torch.bfloat16: 0, torch.float16: 1}
+        self._types = _types()
 
     def _entries(self, a, b, name_a: str, name_b: str, stream, extra: int = 0):
         """Two int32 arrays of as many entries (the second `extra` more)."""
-        i32 = _torch().int32
-        pa, pb, n = _ptr(a, name_a, i32), _ptr(b, name_b, i32), a.numel()
+        i32, n = self._i32, a.numel()
         if a.dim() != 1 or b.dim() != 1 or b.numel() != n + extra:
             raise ValueError(f"{name_a} must be [n] and {name_b} [n{' + 1' if extra else ''}]")
-        _used(stream, a, b)
-        return pa, pb, n
+        if stream is not None:
+            _used(stream, a, b)
+        return _ptr(a, name_a, i32), _ptr(b, name_b, i32), n
 
     def _need(self, fn: str, *sizes) -> int:
         need = self._needs.get((fn, sizes))
         if need is None:
             out = C.c_size_t()
-            check(getattr(load(), fn)(self._handle, *sizes, C.byref(out)))
+            check(getattr(self._lib, fn)(self._handle, *sizes, C.byref(out)))
             if len(self._needs) >= 4096:
                 self._needs.clear()
             need = self._needs[fn, sizes] = max(out.value, 16)
@@ -162,8 +168,9 @@ class KVCache:
 
     def _workspace(self, workspace, stream, fn: str, *sizes):
         if workspace is None:
-            workspace = _empty(self._need(fn, *sizes), _torch().uint8, self.k.device, stream)
-            return workspace, workspace.data_ptr(), workspace.numel()
+            need = self._need(fn, *sizes)
+            workspace = _empty(need, self._u8, self._device, stream)
+            return workspace, workspace.data_ptr(), need
         return workspace, _dev_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size()
 
     def append(self, layer: int, slots, starts, k, v, stream=None) -> None:
@@ -171,16 +178,15 @@ class KVCache:
         sequence i's at starts[i] .. starts[i+1] - 1 (int32 [n + 1]) of k and v
         ([tokens, kv_heads, head_dim], bfloat16, float16 or float32, any strides
         but the last)."""
-        c = self._c
         ps, pt, n = self._entries(slots, starts, "slots", "starts", stream, 1)
-        types = tuple(_types())
-        kp, kt, k0, k1 = _rows(k, "k", c.kv_heads, c.head_dim, types)
-        vp, vt, v0, v1 = _rows(v, "v", c.kv_heads, c.head_dim, types)
-        if kt != vt or k.shape != v.shape:
+        kp, kt, k0, k1, total = _rows(k, "k", self._heads, self._dim, self._types)
+        vp, vt, v0, v1, tokens = _rows(v, "v", self._heads, self._dim, self._types)
+        if kt != vt or tokens != total:
             raise ValueError("k and v must have one type and shape")
-        _used(stream, k, v)
-        check(load().tq_kv_append(self._handle, layer, ps, pt, n, kp, vp, kt, k.shape[0], k0, k1, v0, v1,
-                                  _stream(stream)))
+        if stream is not None:
+            _used(stream, k, v)
+        check(self._lib.tq_kv_append(self._handle, layer, ps, pt, n, kp, vp, kt, total, k0, k1, v0, v1,
+                                     _stream(stream)))
 
     def attention_workspace(self, n: int, total: int, heads: int) -> int:
         """tq_kv_attend_workspace: device bytes for `total` queries of n sequences."""
@@ -194,59 +200,63 @@ class KVCache:
         default; window 0, or the tokens that a query sees.  Returns out
         [tokens, heads, head_dim], or (out, lse float32 [tokens, heads]) with
         `return_lse`."""
-        torch = _torch()
-        c = self._c
         ps, pt, n = self._entries(slots, starts, "slots", "starts", stream, 1)
         if q.dim() != 3:
-            raise ValueError(f"q must be [tokens, heads, {c.head_dim}]")
-        total, heads, dim = q.shape
-        qp, qt, q0, q1 = _rows(q, "q", heads, c.head_dim, (torch.bfloat16, torch.float16))
-        _used(stream, q)
+            raise ValueError(f"q must be [tokens, heads, {self._dim}]")
+        heads, dim = q.shape[1], self._dim
+        qp, qt, q0, q1, total = _rows(q, "q", heads, dim, self._query_types)
+        if stream is not None:
+            _used(stream, q)
         if out is None:
             out = _empty((total, heads, dim), q.dtype, q.device, stream)
-        elif tuple(out.shape) != (total, heads, dim):
-            raise ValueError(f"out must be {(total, heads, dim)}")
-        if lse is None:
-            if return_lse:
-                lse = _empty((total, heads), torch.float32, q.device, stream)
-        elif tuple(lse.shape) != (total, heads):
-            raise ValueError(f"lse must be {(total, heads)}")
+            op = out.data_ptr()
+        else:
+            if out.shape != (total, heads, dim):
+                raise ValueError(f"out must be {(total, heads, dim)}")
+            op = _ptr(out, "out", q.dtype)
+        lp = None
+        if lse is not None:
+            if lse.shape != (total, heads):
+                raise ValueError(f"lse must be {(total, heads)}")
+            lp = _ptr(lse, "lse", self._f32)
+        elif return_lse:
+            lse = _empty((total, heads), self._f32, q.device, stream)
+            lp = lse.data_ptr()
         workspace, wp, wb = self._workspace(workspace, stream, "tq_kv_attend_workspace", n, total, heads)
-        check(load().tq_kv_attend(self._handle, layer, ps, pt, n, qp, qt, total, heads, q0, q1,
-                                  dim ** -0.5 if scale is None else scale, window, _ptr(out, "out", q.dtype),
-                                  None if lse is None else _ptr(lse, "lse", torch.float32), wp, wb, _stream(stream)))
+        check(self._lib.tq_kv_attend(self._handle, layer, ps, pt, n, qp, qt, total, heads, q0, q1,
+                                     dim ** -0.5 if scale is None else scale, window, op, lp, wp, wb, _stream(stream)))
         return (out, lse) if return_lse else out
 
     def fork(self, dst, src, stream=None) -> None:
         """tq_kv_fork: slots dst hold what slots src hold, in the same pages."""
         pd, ps, n = self._entries(dst, src, "dst", "src", stream)
-        check(load().tq_kv_fork(self._handle, pd, ps, n, _stream(stream)))
+        check(self._lib.tq_kv_fork(self._handle, pd, ps, n, _stream(stream)))
 
     def extend(self, slots, counts, workspace=None, stream=None) -> None:
         """tq_kv_extend: room for counts[i] more tokens in slots[i]; a shared last
         page that is part full is replaced by a copy."""
         ps, pc, n = self._entries(slots, counts, "slots", "counts", stream)
         workspace, wp, wb = self._workspace(workspace, stream, "tq_kv_extend_workspace", n)
-        check(load().tq_kv_extend(self._handle, ps, pc, n, wp, wb, _stream(stream)))
+        check(self._lib.tq_kv_extend(self._handle, ps, pc, n, wp, wb, _stream(stream)))
 
     def truncate(self, slots, lens, stream=None) -> None:
         """tq_kv_truncate: slots[i] keeps its first lens[i] tokens (0: none)."""
         ps, pl, n = self._entries(slots, lens, "slots", "lens", stream)
-        check(load().tq_kv_truncate(self._handle, ps, pl, n, _stream(stream)))
+        check(self._lib.tq_kv_truncate(self._handle, ps, pl, n, _stream(stream)))
 
     def compact(self, workspace=None, stream=None):
         """tq_kv_compact: moves the pages in use to the front of the pool; returns
         how many there are (int32 [1] on the device)."""
         workspace, wp, wb = self._workspace(workspace, stream, "tq_kv_compact_workspace")
         used = _empty(1, _torch().int32, self.k.device, stream)
-        check(load().tq_kv_compact(self._handle, used.data_ptr(), wp, wb, _stream(stream)))
+        check(self._lib.tq_kv_compact(self._handle, used.data_ptr(), wp, wb, _stream(stream)))
         return used
 
     def check(self, stream=None) -> None:
         """tq_kv_check: waits for the stream; raises TQError if a call since the
         last check found too few free pages (TQ_ENOMEM) or left entries out
         (TQ_EINVAL)."""
-        check(load().tq_kv_check(self._handle, _stream(stream)))
+        check(self._lib.tq_kv_check(self._handle, _stream(stream)))
 
 
 def verify_drafts(target_probs, drafts, uniforms, noise, draft_probs=None, draft_lens=None, tokens=None, accepted=None,
