@@ -170,7 +170,7 @@ __global__ __launch_bounds__(THREADS, per_sm(D, NT)) void k_kv_attend(AttendArgs
     }
     const int blk = span.first + run.seg.b_first, blk_end = span.first + run.seg.b_last;
     // blocks that every row of the tile sees whole
-    const int whole_from = a.window ? max(0, span.place_hi - a.window + kKvBlock) / kKvBlock : 0;
+    const int whole_from = a.window && span.place_hi >= a.window ? (span.place_hi - a.window) / kKvBlock + 1 : 0;
     const int whole_to = span.place_lo >= 0 ? (span.place_lo + 1) / kKvBlock : 0;
 
     float o[NT][MT][4], m[NT][2], l[NT][2];

@@ -86,7 +86,8 @@ __device__ __forceinline__ void load_each(const T* __restrict__ p, float (&x)[EA
 
 // The race over tokens [begin, end); begin is a multiple of EACH.  Every quotient
 // that could win is a correctly rounded division; one that is below the
-// thread's best by more than the product's rounding is not taken.
+// thread's best by more than the product's rounding (not to be trusted close to
+// float32's smallest) is not taken.
 template <typename T>
 __device__ uint64_t race(const T* __restrict__ p, const T* __restrict__ q, int without, const float* __restrict__ noise,
                          int begin, int end) {
@@ -119,7 +120,8 @@ __device__ uint64_t race(const T* __restrict__ p, const T* __restrict__ q, int w
 #pragma unroll
     for (int j = 0; j < EACH; ++j) {
       const int v = first + j * stride;
-      if (!(w[j] > 0.0f) || v == without || w[j] < best * e[j] * 0.999999f) continue;
+      const float bar = best * e[j] * 0.999999f;
+      if (!(w[j] > 0.0f) || v == without || (w[j] < bar && bar > 0x1p-100f)) continue;
       const float x = __fdiv_rn(w[j], e[j]);
       if (x > best) {
         best = x;
