@@ -47,8 +47,9 @@ constexpr float LEAD = 10.0f, LAZY = 5.0f;
 constexpr int AHEAD = 3;       // tiles on their way to L2 (less than four: see the converters' look-ups)
 constexpr int SCALE_RING = 4;  // tiles whose scales are held (two being converted, two in the softmax)
 
-// A run is worth a tile of tokens; an item costs about as much as two beside its own.
-using TileCut = Cut<256, TOKENS, 2, 1>;
+// A run is worth a tile of tokens; an item costs about as much as four beside its
+// own (two long prompts: 383 us counted as two, 313 as four, 318 as six).
+using TileCut = Cut<256, TOKENS, 4, 1>;
 
 template <int D>
 struct TileSmem {
