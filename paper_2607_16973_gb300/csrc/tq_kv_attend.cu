@@ -43,10 +43,12 @@ constexpr float LEAD = 10.0f, LAZY = 5.0f;
 constexpr int AHEAD = 1;         // blocks of a warp on their way to L2 beyond the one on its way to registers (none: 102 us
                                  // for 200,001 tokens, 1: 84, 2: 85, 4: 98, 10: 123, what is on its way then fills L2)
 
-// Rows come in tiles of 8 or 16; a run is worth 4 blocks, and an item costs about as
-// much as 4 blocks beside its own (looking it up, its queries, its sums).
+// Rows come in tiles of 8 or 16; a run is worth 4 blocks (2: 12.4 us for one query
+// over 1,031 tokens, 4: 11.6, 8: 12.8), and an item costs about as much as 16
+// beside its own: looking it up, its queries, its sums (128 ragged sequences: 138 us
+// counted as 4, 124 as 8, 114 as 16 to 32, 116 as 48).
 template <int NT>
-using StreamCut = Cut<8 * NT, kKvBlock, 4, 4>;
+using StreamCut = Cut<8 * NT, kKvBlock, 16, 4>;
 
 // Two pairs of fp16 values from the four codes of a word: every code is exact.
 template <int CODES>
@@ -118,6 +120,18 @@ __global__ __launch_bounds__(THREADS, per_sm(D, NT)) void k_kv_attend(AttendArgs
     const KvSeq sq = run.seg.it.s;
     const Span span = run.seg.it.span;
     const int head = run.seg.it.head, row0 = run.seg.row0, rows = run.seg.rows;
+
+    if (run.seg.b_first == run.seg.b_last) {  // no row sees a token
+      for (int e = threadIdx.x; e < min(ROWS, rows - row0) * D; e += THREADS) {
+        const int64_t at = out_row(a, sq.token, head, row0 + e / D);
+        static_cast<T*>(a.out)[at * D + e % D] = from_float<T>(0.0f);
+        if (a.lse && e % D == 0) a.lse[at] = -INFINITY;
+      }
+      __syncthreads();
+      if (threadIdx.x == 0) run.u = run.seg.next;
+      __syncthreads();
+      continue;
+    }
 
     // the queries, scaled by a power of two to fp16's middle: row n = g of each 8
     uint32_t qf[NT][KP * 4][2];
