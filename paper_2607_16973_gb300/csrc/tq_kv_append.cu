@@ -9,6 +9,7 @@
 // Bound: HBM, 2 + 1 bytes per element (16-bit input); for single tokens
 // (a decoding step) the latency of the chain starts -> lens -> table -> codes.
 #include <algorithm>
+#include <cstdint>
 #include <cstring>
 
 #include "tq_kv.cuh"
@@ -93,8 +94,15 @@ __global__ __launch_bounds__(APPEND_WARPS * 32, kKvBlock * D * sizeof(T) <= 4096
   const int lane = threadIdx.x & 31;
   const int64_t w = (int64_t)blockIdx.x * APPEND_WARPS + (threadIdx.x >> 5);
   if (w >= work) return;
-  const int head = (int)(w % kv.c.kv_heads);
-  const int64_t rest = w / kv.c.kv_heads;
+  int head;
+  int64_t rest;
+  if (work <= UINT32_MAX) {  // (a division of 32 bits; nearly always)
+    rest = (uint32_t)w / (uint32_t)kv.c.kv_heads;
+    head = (int)((uint32_t)w - (uint32_t)rest * (uint32_t)kv.c.kv_heads);
+  } else {
+    rest = w / kv.c.kv_heads;
+    head = (int)(w - rest * kv.c.kv_heads);
+  }
   const bool is_v = rest & 1;
   const int64_t unit = rest >> 1;
   // m tokens touch at most m / 16 + 2 blocks (rounded down), so units
@@ -125,19 +133,24 @@ __global__ __launch_bounds__(APPEND_WARPS * 32, kKvBlock * D * sizeof(T) <= 4096
     uint4 u;
     T e[E];
   } r[CHUNKS];
+  // a chunk's row: 32 lanes cover STEP rows, or a row takes several chunks
+  constexpr int STEP = 32 * E >= D ? 32 * E / D : 1, PIECES = 32 * E >= D ? 1 : D / (32 * E);
+  const T* p = x + (32 * E >= D ? lane * E / D : 0) * src.token_stride + lane * E % D;
+  const int64_t down = STEP * src.token_stride;
 #pragma unroll
   for (int c = 0; c < CHUNKS; ++c) {
-    const int e = (c * 32 + lane) * E, row = e / D, col = e % D;
+    const int row = (c * 32 + lane) * E / D;
     r[c].u = make_uint4(0, 0, 0, 0);
     if (row >= lo && row < hi) {
-      const T* p = x + row * src.token_stride + col;
+      const T* y = p + c % PIECES * 32 * E;
       if (VEC) {
-        r[c].u = __ldcs(reinterpret_cast<const uint4*>(p));
+        r[c].u = __ldcs(reinterpret_cast<const uint4*>(y));
       } else {
 #pragma unroll
-        for (int j = 0; j < E; ++j) r[c].e[j] = p[j];
+        for (int j = 0; j < E; ++j) r[c].e[j] = y[j];
       }
     }
+    if (c % PIECES == PIECES - 1) p += down;
   }
   // the largest magnitude, by the bits without their sign; an infinity or a NaN
   // shows in it, and only then are the finite values looked for one by one

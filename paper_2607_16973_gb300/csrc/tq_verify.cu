@@ -84,14 +84,15 @@ __device__ __forceinline__ void load_each(const T* __restrict__ p, float (&x)[EA
   for (int j = 0; j < EACH; ++j) x[j] = to_float(u.e[j]);
 }
 
-// The race over tokens [begin, end); begin is a multiple of EACH.  Every quotient
-// that could win is a correctly rounded division; one that is below the
-// thread's best by more than the product's rounding (not to be trusted close to
-// float32's smallest) is not taken.
+// The race over tokens [begin, end); begin is a multiple of EACH.  A quotient that
+// could win is a correctly rounded division; most are ruled out before, by
+// w < 0.999999 best * noise (the margin is more than the products round; below
+// float32's normal range both sides are multiples of one step, and the product's
+// rounding is at most half of it).
 template <typename T>
 __device__ uint64_t race(const T* __restrict__ p, const T* __restrict__ q, int without, const float* __restrict__ noise,
                          int begin, int end) {
-  float best = 0.0f;
+  float best = 0.0f, bar = 0.0f;
   int token = -1;
   const bool wide = (((uintptr_t)p | (uintptr_t)q | (uintptr_t)noise) & 15u) == 0;
   for (int base = begin; base < end; base += VERIFY * EACH) {
@@ -120,11 +121,11 @@ __device__ uint64_t race(const T* __restrict__ p, const T* __restrict__ q, int w
 #pragma unroll
     for (int j = 0; j < EACH; ++j) {
       const int v = first + j * stride;
-      const float bar = best * e[j] * 0.999999f;
-      if (!(w[j] > 0.0f) || v == without || (w[j] < bar && bar > 0x1p-100f)) continue;
+      if (!(w[j] >= fmaxf(bar * e[j], 0x1p-149f)) || v == without) continue;  // (0x1p-149: weights that are 0 or less)
       const float x = __fdiv_rn(w[j], e[j]);
       if (x > best) {
         best = x;
+        bar = best * 0.999999f;
         token = v;
       }
     }
