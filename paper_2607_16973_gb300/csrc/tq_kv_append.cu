@@ -8,6 +8,8 @@
 //
 // Bound: HBM, 2 + 1 bytes per element (16-bit input); for single tokens
 // (a decoding step) the latency of the chain starts -> lens -> table -> codes.
+// 64 single tokens: 4.1 us.  Prompts (154 MB): 34 us, 4.5 TB/s; 72 us with a division
+// for every element, 53 with a test for each that a product may round otherwise.
 #include <algorithm>
 #include <cstdint>
 #include <cstring>

@@ -13,11 +13,12 @@
 // One CTA per SM, 12 warps (168 registers each):
 //   0-7   softmax: warps 0-3 the first 128 rows, 4-7 the others; a thread per row.
 //         (Up to 128 rows: both have them all and take tiles of tokens in turn.)
-//         S is read from tensor memory 32 columns at a time (two blocks of
-//         tokens) and weighed with the reference m of the tiles before; only where
-//         a weight passes it by 2^15 does m move, the row's O is scaled in tensor
-//         memory and the tile weighed again (LEAD, LAZY: as in tq_kv_attend.cu).
-//         P goes over the columns of S as the A operand of the second product.
+//         S is read from tensor memory 64 columns at a time (four blocks of
+//         tokens): the second half's and the first half's maxima, the first half's
+//         weights, and the second half again for its own.  P goes over the columns
+//         of S as the A operand of the second product.  The reference m only
+//         moves when a weight passes it by 2^15; then the row's O is scaled in
+//         tensor memory (LEAD, LAZY: as in tq_kv_attend.cu).
 //         The first warp of each four issues their MMAs: P V once all four have
 //         written P, then, when that product is complete (S and P share columns),
 //         the scores of the next tokens.  While one row tile's softmax runs, the
@@ -29,9 +30,14 @@
 //
 // Tensor memory (512 columns): S/P of the two row tiles, 128 each, O of the two.
 //
-// Bound: per 256 x 128 tile (head_dim 128) about 2,200 cycles of MMAs, 2 x 128
-// columns of softmax per scheduler (about 1,600 issue slots) and the converters'
-// 500; for few rows the chain S -> softmax -> O.
+// Bound: the chain softmax -> P V -> S of a row tile, half of which the other's
+// fills.  Per 256 x 128 tile (head_dim 128) about 5,000 cycles: 3,300 of MMAs (32 of
+// M128 N128 K16, ~100 each) and per row tile 620 for the maxima and 1,400 for the
+// weights.  (Weighing in one pass with the old reference and again where it has to
+// move was slower: 448 us against 418 for two prompts, for want of registers.)
+// A prompt of 2,048 tokens and the last 2,046 of 6,000 (201 GFLOP): 313 us, 643
+// TFLOP/s, 0.34 of the measured rate.  Up to 128 rows the converters bound it: 255 MB of codes in
+// 154 us.
 #include <algorithm>
 
 #include "tq_kv_attend.cuh"

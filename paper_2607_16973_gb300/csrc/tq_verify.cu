@@ -12,11 +12,13 @@
 // k_verify: several blocks per sequence settle the acceptance each for
 // themselves (a few loads), then race over a part of one row; their winners
 // go to the workspace as 64-bit keys (weight's bits, then the token
-// inverted).  k_verify_finish: a warp per sequence takes the largest key and
+// inverted).  k_verify_finish: a block per sequence takes the largest key and
 // writes the tokens.
 //
 // Bound: HBM, one row of the target's probabilities, the noise, and after a
-// rejection the draft's row, read once per sequence.
+// rejection the draft's row, read once per sequence; 256 sequences over 128,000
+// bfloat16 entries (249 MB): 46 us, 5.4 TB/s.  (Blocks of a call per SM: 8 52 us, 16 46,
+// 32 54.)
 #include <algorithm>
 
 #include "tq_kv.cuh"
