@@ -108,6 +108,7 @@ struct Units {
 template <class P>
 __device__ void load_chunk(const AttendArgs& a, Units& u, int64_t base, int64_t sum) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  __syncthreads();  // (a warp may still look an item up in the chunk that this one replaces)
   for (int j0 = 0; j0 < CHUNK; j0 += SCAN) {
     if (base + j0 >= a.n && j0) break;
     const int j = j0 + threadIdx.x;
@@ -270,7 +271,7 @@ __device__ bool my_run(const AttendArgs& a, Units& units, Run& run) {
     run.end = end;
   }
   __syncthreads();
-  return u < end;
+  return run.u < run.end;
 }
 
 // Finds the next segment of the run, in run.seg; the caller moves run.u on, behind
