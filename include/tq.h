@@ -609,7 +609,8 @@ tq_status tq_kv_append(const tq_kv_cache* cache, int layer, const int32_t* slots
  * of two; scores, their statistics and the sums are float32, weights fp16
  * relative to the row's largest.  Scores are taken to be below 2^22 ln 2 in
  * magnitude: beyond that float32 does not tell them apart to a factor of e^(1/2),
- * and weights may leave fp16's range.  Queries that are not finite give results that are not.
+ * and weights may leave fp16's range.  A query with an element that is not
+ * finite gives NaN in its whole row of out and in lse, if it sees a token.
  */
 tq_status tq_kv_attend_workspace(const tq_kv_cache* cache, int64_t n, int64_t total,
                                  int heads, size_t* bytes);

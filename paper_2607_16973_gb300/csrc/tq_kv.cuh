@@ -8,6 +8,7 @@
 #include <cuda_runtime.h>
 
 #include <cstdint>
+#include <cstring>
 
 #include "tq_kv.h"
 
@@ -82,6 +83,26 @@ constexpr float kv_qmax() { return CODES == TQ_KV_INT8 ? 127.0f : 448.0f; }
 __device__ __forceinline__ float to_float(float x) { return x; }
 __device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
 __device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+
+// Largest magnitude of the elements of two words (one element of float32, two of
+// the 16-bit types side by side), as bits without sign: they order as the values
+// do, infinity above them and NaN above that.
+template <typename T>
+__device__ __forceinline__ uint32_t max_magnitude(uint32_t a, uint32_t b) {
+  return sizeof(T) == 2 ? __vmaxu2(a, b & 0x7FFF7FFFu) : max(a, b & 0x7FFFFFFFu);
+}
+template <typename T>
+__device__ __forceinline__ uint32_t max_magnitude(uint32_t a, const uint4& b) {
+  return max_magnitude<T>(max_magnitude<T>(max_magnitude<T>(max_magnitude<T>(a, b.x), b.y), b.z), b.w);
+}
+template <typename T>
+__device__ __forceinline__ float magnitude(uint32_t bits) {
+  if (sizeof(T) == 4) return __uint_as_float(bits);
+  const uint32_t top = max(bits & 0xFFFFu, bits >> 16);
+  T x;
+  memcpy(&x, &top, sizeof(T));
+  return to_float(x);
+}
 
 }  // namespace
 }  // namespace tq

@@ -12,7 +12,6 @@
 // for every element, 53 with a test for each that a product may round otherwise.
 #include <algorithm>
 #include <cstdint>
-#include <cstring>
 
 #include "tq_kv.cuh"
 
@@ -20,22 +19,6 @@ namespace tq {
 namespace {
 
 constexpr int APPEND_WARPS = 8;
-
-// Largest magnitude of the elements of two words (one element of float32, two of
-// the 16-bit types side by side), as bits without sign: they order as the values
-// do.
-template <typename T>
-__device__ __forceinline__ uint32_t max_magnitude(uint32_t a, uint32_t b) {
-  return sizeof(T) == 2 ? __vmaxu2(a, b & 0x7FFF7FFFu) : max(a, b & 0x7FFFFFFFu);
-}
-template <typename T>
-__device__ __forceinline__ float magnitude(uint32_t bits) {
-  if (sizeof(T) == 4) return __uint_as_float(bits);
-  const uint32_t top = max(bits & 0xFFFFu, bits >> 16);
-  T x;
-  memcpy(&x, &top, sizeof(T));
-  return to_float(x);
-}
 
 // Codes of a chunk by the definition: divided, NaN and everything at scale 0 to 0,
 // infinities to the ends.  A call, because it is rare and eight of it would not
@@ -158,8 +141,7 @@ __global__ __launch_bounds__(APPEND_WARPS * 32, kKvBlock * D * sizeof(T) <= 4096
   // shows in it, and only then are the finite values looked for one by one
   uint32_t bits = 0;
 #pragma unroll
-  for (int c = 0; c < CHUNKS; ++c)
-    bits = max_magnitude<T>(max_magnitude<T>(max_magnitude<T>(max_magnitude<T>(bits, r[c].u.x), r[c].u.y), r[c].u.z), r[c].u.w);
+  for (int c = 0; c < CHUNKS; ++c) bits = max_magnitude<T>(bits, r[c].u);
 #pragma unroll
   for (int o = 16; o; o >>= 1) bits = max_magnitude<T>(bits, __shfl_xor_sync(0xffffffffu, bits, o));
   float top = magnitude<T>(bits);

@@ -135,7 +135,8 @@ __global__ __launch_bounds__(THREADS, per_sm(D, NT)) void k_kv_attend(AttendArgs
       continue;
     }
 
-    // the queries, scaled by a power of two to fp16's middle: row n = g of each 8
+    // the queries, scaled by a power of two to fp16's middle: row n = g of each 8.  A row
+    // that is not finite becomes NaN throughout, and so do its scores, whatever the codes.
     uint32_t qf[NT][KP * 4][2];
     float unscale[NT][2];         // of rows 2t and 2t + 1: scores in log2 units
     int place[NT][2];             // last token that they see; -1: none
@@ -147,7 +148,7 @@ __global__ __launch_bounds__(THREADS, per_sm(D, NT)) void k_kv_attend(AttendArgs
       const T* p = static_cast<const T*>(a.q.p) + token * a.q.token_stride +
                    (int64_t)(head * a.group + row % a.group) * a.q.head_stride + 16 * t;
       union { uint4 v[2]; T e[16]; } x[KP];
-      float top = 0.0f;
+      uint32_t bits = 0;
 #pragma unroll
       for (int c = 0; c < KP; ++c) {
         x[c].v[0] = x[c].v[1] = make_uint4(0, 0, 0, 0);
@@ -160,14 +161,14 @@ __global__ __launch_bounds__(THREADS, per_sm(D, NT)) void k_kv_attend(AttendArgs
             for (int e = 0; e < 16; ++e) x[c].e[e] = p[64 * c + e];
           }
         }
-#pragma unroll
-        for (int e = 0; e < 16; ++e) top = fmaxf(top, fabsf(to_float(x[c].e[e])));
+        bits = max_magnitude<T>(max_magnitude<T>(bits, x[c].v[0]), x[c].v[1]);
       }
-      top = fmaxf(top, __shfl_xor_sync(FULL, top, 1));
-      top = fmaxf(top, __shfl_xor_sync(FULL, top, 2));
+      bits = max_magnitude<T>(bits, __shfl_xor_sync(FULL, bits, 1));
+      bits = max_magnitude<T>(bits, __shfl_xor_sync(FULL, bits, 2));
+      const float top = magnitude<T>(bits);
       // the largest element to [2^8, 2^9): both factors are powers of two within float32's normal range
       const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -110), 127);
-      const float up = __uint_as_float((uint32_t)(127 + min(8 - e, 118)) << 23);
+      const float up = top < INFINITY ? __uint_as_float((uint32_t)(127 + min(8 - e, 118)) << 23) : NAN;
       const float down = a.scale * LOG2E / up;
 #pragma unroll
       for (int c = 0; c < KP; ++c)

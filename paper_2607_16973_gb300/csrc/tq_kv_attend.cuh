@@ -313,12 +313,14 @@ __device__ __forceinline__ float* part_of(const AttendArgs& a, const Segment& g)
 __device__ __forceinline__ int64_t out_row(const AttendArgs& a, int token, int head, int r) {
   return (int64_t)(token + r / a.group) * a.heads + head * a.group + r % a.group;
 }
-__device__ __forceinline__ float lse_of(float m, float l) { return l > 0.0f ? m * LN2 + logf(l) : -INFINITY; }
+// (l = 0: nothing was seen; NaN: the query is not finite)
+__device__ __forceinline__ float lse_of(float m, float l) { return l == 0.0f ? -INFINITY : m * LN2 + logf(l); }
 
 // Joins the items that several runs share, in the runs' order: a block per run
 // that continues one and 8 of its rows.  A warp takes every 8th part, the 8
 // rows of it at once, so that many parts are on their way together (every 4th at
-// head_dim 256).
+// head_dim 256).  A part in which a row saw nothing has m = -inf and l = 0 and is
+// left out; m = -inf beside another l is a row of NaN, which joins to NaN.
 constexpr int join_warps(int dim) { return dim == 256 ? 4 : 8; }  // (their sums take 32 KB of shared memory)
 template <typename T, int D, int ROWS>
 __global__ __launch_bounds__(join_warps(D) * 32) void k_kv_join(AttendArgs a) {
@@ -360,7 +362,7 @@ __global__ __launch_bounds__(join_warps(D) * 32) void k_kv_join(AttendArgs a) {
       }
 #pragma unroll
     for (int r = 0; r < 8; ++r)
-      if (r < live && mm[r] > -INFINITY) {
+      if (r < live && (mm[r] > -INFINITY || ll[r] != 0.0f)) {
         const float top = fmaxf(m[r], mm[r]), keep = ex2(m[r] - top), f = ex2(mm[r] - top);
         m[r] = top;
         l[r] = l[r] * keep + ll[r] * f;
@@ -384,14 +386,12 @@ __global__ __launch_bounds__(join_warps(D) * 32) void k_kv_join(AttendArgs a) {
     for (int e = 0; e < E; ++e) y[e] = 0.0f;
 #pragma unroll
     for (int x = 0; x < JOIN_WARPS; ++x) top = fmaxf(top, sh_m[x][r]);
-    if (top > -INFINITY) {
 #pragma unroll
-      for (int x = 0; x < JOIN_WARPS; ++x) {
-        const float f = ex2(sh_m[x][r] - top);
-        sum += f * sh_l[x][r];
+    for (int x = 0; x < JOIN_WARPS; ++x) {
+      const float f = top > -INFINITY ? ex2(sh_m[x][r] - top) : 1.0f;  // (1: sums of 0, or NaN)
+      sum += f * sh_l[x][r];
 #pragma unroll
-        for (int e = 0; e < E; ++e) y[e] += f * sh_o[x][r][lane * E + e];
-      }
+      for (int e = 0; e < E; ++e) y[e] += f * sh_o[x][r][lane * E + e];
     }
     const int64_t at = out_row(a, sp.token, sp.head, sp.row0 + row0 + r);
     const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;

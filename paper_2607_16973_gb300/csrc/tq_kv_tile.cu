@@ -211,7 +211,8 @@ __global__ __launch_bounds__(TILE_THREADS, 1) void k_kv_tile(AttendArgs a) {
       const int j0 = two ? 0 : w, step_j = two ? 1 : 2;
       if (w == 0 || two) {
         // The warp's 32 rows of queries, D / 8 lanes to a row, each row scaled so that
-        // its largest element lies in [2^8, 2^9).
+        // its largest element lies in [2^8, 2^9).  A row that is not finite becomes NaN
+        // throughout, and so do its scores, whatever the codes.
         constexpr int LANES = D / 8, STEP = 32 / LANES;
         const int c = lane % LANES;
         union Chunk {
@@ -221,21 +222,18 @@ __global__ __launch_bounds__(TILE_THREADS, 1) void k_kv_tile(AttendArgs a) {
         // N rows, y, y + STEP, ...: their reductions run side by side
         auto put_rows = [&](int y, const auto& in) {
           constexpr int N = sizeof(in) / sizeof(Chunk);
-          float top[N];
+          uint32_t bits[N];
 #pragma unroll
-          for (int x = 0; x < N; ++x) {
-            top[x] = 0.0f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) top[x] = fmaxf(top[x], fabsf(to_float(in[x].e[e])));
-          }
+          for (int x = 0; x < N; ++x) bits[x] = max_magnitude<T>(0u, in[x].v);
 #pragma unroll
           for (int o = LANES / 2; o; o >>= 1)
 #pragma unroll
-            for (int x = 0; x < N; ++x) top[x] = fmaxf(top[x], __shfl_xor_sync(FULL, top[x], o));
+            for (int x = 0; x < N; ++x) bits[x] = max_magnitude<T>(bits[x], __shfl_xor_sync(FULL, bits[x], o));
 #pragma unroll
           for (int x = 0; x < N; ++x) {
-            const int e2 = min(max((int)(__float_as_uint(top[x]) >> 23) - 127, -110), 127), at = y + x * STEP;
-            const float up = __uint_as_float((uint32_t)(127 + min(8 - e2, 118)) << 23);
+            const float top = magnitude<T>(bits[x]);
+            const int e2 = min(max((int)(__float_as_uint(top) >> 23) - 127, -110), 127), at = y + x * STEP;
+            const float up = top < INFINITY ? __uint_as_float((uint32_t)(127 + min(8 - e2, 118)) << 23) : NAN;
             const float f = a.scale < 0.0f ? -up : up;  // (the scale's sign goes with the queries)
             uint32_t h[4];
 #pragma unroll

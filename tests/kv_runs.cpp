@@ -136,6 +136,8 @@ static int __ffs(unsigned x) { return __builtin_ffs((int)x); }
 static int atomicOr(int* p, int x) { return __sync_fetch_and_or(p, x); }
 static unsigned __float_as_uint(float x) { return emu::value<unsigned>(emu::bits(x)); }
 static unsigned __byte_perm(unsigned, unsigned, unsigned) { abort(); }  // (not reached)
+static unsigned __vmaxu2(unsigned, unsigned) { abort(); }
+static float __uint_as_float(unsigned) { abort(); }
 template <typename A, typename B> typename std::common_type<A, B>::type min(A a, B b) { return a < b ? a : b; }
 template <typename A, typename B> typename std::common_type<A, B>::type max(A a, B b) { return a > b ? a : b; }
 

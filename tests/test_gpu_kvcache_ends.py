@@ -1,0 +1,50 @@
+"""Attention at the ends of what it is given: queries that are not finite."""
+import numpy as np
+import pytest
+
+from test_gpu_kvcache import Case, compare
+
+pytestmark = pytest.mark.gpu
+
+
+def attend(case, q, window=0, **kw):
+    cache = case.cache()
+    out, lse = cache.attention(case.layer, case.device(case.slots), case.device(case.starts), q, window=window,
+                               return_lse=True, **kw)
+    cache.check()
+    return out, lse
+
+
+# sequences whose work is cut over several runs, ones that a run takes whole, of one token and of none;
+# up to 8 rows per key head, up to 16, one row tile of the tensor cores, two
+SHAPES = pytest.mark.parametrize("lens,new,dim,group", [
+    ([3000, 40, 1, 0], [1, 1, 1, 1], 128, 4), ([2000, 50, 9, 0], [2, 2, 2, 2], 64, 8), ([1500, 30, 2], [3, 2, 2], 256, 2),
+    ([3000, 60, 61, 30], [60, 60, 60, 60], 128, 1), ([2500, 200, 201, 130], [200, 200, 200, 200], 64, 1)])
+
+
+@SHAPES
+@pytest.mark.parametrize("codes", ["int8", "e4m3"])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("type", ["bfloat16", "float16"])
+def test_a_query_that_is_not_finite_gives_nan(cuda_lib, lens, new, dim, group, codes, value, type):
+    """In the row itself, in every element and in its lse, if it sees a token; the other rows are what they were, up to
+    the order of the running maximum's steps."""
+    import torch
+    case = Case(cuda_lib, lens, new, dim=dim, codes=codes, seed=dim + len(lens)).fill()
+    clean = case.queries(2 * group, type)
+    q = clean.clone()
+    bad = torch.zeros(q.shape[:2], dtype=torch.bool, device="cuda")
+    seen = torch.zeros_like(bad)
+    for i, (length, count) in enumerate(zip(lens, new)):
+        at = int(case.starts[i])
+        seen[at + max(0, count - length): at + count] = True
+        for r in {0, count // 2, count - 1}:
+            h = (r + i) % (2 * group)
+            bad[at + r, h] = True
+            q[at + r, h, (7 * r + i) % dim] = value
+    want, want_lse = attend(case, clean)
+    out, lse = attend(case, q)
+    hit = bad & seen
+    assert hit.any() and (bad & ~seen).any() == (min(lens) == 0 or any(n > x for n, x in zip(new, lens)))
+    assert out[hit].isnan().all() and lse[hit].isnan().all()
+    compare(case, clean, torch.where(hit[..., None], want, out), torch.where(hit, want_lse, lse))
