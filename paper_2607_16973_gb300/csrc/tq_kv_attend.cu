@@ -182,7 +182,7 @@ __global__ __launch_bounds__(THREADS, per_sm(D, NT)) void k_kv_attend(AttendArgs
       for (int h = 0; h < 2; ++h) {
         unscale[nt][h] = __shfl_sync(FULL, down, (2 * t + h) * 4);
         const int r = row0 + nt * 8 + 2 * t + h;
-        place[nt][h] = r < rows ? sq.len - sq.count + r / a.group : -1;
+        place[nt][h] = r < rows ? max(-1, sq.len - sq.count + r / a.group) : -1;
       }
     }
     const int blk = span.first + run.seg.b_first, blk_end = span.first + run.seg.b_last;

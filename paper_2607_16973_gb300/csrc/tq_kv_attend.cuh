@@ -85,7 +85,8 @@ __device__ __forceinline__ Span tile_span(const AttendArgs& a, const KvSeq& s, i
   const unsigned last = min((unsigned)s.count * group, row0 + P::ROWS) - 1;
   w.place_lo = s.len - s.count + (int)(row0 / group);
   w.place_hi = s.len - s.count + (int)(last / group);
-  w.first = a.window ? max(0, w.place_lo - a.window + 1) / P::BLOCK : 0;
+  // (a row in front of the sequence's first token sees nothing; its place may be as far below 0 as int reaches)
+  w.first = a.window ? max(0, max(0, w.place_lo) - a.window + 1) / P::BLOCK : 0;
   w.blocks = w.place_hi < 0 ? 0 : max(0, w.place_hi / P::BLOCK + 1 - w.first);
   return w;
 }

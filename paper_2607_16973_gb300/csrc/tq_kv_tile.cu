@@ -287,7 +287,7 @@ __global__ __launch_bounds__(TILE_THREADS, 1) void k_kv_tile(AttendArgs a) {
       float m = -INFINITY, l = 0.0f;
       bool ok = all_wait(sh.q_full + rt, segments & 1, abort_flag, err, 6);
       const float unscale = sh.unscale[rt * 128 + row];
-      const int place = real ? sq.len - sq.count + r / a.group : -1;
+      const int place = real ? max(-1, sq.len - sq.count + r / a.group) : -1;
       // what the first warp issues for the four
       const bool issuer = (warp & 3) == 0;
       const uint32_t tm = __shfl_sync(FULL, tmem, 0), sm0 = __shfl_sync(FULL, smem_u32(sm), 0);
@@ -332,7 +332,7 @@ __global__ __launch_bounds__(TILE_THREADS, 1) void k_kv_tile(AttendArgs a) {
           const float(*sc)[8] = sh.scales[(done + j) % SCALE_RING];
           const int t0 = (first + j) * TOKENS;
           // columns [lo, hi) are seen; they are looked at only where some row does not see them all
-          const int hi = place - t0 + 1, lo = a.window ? place - a.window + 1 - t0 : 0;
+          const int hi = place - t0 + 1, lo = a.window ? max(0, hi) - a.window : 0;
           const bool edge = __any_sync(FULL, real && (hi < TOKENS || lo > 0));
           // Half of S at a time (64 columns, 4 blocks): the second half's maximum, the
           // first half's, its weights, and the second half read again for its.  P goes

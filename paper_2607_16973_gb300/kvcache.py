@@ -25,6 +25,7 @@ from . import _dev_ptr, _on_stream, _stream_handle, _torch, _used_on
 from ._lib import KV_CODES, KvCacheStruct, check, load
 
 BLOCK = 16  # tokens that share a scale
+INT_MAX = 2**31 - 1  # (a wider window hides no more; ctypes would take its low 32 bits)
 
 # A decoding step makes these calls once per layer on a few tokens, and their
 # host side is then what it waits for: the checks below take the short way where
@@ -224,7 +225,8 @@ class KVCache:
             lp = lse.data_ptr()
         workspace, wp, wb = self._workspace(workspace, stream, "tq_kv_attend_workspace", n, total, heads)
         check(self._lib.tq_kv_attend(self._handle, layer, ps, pt, n, qp, qt, total, heads, q0, q1,
-                                     dim ** -0.5 if scale is None else scale, window, op, lp, wp, wb, _stream(stream)))
+                                     dim ** -0.5 if scale is None else scale, min(window, INT_MAX), op, lp, wp, wb,
+                                     _stream(stream)))
         return (out, lse) if return_lse else out
 
     def fork(self, dst, src, stream=None) -> None:

@@ -1,4 +1,4 @@
-"""Attention at the ends of what it is given: queries that are not finite."""
+"""Attention at the ends of what it is given: queries that are not finite, windows as wide as int."""
 import numpy as np
 import pytest
 
@@ -48,3 +48,18 @@ def test_a_query_that_is_not_finite_gives_nan(cuda_lib, lens, new, dim, group, c
     assert hit.any() and (bad & ~seen).any() == (min(lens) == 0 or any(n > x for n, x in zip(new, lens)))
     assert out[hit].isnan().all() and lse[hit].isnan().all()
     compare(case, clean, torch.where(hit[..., None], want, out), torch.where(hit, want_lse, lse))
+
+
+@pytest.mark.parametrize("window", [2**31 - 1, 2**31 - 4, 2**31 + 3, 2**32 + 5, 2**63])
+@pytest.mark.parametrize("lens,new,dim,group", [
+    ([1, 3, 40, 0], [4, 8, 40, 3], 128, 2), ([2, 700, 5], [9, 9, 9], 64, 1), ([3, 200], [60, 60], 128, 1),
+    ([5, 129, 400], [300, 300, 300], 64, 1)])
+def test_a_window_that_hides_nothing(cuda_lib, lens, new, dim, group, window):
+    """As wide as int allows, or wider: the results without one, also where a sequence brings more queries than it has
+    tokens."""
+    case = Case(cuda_lib, lens, new, dim=dim, seed=dim + len(lens)).fill()
+    q = case.queries(2 * group, "bfloat16")
+    want = attend(case, q)
+    got = attend(case, q, window=window)
+    assert all(case.torch.equal(a, b) for a, b in zip(got, want))
+    compare(case, q, *got)

@@ -108,3 +108,11 @@ def test_more_sequences_than_are_summed_at_a_time(program, kernel, ahead, n):
     counts = rng.integers(0, 4, n)
     lens = counts + rng.integers(0, 300, n)
     check(program, kernel, ahead, 11, lens.tolist(), counts.tolist(), group=4, kv_heads=1)
+
+
+@KERNELS
+@pytest.mark.parametrize("window", [2**31 - 1, 2**31 - 3])
+def test_a_window_as_wide_as_int_allows(program, kernel, window):
+    """Sequences that bring more queries than they hold tokens: places below 0."""
+    check(program, kernel, 0, 7, [1, 3, 900, 0], [4, 8, 40, 3], group=2, window=window)
+    check(program, kernel, 0, 7, [1, 300], [2000, 5], group=2, window=window)
