@@ -13,7 +13,8 @@
 // themselves (a few loads), then race over a part of one row; their winners
 // go to the workspace as 64-bit keys (weight's bits, then the token
 // inverted).  k_verify_finish: a block per sequence takes the largest key and
-// writes the tokens.
+// writes the tokens.  It may start while k_verify still writes the keys, so they
+// are not read-only to it.
 //
 // Bound: HBM, one row of the target's probabilities, the noise, and after a
 // rejection the draft's row, read once per sequence; 256 sequences over 128,000
@@ -180,7 +181,7 @@ __global__ __launch_bounds__(VERIFY) void k_verify_finish(const T* __restrict__ 
                                                           const int32_t* __restrict__ draft_lens,
                                                           const float* __restrict__ uniforms,
                                                           const float* __restrict__ noise, int64_t n, int t, int vocab,
-                                                          const uint64_t* __restrict__ keys, int parts,
+                                                          const uint64_t* keys, int parts,
                                                           int32_t* __restrict__ tokens, int32_t* __restrict__ accepted) {
   __shared__ uint64_t shared[2][VERIFY / 32];
   const int64_t i = blockIdx.x;
