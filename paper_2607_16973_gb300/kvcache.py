@@ -147,14 +147,23 @@ class KVCache:
         self._lib, self._i32, self._f32, self._u8 = load(), i32, f32, u8
         self._query_types = {torch.bfloat16: 0, torch.float16: 1}
         self._types = _types()
+        self._own = (k, v, k_scale, v_scale, table, lens, refs, self.status)
+        self._streams = set()  # that the cache has been used on by name
+
+    def _used(self, stream, *tensors) -> None:
+        """Keeps the memory of what a call works on until work queued on `stream` is done."""
+        if stream is not None:
+            if stream.cuda_stream not in self._streams:  # (once is enough for as long as they live)
+                self._streams.add(stream.cuda_stream)
+                _used(stream, *self._own)
+            _used(stream, *tensors)
 
     def _entries(self, a, b, name_a: str, name_b: str, stream, extra: int = 0):
         """Two int32 arrays of as many entries (the second `extra` more)."""
         i32, n = self._i32, a.numel()
         if a.dim() != 1 or b.dim() != 1 or b.numel() != n + extra:
             raise ValueError(f"{name_a} must be [n] and {name_b} [n{' + 1' if extra else ''}]")
-        if stream is not None:
-            _used(stream, a, b)
+        self._used(stream, a, b)
         return _ptr(a, name_a, i32), _ptr(b, name_b, i32), n
 
     def _need(self, fn: str, *sizes) -> int:
@@ -172,6 +181,7 @@ class KVCache:
             need = self._need(fn, *sizes)
             workspace = _empty(need, self._u8, self._device, stream)
             return workspace, workspace.data_ptr(), need
+        self._used(stream, workspace)
         return workspace, _dev_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size()
 
     def append(self, layer: int, slots, starts, k, v, stream=None) -> None:
@@ -184,8 +194,7 @@ class KVCache:
         vp, vt, v0, v1, tokens = _rows(v, "v", self._heads, self._dim, self._types)
         if kt != vt or tokens != total:
             raise ValueError("k and v must have one type and shape")
-        if stream is not None:
-            _used(stream, k, v)
+        self._used(stream, k, v)
         check(self._lib.tq_kv_append(self._handle, layer, ps, pt, n, kp, vp, kt, total, k0, k1, v0, v1,
                                      _stream(stream)))
 
@@ -206,8 +215,7 @@ class KVCache:
             raise ValueError(f"q must be [tokens, heads, {self._dim}]")
         heads, dim = q.shape[1], self._dim
         qp, qt, q0, q1, total = _rows(q, "q", heads, dim, self._query_types)
-        if stream is not None:
-            _used(stream, q)
+        self._used(stream, q, out, lse)
         if out is None:
             out = _empty((total, heads, dim), q.dtype, q.device, stream)
             op = out.data_ptr()
@@ -250,6 +258,7 @@ class KVCache:
         """tq_kv_compact: moves the pages in use to the front of the pool; returns
         how many there are (int32 [1] on the device)."""
         workspace, wp, wb = self._workspace(workspace, stream, "tq_kv_compact_workspace")
+        self._used(stream)
         used = _empty(1, _torch().int32, self.k.device, stream)
         check(self._lib.tq_kv_compact(self._handle, used.data_ptr(), wp, wb, _stream(stream)))
         return used
@@ -291,7 +300,7 @@ def verify_drafts(target_probs, drafts, uniforms, noise, draft_probs=None, draft
             ptr(uniforms, "uniforms", f32, n, t), ptr(noise, "noise", f32, n, vocab), n, t, vocab)
     if not target_probs.is_cuda or dtype not in types or not target_probs.is_contiguous():
         _dev_ptr(target_probs, "target_probs", tuple(types))
-    _used(stream, target_probs, draft_probs, drafts, draft_lens, uniforms, noise)
+    _used(stream, target_probs, draft_probs, drafts, draft_lens, uniforms, noise, tokens, accepted, workspace)
     if tokens is None:
         tokens = _empty((n, t + 1), i32, dev, stream)
     if accepted is None:
