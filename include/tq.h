@@ -603,7 +603,9 @@ tq_status tq_kv_append(const tq_kv_cache* cache, int layer, const int32_t* slots
  *   out      device out [total][heads][head_dim], contiguous, q's type:
  *            sum_j exp(s_j) v_j / sum_j exp(s_j)
  *   lse      device out [total][heads] float32 (nullable): ln sum_j exp(s_j)
- *   workspace  device, 16-byte aligned, of ws_bytes >= tq_kv_attend_workspace
+ *   workspace  device, 16-byte aligned, of ws_bytes >= tq_kv_attend_workspace, whose
+ *            bytes are enough for every call of up to n sequences, total queries
+ *            and heads heads: one kept for a program's largest call serves the others
  * A query that sees no token (an empty sequence) gets zeros and -INFINITY.
  * Products are taken in fp16 with exact codes and queries scaled by a power
  * of two; scores, their statistics and the sums are float32, weights fp16

@@ -51,7 +51,8 @@ struct KvRows {  // new keys or values, or queries: rows of head_dim elements
 cudaError_t launch_kv_append(const KvView& kv, int layer, const int32_t* slots, const int32_t* starts, int64_t n,
                              const KvRows& k, const KvRows& v, int type, int64_t total, cudaStream_t s);
 
-size_t kv_attend_workspace(const KvView& kv, int64_t n, int64_t total, int heads);
+size_t kv_attend_needs(const KvView& kv, int64_t n, int64_t total, int heads);      // of this call
+size_t kv_attend_workspace(const KvView& kv, int64_t n, int64_t total, int heads);  // of every one that is not larger
 cudaError_t launch_kv_attend(const KvView& kv, int layer, const int32_t* slots, const int32_t* starts, int64_t n,
                              const KvRows& q, int type, int64_t total, int heads, float scale, int window, void* out,
                              float* lse, void* workspace, cudaStream_t s);

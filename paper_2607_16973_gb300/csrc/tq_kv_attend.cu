@@ -481,10 +481,20 @@ cudaError_t attend_for(const AttendArgs& a, int nt, void* workspace, cudaStream_
 
 }  // namespace
 
-size_t kv_attend_workspace(const KvView& kv, int64_t n, int64_t total, int heads) {
+size_t kv_attend_needs(const KvView& kv, int64_t n, int64_t total, int heads) {
   if (kv_tile_supported(kv, n, total, heads)) return kv_tile_workspace(kv);
   const int nt = row_tiles_of(kv, n, total, heads);
   return attend_workspace(device_sm_count() * per_sm(kv.c.head_dim, nt), 8 * nt, kv.c.head_dim);
+}
+
+// The kernel and its row tiles go by the rows that a sequence brings on average, and
+// fewer sequences may bring as many queries: the most that any of them needs.
+size_t kv_attend_workspace(const KvView& kv, int64_t n, int64_t total, int heads) {
+  size_t need = kv_attend_needs(kv, 1, std::min<int64_t>(total, 1), kv.c.kv_heads);  // (one row: in eights)
+  if (n == 0 || total == 0) return need;
+  if (row_tiles_of(kv, 1, total, heads) == 2)
+    need = std::max(need, attend_workspace(device_sm_count() * per_sm(kv.c.head_dim, 2), 16, kv.c.head_dim));
+  return kv_tile_supported(kv, 1, total, heads) ? std::max(need, kv_tile_workspace(kv)) : need;
 }
 
 cudaError_t launch_kv_attend(const KvView& kv, int layer, const int32_t* slots, const int32_t* starts, int64_t n,

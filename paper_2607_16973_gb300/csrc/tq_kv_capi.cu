@@ -154,7 +154,7 @@ extern "C" tq_status tq_kv_attend(const tq_kv_cache* cache, int layer, const int
   TRY(check_rows(fn, "q", rows, type));
   if (!out || !tq::aligned16(out)) return fail(TQ_EINVAL, "%s: out must be 16-byte aligned", fn);
   if (!aligned(lse, 4)) return fail(TQ_EINVAL, "%s: lse must be 4-byte aligned", fn);
-  TRY(check_workspace(fn, workspace, ws_bytes, tq::kv_attend_workspace(kv, n, total, heads)));
+  TRY(check_workspace(fn, workspace, ws_bytes, tq::kv_attend_needs(kv, n, total, heads)));
   const cudaError_t e = tq::launch_kv_attend(kv, layer, slots, starts, n, rows, type, total, heads, scale, window, out,
                                              lse, workspace, static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? tq::ok() : cuda_fail(fn, e);

@@ -199,7 +199,7 @@ class KVCache:
                                      _stream(stream)))
 
     def attention_workspace(self, n: int, total: int, heads: int) -> int:
-        """tq_kv_attend_workspace: device bytes for `total` queries of n sequences."""
+        """tq_kv_attend_workspace: device bytes for up to `total` queries of up to n sequences and `heads` heads."""
         return self._need("tq_kv_attend_workspace", n, total, heads)
 
     def attention(self, layer: int, slots, starts, q, scale: float | None = None, window: int = 0, out=None,
