@@ -573,7 +573,8 @@ typedef struct tq_kv_cache {
  *            at token * token_stride + head * head_stride + j (strides in
  *            elements, >= 0, any alignment of the elements' own size; 16-byte
  *            aligned rows are read fastest)
- *   total    tokens in all (starts[n]); 0 is a no-op
+ *   total    rows of k and v; 0 is a no-op.  Rows outside [starts[0], starts[n])
+ *            belong to no sequence and are passed over
  * For each block of 16 tokens, head, and of K and V: a = the largest finite |x|
  * of the new tokens; scale = a / 127 (int8) or a / 448 (e4m3) in float32, or the
  * block's present scale if it holds older tokens and that is larger; where the
@@ -594,7 +595,8 @@ tq_status tq_kv_append(const tq_kv_cache* cache, int layer, const int32_t* slots
  * cache.
  *   slots, starts, n, total  as for tq_kv_append: queries starts[i] ..
  *            starts[i+1] - 1 stand at the last places of sequence i, the query
- *            r of m at place p = lens - m + r
+ *            r of m at place p = lens - m + r; queries outside [starts[0],
+ *            starts[n]) belong to no sequence and see no token
  *   q        device, TQ_BF16 or TQ_FP16, [total][heads][head_dim] with strides in
  *            elements; heads is a multiple of kv_heads, head h reads the keys
  *            of head h / (heads / kv_heads)
@@ -606,7 +608,10 @@ tq_status tq_kv_append(const tq_kv_cache* cache, int layer, const int32_t* slots
  *   workspace  device, 16-byte aligned, of ws_bytes >= tq_kv_attend_workspace, whose
  *            bytes are enough for every call of up to n sequences, total queries
  *            and heads heads: one kept for a program's largest call serves the others
- * A query that sees no token (an empty sequence) gets zeros and -INFINITY.
+ * A query that sees no token (an empty sequence) gets zeros and -INFINITY, and so
+ * do those of a sequence that is left out (status) for its slot or length; tokens
+ * whose page is not valid are not seen (status).  An entry whose range of queries
+ * is not valid is left out too (status), and writes nothing.
  * Products are taken in fp16 with exact codes and queries scaled by a power
  * of two; scores, their statistics and the sums are float32, weights fp16
  * relative to the row's largest.  Scores are taken to be below 2^22 ln 2 in

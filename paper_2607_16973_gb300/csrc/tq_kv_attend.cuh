@@ -322,6 +322,10 @@ __device__ __forceinline__ float lse_of(float m, float l) { return l == 0.0f ? -
 // rows of it at once, so that many parts are on their way together (every 4th at
 // head_dim 256).  A part in which a row saw nothing has m = -inf and l = 0 and is
 // left out; m = -inf beside another l is a row of NaN, which joins to NaN.
+//
+// All blocks together also write the queries that no sequence brings, in front of
+// the first one's and behind the last one's (a call padded to a size that is
+// kept): what a query that sees nothing gets.
 constexpr int join_warps(int dim) { return dim == 256 ? 4 : 8; }  // (their sums take 32 KB of shared memory)
 template <typename T, int D, int ROWS>
 __global__ __launch_bounds__(join_warps(D) * 32) void k_kv_join(AttendArgs a) {
@@ -331,7 +335,19 @@ __global__ __launch_bounds__(join_warps(D) * 32) void k_kv_join(AttendArgs a) {
   constexpr int V = E * 4 / sizeof(Vec);
   __shared__ float sh_o[JOIN_WARPS][8][D];
   __shared__ float sh_l[JOIN_WARPS][8], sh_m[JOIN_WARPS][8];
+  const int64_t front = min(max((int64_t)a.starts[0], (int64_t)0), a.total);
+  const int64_t behind = min(max((int64_t)a.starts[a.n], front), a.total), lost = front + a.total - behind;
   griddep_wait();
+  if (lost) {
+    const int pieces = a.heads * (D / 8);  // of 16 bytes, of a token
+    for (int64_t e = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * blockDim.x + threadIdx.x; e < lost * pieces;
+         e += (int64_t)gridDim.x * gridDim.y * blockDim.x) {
+      const int64_t nth = e / pieces, token = nth < front ? nth : behind + nth - front;
+      const int piece = (int)(e - nth * pieces);
+      reinterpret_cast<uint4*>(a.out)[token * pieces + piece] = make_uint4(0, 0, 0, 0);
+      if (a.lse && piece % (D / 8) == 0) a.lse[token * a.heads + piece / (D / 8)] = -INFINITY;
+    }
+  }
   const Split sp = a.splits[blockIdx.x];
   const int row0 = blockIdx.y * 8;
   if (sp.first < 0 || sp.row0 + row0 >= sp.rows) return;

@@ -1,4 +1,5 @@
-"""Attention at the ends of what it is given: queries that are not finite, windows as wide as int."""
+"""Attention at the ends of what it is given: queries that are not finite, windows as wide as int, queries that no
+sequence brings."""
 import numpy as np
 import pytest
 
@@ -63,3 +64,38 @@ def test_a_window_that_hides_nothing(cuda_lib, lens, new, dim, group, window):
     got = attend(case, q, window=window)
     assert all(case.torch.equal(a, b) for a, b in zip(got, want))
     compare(case, q, *got)
+
+
+@pytest.mark.parametrize("rows", [1, 3, 60, 200])
+@pytest.mark.parametrize("front,behind", [(0, 5), (2, 0), (3, 300)])
+def test_queries_that_no_sequence_brings(cuda_lib, rows, front, behind):
+    """A step padded to a size that is kept: queries in front of the first sequence's and behind the last one's get what
+    a query that sees nothing gets, and the others what they get without them."""
+    import torch
+    case = Case(cuda_lib, [700, 30, 250], [rows] * 3, dim=64, kv_heads=1, seed=rows).fill()
+    q = case.queries(2, "float16")
+    want, want_lse = attend(case, q)
+    total = front + q.shape[0] + behind
+    padded = torch.randn(total, 2, 64, device="cuda").to(q.dtype)
+    padded[front: front + q.shape[0]] = q
+    out, lse = torch.full_like(padded, float("nan")), torch.full((total, 2), float("nan"), device="cuda")
+    cache = case.cache()
+    cache.attention(case.layer, case.device(case.slots), case.device(case.starts + front), padded, out=out, lse=lse)
+    cache.check()
+    inside = slice(front, front + q.shape[0])
+    # (which kernel takes a call goes by its queries, so the order of sums may differ)
+    compare(case, q, out[inside], lse[inside])
+    outside = torch.ones(total, dtype=torch.bool, device="cuda")
+    outside[inside] = False
+    assert not out[outside].any() and (lse[outside] == -float("inf")).all()
+
+
+def test_queries_of_sequences_that_bring_none(cuda_lib):
+    import torch
+    case = Case(cuda_lib, [70, 30], [0, 0], dim=128, seed=1).fill()
+    q = torch.randn(9, 4, 128, device="cuda").to(torch.bfloat16)
+    out, lse = torch.full_like(q, 3), torch.full((9, 4), 3.0, device="cuda")
+    cache = case.cache()
+    cache.attention(case.layer, case.device(case.slots), case.device(case.starts), q, out=out, lse=lse)
+    cache.check()
+    assert not out.any() and (lse == -float("inf")).all()
