@@ -86,6 +86,12 @@ def _rows(t, name: str, heads: int, dim: int, types):
     return t.data_ptr(), kind, s0, s1, shape[0]
 
 
+def _checked(c):
+    """Reference to a cache's struct; raises TQError where the calls would refuse it."""
+    check(load().tq_kv_compact_workspace(C.byref(c), C.byref(C.c_size_t())))
+    return C.byref(c)
+
+
 class KVCache:
     """Keys and values of sequences in slots, as 8-bit codes in pages.
 
@@ -102,6 +108,11 @@ class KVCache:
         if min(pages, slots, max_pages, kv_heads, head_dim, page_tokens // BLOCK, layers) < 1:
             raise ValueError("pages, slots, max_pages, kv_heads, head_dim and layers must be positive, "
                              "page_tokens at least 16")
+        if codes not in KV_CODES:
+            raise ValueError(f"codes must be one of {sorted(KV_CODES)}, got {codes!r}")
+        # the library's own checks of the sizes, before any memory is taken (addresses that nothing is read from)
+        _checked(KvCacheStruct(*[BLOCK] * 8, pages, slots, max_pages, layers, kv_heads, head_dim, page_tokens,
+                               KV_CODES[codes]))
         shape = (layers, pages, kv_heads, page_tokens, head_dim)
         scales = (layers, pages, kv_heads, page_tokens // BLOCK)
         i32 = torch.int32
@@ -141,7 +152,7 @@ class KVCache:
             _dev_ptr(v_scale, "v_scale", f32), _dev_ptr(table, "table", i32), _dev_ptr(lens, "lens", i32),
             _dev_ptr(refs, "refs", i32), _dev_ptr(self.status, "status"), pages, table.shape[0], table.shape[1],
             layers, kv_heads, head_dim, page_tokens, KV_CODES[codes])
-        self._handle = C.byref(self._c)
+        self._handle = _checked(self._c)
         self._needs = {}  # workspace bytes by call and sizes
         self._heads, self._dim, self._device = kv_heads, head_dim, k.device
         self._lib, self._i32, self._f32, self._u8 = load(), i32, f32, u8
