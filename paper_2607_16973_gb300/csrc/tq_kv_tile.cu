@@ -331,8 +331,9 @@ __global__ __launch_bounds__(TILE_THREADS, 1) void k_kv_tile(AttendArgs a) {
         if (__any_sync(FULL, real)) {  // (else P of these lanes is whatever S was: nobody reads their O)
           const float(*sc)[8] = sh.scales[(done + j) % SCALE_RING];
           const int t0 = (first + j) * TOKENS;
-          // columns [lo, hi) are seen; they are looked at only where some row does not see them all
-          const int hi = place - t0 + 1, lo = a.window ? max(0, hi) - a.window : 0;
+          // columns [lo, hi) are seen; they are looked at only where some row does not see them
+          // all.  (lo may wrap around only for hi <= 0, where nothing is seen whatever it is.)
+          const int hi = place - t0 + 1, lo = a.window ? (int)((unsigned)hi - (unsigned)a.window) : 0;
           const bool edge = __any_sync(FULL, real && (hi < TOKENS || lo > 0));
           // Half of S at a time (64 columns, 4 blocks): the second half's maximum, the
           // first half's, its weights, and the second half read again for its.  P goes
