@@ -323,9 +323,11 @@ __device__ __forceinline__ float lse_of(float m, float l) { return l == 0.0f ? -
 // head_dim 256).  A part in which a row saw nothing has m = -inf and l = 0 and is
 // left out; m = -inf beside another l is a row of NaN, which joins to NaN.
 //
-// All blocks together also write the queries that no sequence brings, in front of
-// the first one's and behind the last one's (a call padded to a size that is
-// kept): what a query that sees nothing gets.
+// PAD more columns of blocks write the queries that no sequence brings, in front
+// of the first one's and behind the last one's (a call padded to a size that is
+// kept): what a query that sees nothing gets.  (Asked by every block it was 1 us
+// of every call: they start where the attention's blocks end.)
+constexpr int PAD = 16;
 constexpr int join_warps(int dim) { return dim == 256 ? 4 : 8; }  // (their sums take 32 KB of shared memory)
 template <typename T, int D, int ROWS>
 __global__ __launch_bounds__(join_warps(D) * 32) void k_kv_join(AttendArgs a) {
@@ -335,20 +337,22 @@ __global__ __launch_bounds__(join_warps(D) * 32) void k_kv_join(AttendArgs a) {
   constexpr int V = E * 4 / sizeof(Vec);
   __shared__ float sh_o[JOIN_WARPS][8][D];
   __shared__ float sh_l[JOIN_WARPS][8], sh_m[JOIN_WARPS][8];
-  const int64_t front = min(max((int64_t)a.starts[0], (int64_t)0), a.total);
-  const int64_t behind = min(max((int64_t)a.starts[a.n], front), a.total), lost = front + a.total - behind;
-  griddep_wait();
-  if (lost) {
+  if (blockIdx.x < PAD) {
+    const int64_t front = min(max((int64_t)a.starts[0], (int64_t)0), a.total);
+    const int64_t behind = min(max((int64_t)a.starts[a.n], front), a.total);
     const int pieces = a.heads * (D / 8);  // of 16 bytes, of a token
-    for (int64_t e = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * blockDim.x + threadIdx.x; e < lost * pieces;
-         e += (int64_t)gridDim.x * gridDim.y * blockDim.x) {
+    griddep_wait();
+    for (int64_t e = ((int64_t)blockIdx.y * PAD + blockIdx.x) * blockDim.x + threadIdx.x;
+         e < (front + a.total - behind) * pieces; e += (int64_t)gridDim.y * PAD * blockDim.x) {
       const int64_t nth = e / pieces, token = nth < front ? nth : behind + nth - front;
       const int piece = (int)(e - nth * pieces);
-      reinterpret_cast<uint4*>(a.out)[token * pieces + piece] = make_uint4(0, 0, 0, 0);
+      static_cast<uint4*>(a.out)[token * pieces + piece] = make_uint4(0, 0, 0, 0);
       if (a.lse && piece % (D / 8) == 0) a.lse[token * a.heads + piece / (D / 8)] = -INFINITY;
     }
+    return;
   }
-  const Split sp = a.splits[blockIdx.x];
+  griddep_wait();
+  const Split sp = a.splits[blockIdx.x - PAD];
   const int row0 = blockIdx.y * 8;
   if (sp.first < 0 || sp.row0 + row0 >= sp.rows) return;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -422,7 +426,7 @@ __global__ __launch_bounds__(join_warps(D) * 32) void k_kv_join(AttendArgs a) {
 // Workspace: Split [grid] | partial sums.
 template <typename T, int D, int ROWS>
 cudaError_t launch_join(const AttendArgs& a, int grid, cudaStream_t s) {
-  return launch_maybe_pdl(true, k_kv_join<T, D, ROWS>, dim3(grid, ROWS / 8), dim3(join_warps(D) * 32), 0, s, a);
+  return launch_maybe_pdl(true, k_kv_join<T, D, ROWS>, dim3(PAD + grid, ROWS / 8), dim3(join_warps(D) * 32), 0, s, a);
 }
 
 inline size_t split_bytes(int grid) { return ((size_t)grid * sizeof(Split) + 255) / 256 * 256; }
