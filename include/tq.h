@@ -582,6 +582,9 @@ typedef struct tq_kv_cache {
  * rounded again; code = x / scale, rounded to nearest even.  Infinities take
  * the largest code of their sign, NaN and everything at scale 0 takes 0: no
  * code stands for a value that is not finite.
+ * Tokens that tq_kv_truncate cuts off again (rejected drafts) leave this in the
+ * block that they shared with kept ones: its scale stays what they made it, and
+ * the kept codes are rounded to it.
  * Sequences whose slot, length or page is not valid are left out (status).
  */
 tq_status tq_kv_append(const tq_kv_cache* cache, int layer, const int32_t* slots,
@@ -613,8 +616,12 @@ tq_status tq_kv_append(const tq_kv_cache* cache, int layer, const int32_t* slots
  * whose page is not valid are not seen (status).  An entry whose range of queries
  * is not valid is left out too (status), and writes nothing.
  * Products are taken in fp16 with exact codes and queries scaled by a power
- * of two; scores, their statistics and the sums are float32, weights fp16
- * relative to the row's largest.  Scores are taken to be below 2^22 ln 2 in
+ * of two (elements below 2^-22 of their row's largest lose bits); scores, their
+ * statistics and the sums are float32, weights fp16 relative to the row's
+ * largest.  With more than a few queries per key head the values' scales are
+ * folded into the weights, and ones below 2^-100 count as 2^-100.  How a result is
+ * rounded depends on the queries that the call's sequences bring on average and on
+ * where a long sequence is cut; equal calls give equal bits.  Scores are taken to be below 2^22 ln 2 in
  * magnitude: beyond that float32 does not tell them apart to a factor of e^(1/2),
  * and weights may leave fp16's range.  A query with an element that is not
  * finite gives NaN in its whole row of out and in lse, if it sees a token.
@@ -684,7 +691,8 @@ tq_status tq_kv_check(const tq_kv_cache* cache, void* stream);
  * With p_i and q_i the two rows of place i: draft x_i is accepted if u_i q_i(x_i)
  * < p_i(x_i) and those before it were.  Behind a accepted drafts comes argmax_v
  * w(v) / noise(v) (float32; the lowest token of equals), w = max(p_a - q_a, 0) if
- * draft a was rejected (p_a if that is 0 everywhere), p_a if none was; then -1.
+ * draft a was rejected (p_a if no quotient of that is above 0), p_a if none was (token
+ * 0 if no quotient is above 0); then -1.
  * A draft outside [0, vocab) is rejected.  t in [0, 64], vocab in [1, 2^24].
  */
 tq_status tq_verify_drafts_workspace(int64_t n, int64_t vocab, size_t* bytes);

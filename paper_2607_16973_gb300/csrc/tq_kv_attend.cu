@@ -25,9 +25,10 @@
 // The softmax keeps a reference m per row that only moves when a score passes
 // the one it was set to by LAZY: most blocks need no reduction over the warp.
 //
-// Bound: HBM, 2 (D + 1/4) bytes per token and key head; in practice its latency, at
-// 128 registers and 16 warps per SM.  200,001 tokens and 8 key heads (410 MB): 84 us,
-// 4.9 TB/s of 6.8 measured; 128 sequences of 1,000 to 4,096 (663 MB): 115 us, 5.8 TB/s.
+// Bound: HBM, 2 (D + 1/4) bytes per token and key head.  200,001 tokens and 8 key
+// heads (410 MB): 85 us, 4.8 TB/s of 6.8 measured; 100,001 tokens 57, 400,001 143:
+// about 28 us for the start, the first loads, the sums and the join, and the rest at
+// 7 TB/s.  128 sequences of 1,000 to 4,096 (663 MB): 119 us, 5.6 TB/s.
 #include <algorithm>
 
 #include "tq_kv_attend.cuh"

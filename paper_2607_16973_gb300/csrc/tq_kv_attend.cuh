@@ -225,8 +225,10 @@ __device__ __forceinline__ int64_t last_run(int64_t unit, int64_t units, int64_t
 __device__ __forceinline__ int64_t first_run(int64_t unit, int64_t units, int64_t n) { return (unit * n + units - 1) / units; }
 
 // Where run c really starts: not within MIN blocks of an item's ends, but at that
-// end.  Items of less than 2 MIN blocks are never cut, so that a short sequence's
-// result does not depend on the others of its batch.
+// end.  Items of less than 2 MIN blocks are never cut, so that where the cuts fall
+// does not change a short sequence's result.  (The batch still does through the rows
+// that its sequences bring on average: they decide on the kernel and its row tiles,
+// which round weights differently.)
 template <class P>
 __device__ int64_t run_cut(const AttendArgs& a, Units& u, int64_t c, int64_t units, int64_t n) {
   const int64_t x = run_start(c, units, n);

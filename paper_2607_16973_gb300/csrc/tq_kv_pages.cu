@@ -9,8 +9,9 @@
 //
 // Bound: for the tables, latency (one block settles an extend or a compact:
 // scans over the counts, 16,384 pages a step); for pages that move, HBM, read
-// and written once with 16-byte accesses.  1.94 GB of moves: 331 us with all around
-// them, 5.9 TB/s; 256 requests forked and extended by 40 tokens: 28 us.
+// and written once with 16-byte accesses.  1.94 GB of moves: 334 to 340 us with all
+// around them, 5.8 TB/s; 256 requests forked and extended by 40 tokens: 35 us (28 in a
+// graph).
 #include <algorithm>
 
 #include "tq_kv.cuh"

@@ -8,7 +8,9 @@
 // The weight of a token thus is what it adds to the output, and the reference m
 // follows the largest of those, so that P keeps fp16's bits whatever factors lie
 // between the blocks' scales; the softmax's own sum is taken of the same numbers,
-// per block, divided by g.  (g below 2^-100 counts as 2^-100.)
+// per block, divided by g.  (g below 2^-100 counts as 2^-100.  Blocks whose scales lie
+// up to 2^100 apart lose no weight above 2^-36 of the largest: 2^-126 is where a
+// weight's float32 ends.)
 //
 // One CTA per SM, 12 warps (168 registers each):
 //   0-7   softmax: warps 0-3 the first 128 rows, 4-7 the others; a thread per row.
@@ -35,8 +37,8 @@
 // M128 N128 K16, ~100 each) and per row tile 620 for the maxima and 1,400 for the
 // weights.  (Weighing in one pass with the old reference and again where it has to
 // move was slower: 448 us against 418 for two prompts, for want of registers.)
-// A prompt of 2,048 tokens and the last 2,046 of 6,000 (201 GFLOP): 313 us, 643
-// TFLOP/s, 0.34 of the measured rate.  Up to 128 rows the converters bound it: 255 MB of codes in
+// A prompt of 2,048 tokens and the last 2,046 of 6,000 (201 GFLOP): 320 us, 628
+// TFLOP/s, 0.33 of the measured rate.  Up to 128 rows the converters bound it: 255 MB of codes in
 // 154 us.
 #include <algorithm>
 

@@ -18,8 +18,9 @@
 //
 // Bound: HBM, one row of the target's probabilities, the noise, and after a
 // rejection the draft's row, read once per sequence; 256 sequences over 128,000
-// bfloat16 entries (249 MB): 46 us, 5.4 TB/s.  (Blocks of a call per SM: 8 52 us, 16 46,
-// 32 54.)
+// bfloat16 entries (249 MB): 54 us, 4.6 TB/s, on inputs that change from call to call.
+// (In a graph, on one set of inputs, part of them in L2: 46; with 8 blocks of a call
+// per SM 52, with 32 54.)
 #include <algorithm>
 
 #include "tq_kv.cuh"
