@@ -635,6 +635,62 @@ tq_status tq_kv_attend(const tq_kv_cache* cache, int layer, const int32_t* slots
                        float* lse, void* workspace, size_t ws_bytes, void* stream);
 
 /*
+ * tq_kv_cross - attention of queries that are no tokens of the cache's sequences
+ * over all that these hold (a reader over encoded passages): tq_kv_attend without
+ * the order of places.  Arguments, workspace (tq_kv_attend_workspace), arithmetic
+ * and what becomes of empty, padded and invalid entries as there, but every query of
+ * sequence i sees every token of slots[i], whatever the number of queries, and there
+ * is no window.  A slot may be named by several sequences.
+ */
+tq_status tq_kv_cross(const tq_kv_cache* cache, int layer, const int32_t* slots,
+                      const int32_t* starts, int64_t n, const void* q, int type,
+                      int64_t total, int heads, int64_t q_token_stride,
+                      int64_t q_head_stride, float scale, void* out, float* lse,
+                      void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * tq_kv_share - which neighbouring requests of a batch hold the same first pages.
+ *   slots, starts, n  as for tq_kv_attend; b_i = lens - (starts[i+1] - starts[i]),
+ *            the tokens that request i held before its new ones
+ *   plan     device out [3][n] int32: first, members, tokens.  Requests i and i + 1 share
+ *            c_i = min(b_i, b_(i+1), page_tokens * the leading pages that their tables
+ *            name alike) tokens; runs of requests with c > 0 between them are a group:
+ *            requests first .. first + members - 1 share tokens = the smallest c within.
+ *            A request that shares with neither neighbour has (itself, 1, 0).
+ * Requests that hold copies of one passage (tq_kv_fork) have to stand side by side.
+ * One whose slot or length is not valid, or that brings more tokens than it holds,
+ * shares nothing (status).
+ */
+tq_status tq_kv_share(const tq_kv_cache* cache, const int32_t* slots,
+                      const int32_t* starts, int64_t n, int32_t* plan, void* stream);
+
+/*
+ * tq_kv_attend_shared - tq_kv_attend without a window for a batch whose requests
+ * share tokens: a group's shared tokens are read once, from its first request's
+ * pages, for the queries of all its requests; each request's other tokens by
+ * itself; the two sums are joined in float32.
+ *   plan     device [3][n] int32, as tq_kv_share writes it.  It stays right for as long as
+ *            the requests hold those tokens: for every layer of a step, and for later
+ *            steps of the same requests
+ *   groups   in [1, n]: how many groups and single requests the plan has; it decides
+ *            which kernel takes the shared tokens, and costs time alone where it is wrong
+ *   workspace  device, 16-byte aligned, of ws_bytes >= tq_kv_attend_shared_workspace
+ *            (enough for every smaller call too)
+ * The other arguments as for tq_kv_attend.  An entry with tokens <= 0 or members <= 1
+ * shares nothing.  One that does not fit (tokens < 0; another request of its group
+ * that names another group; shared tokens that the request or the group's first does
+ * not hold before its new ones) is attended by itself (status).
+ */
+tq_status tq_kv_attend_shared_workspace(const tq_kv_cache* cache, int64_t n,
+                                        int64_t total, int heads, size_t* bytes);
+tq_status tq_kv_attend_shared(const tq_kv_cache* cache, int layer, const int32_t* slots,
+                              const int32_t* starts, const int32_t* plan, int64_t n,
+                              int64_t groups, const void* q, int type, int64_t total,
+                              int heads, int64_t q_token_stride, int64_t q_head_stride,
+                              float scale, void* out, float* lse, void* workspace,
+                              size_t ws_bytes, void* stream);
+
+/*
  * Pages.  Arrays of n entries are device int32; the slots an array names are
  * distinct.
  * tq_kv_fork      slot dst[i] gives up what it held and holds what src[i] holds,
@@ -701,6 +757,39 @@ tq_status tq_verify_drafts(const void* target, const void* draft, int type,
                            const float* uniforms, const float* noise, int64_t n, int t,
                            int vocab, int32_t* tokens, int32_t* accepted,
                            void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * tq_sample - draws the next token of each of n rows of logits from given random
+ * numbers.
+ *   logits   device [n][vocab], `type` TQ_FP32, TQ_BF16 or TQ_FP16, rows logits_stride
+ *            elements apart (any alignment of the elements' own size).  -INFINITY masks
+ *            a token; NaN counts as -INFINITY, +INFINITY as the largest float
+ *   noise    device [n][vocab] float32 > 0 and finite, exponentially distributed, rows
+ *            noise_stride elements apart
+ *   temperature, top_k, top_p, min_p  device [n] each, nullable (1, 0, 1, 0)
+ *   tokens   device out [n] int32
+ *   logprobs device out [n] float32 (nullable): x_token - ln sum_v e^(x_v), at
+ *            temperature 1 and over all tokens
+ *   workspace  device, 16-byte aligned, of ws_bytes >= tq_sample_workspace (enough for
+ *            every smaller call too)
+ * With w_v = e^((x_v - max x) / temperature) and the tokens in the order of x, largest
+ * first, the lower token first among equals: the first top_k of them are kept (all
+ * for top_k <= 0); of those, the ones with less than top_p times those' weight in front of
+ * them (all for top_p >= 1); of those, the ones with w >= min_p; the first always. The
+ * token is the kept one with the largest w / noise, the lowest of equals. A
+ * temperature that is 0, negative or NaN keeps the first alone, and so does a top_p or
+ * min_p of NaN. A row without a token that is not masked gives token 0 and -INFINITY.
+ * The answer is that of these definitions in 64 bits but for tokens whose weight, or
+ * the weight in front of them, is within 2^-20 of a border, and weights below
+ * 2^-126, which count as 0. n in [0, 65535], vocab in [1, 2^24].
+ */
+tq_status tq_sample_workspace(int64_t n, int64_t vocab, size_t* bytes);
+tq_status tq_sample(const void* logits, int type, int64_t logits_stride,
+                    const float* noise, int64_t noise_stride, int64_t n, int vocab,
+                    const float* temperature, const int32_t* top_k,
+                    const float* top_p, const float* min_p, int32_t* tokens,
+                    float* logprobs, void* workspace, size_t ws_bytes,
+                    void* stream);
 
 #ifdef __cplusplus
 }

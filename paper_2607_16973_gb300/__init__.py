@@ -15,7 +15,7 @@ from ._lib import (MARGINALS, PATHS, SCALE_MODES, TQ_EUNSUPPORTED, TQError, chec
 
 __all__ = ["codebook", "rotation", "encode", "encode_plan", "encode_plan_bytes", "encode_workspace", "encode_check", "calibrate", "Filter", "IdMap", "Index", "search", "search_workspace",
            "search_from_host", "search_host_staging", "search_check", "merge_topk", "set_search_path",
-           "profile_events", "search_kernel", "row_bytes", "load", "TQError", "KVCache", "verify_drafts"]
+           "profile_events", "search_kernel", "row_bytes", "load", "TQError", "KVCache", "verify_drafts", "sample_tokens"]
 
 
 def _torch():
@@ -470,4 +470,4 @@ def profile_events(start=None, stop=None) -> None:
 
 
 from .index import Index  # noqa: E402  (index.py builds on the calls above)
-from .kvcache import KVCache, verify_drafts  # noqa: E402
+from .kvcache import KVCache, sample_tokens, verify_drafts  # noqa: E402

@@ -93,6 +93,14 @@ SIGNATURES = {
     "tq_kv_attend": (C.c_int, [_KV, C.c_int, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int, C.c_int64,
                                C.c_int, C.c_int64, C.c_int64, C.c_float, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p,
                                C.c_size_t, C.c_void_p]),
+    "tq_kv_cross": (C.c_int, [_KV, C.c_int, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int, C.c_int64,
+                              C.c_int, C.c_int64, C.c_int64, C.c_float, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t,
+                              C.c_void_p]),
+    "tq_kv_share": (C.c_int, [_KV, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]),
+    "tq_kv_attend_shared_workspace": (C.c_int, [_KV, C.c_int64, C.c_int64, C.c_int, C.POINTER(C.c_size_t)]),
+    "tq_kv_attend_shared": (C.c_int, [_KV, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_int64,
+                                      C.c_void_p, C.c_int, C.c_int64, C.c_int, C.c_int64, C.c_int64, C.c_float,
+                                      C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
     "tq_kv_fork": (C.c_int, [_KV, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]),
     "tq_kv_extend_workspace": (C.c_int, [_KV, C.c_int64, C.POINTER(C.c_size_t)]),
     "tq_kv_extend": (C.c_int, [_KV, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]),
@@ -104,6 +112,10 @@ SIGNATURES = {
     "tq_verify_drafts": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                                    C.c_int64, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t,
                                    C.c_void_p]),
+    "tq_sample_workspace": (C.c_int, [C.c_int64, C.c_int64, C.POINTER(C.c_size_t)]),
+    "tq_sample": (C.c_int, [C.c_void_p, C.c_int, C.c_int64, C.c_void_p, C.c_int64, C.c_int64, C.c_int, C.c_void_p,
+                            C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t,
+                            C.c_void_p]),
 }
 
 _lib = None

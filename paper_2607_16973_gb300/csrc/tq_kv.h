@@ -51,11 +51,27 @@ struct KvRows {  // new keys or values, or queries: rows of head_dim elements
 cudaError_t launch_kv_append(const KvView& kv, int layer, const int32_t* slots, const int32_t* starts, int64_t n,
                              const KvRows& k, const KvRows& v, int type, int64_t total, cudaStream_t s);
 
+// What the rows of an attention call see of a sequence.
+enum class KvSees : int {
+  CAUSAL,  // the tokens up to their own place
+  ALL,     // all of them
+  SHARED,  // the tokens that a plan's requests share (sums only)
+  OWN,     // the others, up to their own place; joined with the shared ones' sums
+};
+
 size_t kv_attend_needs(const KvView& kv, int64_t n, int64_t total, int heads);      // of this call
 size_t kv_attend_workspace(const KvView& kv, int64_t n, int64_t total, int heads);  // of every one that is not larger
 cudaError_t launch_kv_attend(const KvView& kv, int layer, const int32_t* slots, const int32_t* starts, int64_t n,
                              const KvRows& q, int type, int64_t total, int heads, float scale, int window, void* out,
-                             float* lse, void* workspace, cudaStream_t s);
+                             float* lse, void* workspace, cudaStream_t s, bool all = false);
+
+size_t kv_shared_workspace(const KvView& kv, int64_t n, int64_t total, int heads);
+cudaError_t launch_kv_attend_shared(const KvView& kv, int layer, const int32_t* slots, const int32_t* starts,
+                                    const int32_t* plan, int64_t n, int64_t groups, const KvRows& q, int type,
+                                    int64_t total, int heads, float scale, void* out, float* lse, void* workspace,
+                                    cudaStream_t s);
+cudaError_t launch_kv_share(const KvView& kv, const int32_t* slots, const int32_t* starts, int64_t n, int32_t* plan,
+                            cudaStream_t s);
 
 cudaError_t launch_kv_fork(const KvView& kv, const int32_t* dst, const int32_t* src, int64_t n, cudaStream_t s);
 size_t kv_extend_workspace(const KvView& kv, int64_t n);

@@ -110,7 +110,7 @@ __global__ __launch_bounds__(THREADS, per_sm(D, NT)) void k_kv_attend(AttendArgs
   constexpr int MT = D / 16;  // m-tiles of O^T
   __shared__ Units units;
   __shared__ Run run;
-  __shared__ float sh_o[WARPS][ROWS][D + 4];
+  __shared__ alignas(16) float sh_o[WARPS][ROWS][D + 4];  // (read two at a time)
   __shared__ float sh_m[WARPS][ROWS], sh_l[WARPS][ROWS];
 
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
@@ -183,12 +183,13 @@ __global__ __launch_bounds__(THREADS, per_sm(D, NT)) void k_kv_attend(AttendArgs
       for (int h = 0; h < 2; ++h) {
         unscale[nt][h] = __shfl_sync(FULL, down, (2 * t + h) * 4);
         const int r = row0 + nt * 8 + 2 * t + h;
-        place[nt][h] = r < rows ? max(-1, sq.len - sq.count + r / a.group) : -1;
+        place[nt][h] = r < rows ? max(-1, dense(a) ? sq.len - 1 : sq.len - sq.count + r / a.group) : -1;
       }
     }
     const int blk = span.first + run.seg.b_first, blk_end = span.first + run.seg.b_last;
     // blocks that every row of the tile sees whole
-    const int whole_from = a.window && span.place_hi >= a.window ? (span.place_hi - a.window) / kKvBlock + 1 : 0;
+    const int whole_from = max((sq.from + kKvBlock - 1) / kKvBlock,
+                               a.window && span.place_hi >= a.window ? (span.place_hi - a.window) / kKvBlock + 1 : 0);
     const int whole_to = span.place_lo >= 0 ? (span.place_lo + 1) / kKvBlock : 0;
 
     float o[NT][MT][4], m[NT][2], l[NT][2];
@@ -312,7 +313,7 @@ __global__ __launch_bounds__(THREADS, per_sm(D, NT)) void k_kv_attend(AttendArgs
             float y = s[nt][x] * (k_scale * unscale[nt][h]);
             if (!whole) {
               const int tok = b * kKvBlock + g + (x >> 1) * 8;
-              if (tok > place[nt][h] || (a.window && tok <= place[nt][h] - a.window)) y = -INFINITY;
+              if (tok > place[nt][h] || tok < sq.from || (a.window && tok <= place[nt][h] - a.window)) y = -INFINITY;
             }
             s[nt][x] = y;
             rise |= y > m[nt][h] + (LEAD + LAZY);
@@ -418,6 +419,9 @@ __global__ __launch_bounds__(THREADS, per_sm(D, NT)) void k_kv_attend(AttendArgs
         sum += f[x] * sh_l[x][row];
       }
       const int64_t at = out_row(a, done.it.s.token, done.it.head, done.row0 + row);
+      const bool sums = a.sees == KvSees::SHARED;
+      const int from = done.whole ? done.it.s.from : 0;
+      const Both both = join_shared(a, D, at, from, top, sum);
       const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
       for (int d = lane * 2; d < D; d += 64) {
         float y0 = 0.0f, y1 = 0.0f;
@@ -427,7 +431,14 @@ __global__ __launch_bounds__(THREADS, per_sm(D, NT)) void k_kv_attend(AttendArgs
           y0 += f[x] * z.x;
           y1 += f[x] * z.y;
         }
-        if (done.whole) {
+        if (done.whole && sums) {
+          *reinterpret_cast<float2*>(a.sums + at * D + d) = make_float2(y0, y1);
+        } else if (done.whole) {
+          if (from > 0) {
+            const float2 z = *reinterpret_cast<const float2*>(a.sums + at * D + d);
+            y0 = y0 * both.own + z.x * both.shared;
+            y1 = y1 * both.own + z.y * both.shared;
+          }
           T* out = static_cast<T*>(a.out) + at * D + d;
           out[0] = from_float<T>(y0 * inv);
           out[1] = from_float<T>(y1 * inv);
@@ -439,6 +450,9 @@ __global__ __launch_bounds__(THREADS, per_sm(D, NT)) void k_kv_attend(AttendArgs
         if (!done.whole) {
           part[ROWS * D + row] = top;
           part[ROWS * (D + 1) + row] = sum;
+        } else if (sums) {
+          *sums_m(a, D, at) = top;
+          *sums_l(a, D, at) = sum;
         } else if (a.lse) {
           a.lse[at] = lse_of(top, sum);
         }
@@ -498,14 +512,46 @@ size_t kv_attend_workspace(const KvView& kv, int64_t n, int64_t total, int heads
   return kv_tile_supported(kv, 1, total, heads) ? std::max(need, kv_tile_workspace(kv)) : need;
 }
 
+namespace {
+
+cudaError_t launch(const AttendArgs& a, int type, int64_t sequences, void* workspace, cudaStream_t s) {
+  if (kv_tile_supported(a.kv, sequences, a.total, a.heads)) return launch_kv_tile(a, type, workspace, s);
+  const int nt = row_tiles_of(a.kv, sequences, a.total, a.heads);
+  return type == TQ_BF16 ? attend_for<__nv_bfloat16>(a, nt, workspace, s) : attend_for<__half>(a, nt, workspace, s);
+}
+
+size_t sums_bytes(const KvView& kv, int64_t total, int heads) {
+  return ((size_t)total * heads * (kv.c.head_dim + 2) * sizeof(float) + 255) / 256 * 256;
+}
+
+}  // namespace
+
 cudaError_t launch_kv_attend(const KvView& kv, int layer, const int32_t* slots, const int32_t* starts, int64_t n,
                              const KvRows& q, int type, int64_t total, int heads, float scale, int window, void* out,
-                             float* lse, void* workspace, cudaStream_t s) {
-  AttendArgs a = {kv, layer, slots, starts, n, total, q, false, heads, heads / kv.c.kv_heads, scale, window, out, lse,
-                  nullptr, nullptr};
-  if (kv_tile_supported(kv, n, total, heads)) return launch_kv_tile(a, type, workspace, s);
-  const int nt = row_tiles_of(kv, n, total, heads);
-  return type == TQ_BF16 ? attend_for<__nv_bfloat16>(a, nt, workspace, s) : attend_for<__half>(a, nt, workspace, s);
+                             float* lse, void* workspace, cudaStream_t s, bool all) {
+  const AttendArgs a = {kv, layer, slots, starts, n, total, q, false, heads, heads / kv.c.kv_heads, scale, window, out,
+                        lse, nullptr, nullptr, all ? KvSees::ALL : KvSees::CAUSAL, nullptr, nullptr};
+  return launch(a, type, n, workspace, s);
+}
+
+// Workspace: the shared tokens' sums | what either attention needs (one after the other).
+size_t kv_shared_workspace(const KvView& kv, int64_t n, int64_t total, int heads) {
+  return sums_bytes(kv, total, heads) + kv_attend_workspace(kv, n, total, heads);
+}
+
+// The shared tokens first, each group's once for all its queries, their sums left in
+// float32; then each request's own, which its last kernel joins with them.
+cudaError_t launch_kv_attend_shared(const KvView& kv, int layer, const int32_t* slots, const int32_t* starts,
+                                    const int32_t* plan, int64_t n, int64_t groups, const KvRows& q, int type,
+                                    int64_t total, int heads, float scale, void* out, float* lse, void* workspace,
+                                    cudaStream_t s) {
+  AttendArgs a = {kv, layer, slots, starts, n, total, q, false, heads, heads / kv.c.kv_heads, scale, 0, out, lse,
+                  nullptr, nullptr, KvSees::SHARED, plan, static_cast<float*>(workspace)};
+  void* rest = static_cast<char*>(workspace) + sums_bytes(kv, total, heads);
+  const cudaError_t e = launch(a, type, groups, rest, s);
+  if (e != cudaSuccess) return e;
+  a.sees = KvSees::OWN;
+  return launch(a, type, n, rest, s);
 }
 
 }  // namespace tq

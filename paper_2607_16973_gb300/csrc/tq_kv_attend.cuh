@@ -30,6 +30,9 @@ struct AttendArgs {
   float* lse;
   float* parts;          // [2 * grid][rows * (D + 2)]: partial O, m, l
   struct Split* splits;  // [grid]
+  KvSees sees;
+  const int32_t* plan;   // [3][n]: tq_kv_share
+  float* sums;           // shared tokens: O [total * heads][D], then m, then l of every row
 };
 
 // The item that a run continues, left for k_kv_join by the first run that does.
@@ -37,7 +40,11 @@ struct Split {
   int first, last;      // runs that have a part of it; first = -1: none to join
   int token, head;      // first token of its sequence, its key head
   int row0, rows;       // first row of its tile, rows of its sequence
+  int from;             // first token that it sees
 };
+
+// Whether every query sees all tokens, whatever its place.
+__host__ __device__ inline bool dense(const AttendArgs& a) { return a.sees == KvSees::ALL || a.sees == KvSees::SHARED; }
 
 // Rows per key head that a sequence of the call brings on average.
 inline int64_t attend_rows(const KvView& kv, int64_t n, int64_t total, int heads) {
@@ -83,10 +90,10 @@ __device__ __forceinline__ Span tile_span(const AttendArgs& a, const KvSeq& s, i
   Span w;
   const unsigned group = (unsigned)a.group, row0 = (unsigned)tile * P::ROWS;
   const unsigned last = min((unsigned)s.count * group, row0 + P::ROWS) - 1;
-  w.place_lo = s.len - s.count + (int)(row0 / group);
-  w.place_hi = s.len - s.count + (int)(last / group);
+  w.place_lo = dense(a) ? s.len - 1 : s.len - s.count + (int)(row0 / group);
+  w.place_hi = dense(a) ? s.len - 1 : s.len - s.count + (int)(last / group);
   // (a row in front of the sequence's first token sees nothing; its place may be as far below 0 as int reaches)
-  w.first = a.window ? max(0, max(0, w.place_lo) - a.window + 1) / P::BLOCK : 0;
+  w.first = max(s.from, a.window ? max(0, max(0, w.place_lo) - a.window + 1) : 0) / P::BLOCK;
   w.blocks = w.place_hi < 0 ? 0 : max(0, w.place_hi / P::BLOCK + 1 - w.first);
   return w;
 }
@@ -95,6 +102,47 @@ __device__ __forceinline__ Span tile_span(const AttendArgs& a, const KvSeq& s, i
 template <class P>
 __device__ __forceinline__ int tiles_of(const AttendArgs& a, const KvSeq& s) {
   return (int)(((unsigned)s.count * (unsigned)a.group + P::ROWS - 1) / P::ROWS);
+}
+
+// Whether request i shares tokens that its plan's entry says: false, with `bad` set,
+// where the entry does not fit the call (it is then attended by itself).  Both sides
+// of the call, the shared tokens' and the requests' own, ask here.
+__device__ __forceinline__ bool shares(const AttendArgs& a, int64_t i, const KvSeq& s, int& first, int& members,
+                                       int& tokens, bool& bad) {
+  first = a.plan[i], members = a.plan[a.n + i], tokens = a.plan[2 * a.n + i];
+  bad = tokens < 0;
+  if (tokens <= 0 || members <= 1) return false;
+  bad = true;
+  if (first < 0 || first > i || members > a.n - first || i >= (int64_t)first + members) return false;
+  if (a.plan[first] != first || a.plan[a.n + first] != members || a.plan[2 * a.n + first] != tokens) return false;
+  KvSeq lead;  // its pages hold the tokens, its group's queries lie side by side
+  if (!kv_seq(a.kv, a.slots, a.starts, first, a.total, true, lead) || lead.len - lead.count < tokens) return false;
+  const int end = a.starts[first + members];
+  if (end > a.total || s.token < lead.token || s.token + s.count > end || s.len - s.count < tokens) return false;
+  bad = false;
+  return true;
+}
+
+// Sequence i as this call's rows see it; false where it is left out.
+__device__ __forceinline__ bool attend_seq(const AttendArgs& a, int64_t i, KvSeq& s, bool& bad) {
+  bad = false;
+  if (!kv_seq(a.kv, a.slots, a.starts, i, a.total, true, s)) {
+    bad = a.sees != KvSees::SHARED;  // (the requests' own side says it)
+    if (a.sees == KvSees::SHARED) s.count = 0;
+    return false;
+  }
+  if (a.sees == KvSees::SHARED || a.sees == KvSees::OWN) {
+    int first, members, tokens;
+    const bool shared = shares(a, i, s, first, members, tokens, bad);
+    if (a.sees == KvSees::OWN) {
+      s.from = shared ? tokens : 0;
+    } else {
+      bad = false;
+      s.count = shared && first == i ? a.starts[first + members] - s.token : 0;
+      s.len = tokens;
+    }
+  }
+  return true;
 }
 
 // Sums of the sequences' units, found by a whole block: before[i] is what lies
@@ -117,11 +165,12 @@ __device__ void load_chunk(const AttendArgs& a, Units& u, int64_t base, int64_t 
     if (threadIdx.x < SCAN) {
       if (base + j < a.n) {
         KvSeq s;
-        if (!kv_seq(a.kv, a.slots, a.starts, base + j, a.total, true, s)) {
-          if (blockIdx.x == 0) kv_status(a.kv, kKvBadEntry);
+        bool bad;
+        if (!attend_seq(a, base + j, s, bad)) {
           s.len = 0;
           if (s.token < 0 || s.count < 0 || s.count > a.total || s.token > a.total - s.count) s.count = 0;
         }
+        if (bad && blockIdx.x == 0) kv_status(a.kv, kKvBadEntry);
         u.seq[j] = s;
         const int tiles = tiles_of<P>(a, s);
         for (int t = 0; t < tiles; ++t) mine += P::ITEM + tile_span<P>(a, s, t).blocks;
@@ -299,7 +348,7 @@ __device__ __forceinline__ void next_segment(const AttendArgs& a, Units& units, 
         const int first = (int)first_run(g.it.begin + P::ITEM + P::MIN, run.all, run.n_runs) - 1;
         if (first + 1 == (int)blockIdx.x)
           a.splits[blockIdx.x] = {first,         (int)last_run(g.it.begin + g.it.units - P::MIN, run.all, run.n_runs),
-                                  g.it.s.token, g.it.head, g.row0, g.rows};
+                                  g.it.s.token, g.it.head, g.row0, g.rows, g.it.s.from};
       }
     }
   }
@@ -318,6 +367,28 @@ __device__ __forceinline__ int64_t out_row(const AttendArgs& a, int token, int h
 }
 // (l = 0: nothing was seen; NaN: the query is not finite)
 __device__ __forceinline__ float lse_of(float m, float l) { return l == 0.0f ? -INFINITY : m * LN2 + logf(l); }
+
+// What the shared tokens give row `at` of the output: its place in the sums.
+__device__ __forceinline__ float* sums_m(const AttendArgs& a, int dim, int64_t at) {
+  return a.sums + a.total * a.heads * dim + at;
+}
+__device__ __forceinline__ float* sums_l(const AttendArgs& a, int dim, int64_t at) {
+  return a.sums + a.total * a.heads * (dim + 1) + at;
+}
+// A row's own sums (m, l) and the shared tokens' joined: factors of either O; m and
+// l of both are left in place.  Without shared tokens (from = 0) its own stay as they are.
+struct Both {
+  float own, shared;
+};
+__device__ __forceinline__ Both join_shared(const AttendArgs& a, int dim, int64_t at, int from, float& m, float& l) {
+  if (from <= 0) return {1.0f, 0.0f};
+  const float ms = *sums_m(a, dim, at), ls = *sums_l(a, dim, at), top = fmaxf(m, ms);
+  // (both -inf: sums of 0, or NaN)
+  const Both f = {top > -INFINITY ? ex2(m - top) : 1.0f, top > -INFINITY ? ex2(ms - top) : 1.0f};
+  l = l * f.own + ls * f.shared;
+  m = top;
+  return f;
+}
 
 // Joins the items that several runs share, in the runs' order: a block per run
 // that continues one and 8 of its rows.  A warp takes every 8th part, the 8
@@ -340,6 +411,7 @@ __global__ __launch_bounds__(join_warps(D) * 32) void k_kv_join(AttendArgs a) {
   __shared__ float sh_o[JOIN_WARPS][8][D];
   __shared__ float sh_l[JOIN_WARPS][8], sh_m[JOIN_WARPS][8];
   if (blockIdx.x < PAD) {
+    if (a.sees == KvSees::SHARED) return;  // (the requests' own side writes them)
     const int64_t front = min(max((int64_t)a.starts[0], (int64_t)0), a.total);
     const int64_t behind = min(max((int64_t)a.starts[a.n], front), a.total);
     const int pieces = a.heads * (D / 8);  // of 16 bytes, of a token
@@ -417,10 +489,23 @@ __global__ __launch_bounds__(join_warps(D) * 32) void k_kv_join(AttendArgs a) {
       for (int e = 0; e < E; ++e) y[e] += f * sh_o[x][r][lane * E + e];
     }
     const int64_t at = out_row(a, sp.token, sp.head, sp.row0 + row0 + r);
+    if (a.sees == KvSees::SHARED) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) a.sums[at * D + lane * E + e] = y[e];
+      if (lane == 0) {
+        *sums_m(a, D, at) = top;
+        *sums_l(a, D, at) = sum;
+      }
+      continue;
+    }
+    const Both f = join_shared(a, D, at, sp.from, top, sum);
     const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
     T* out = static_cast<T*>(a.out) + at * D + lane * E;
 #pragma unroll
-    for (int e = 0; e < E; ++e) out[e] = from_float<T>(y[e] * inv);
+    for (int e = 0; e < E; ++e) {
+      if (sp.from > 0) y[e] = y[e] * f.own + a.sums[at * D + lane * E + e] * f.shared;
+      out[e] = from_float<T>(y[e] * inv);
+    }
     if (a.lse && lane == 0) a.lse[at] = lse_of(top, sum);
   }
 }

@@ -1,4 +1,4 @@
-// C ABI entry points of the 8-bit key-value cache and of draft verification:
+// C ABI entry points of the 8-bit key-value cache, of draft verification and of sampling:
 // every argument is checked before any work is queued.
 #include <cuda_runtime.h>
 
@@ -6,6 +6,7 @@
 
 #include "tq_internal.h"
 #include "tq_kv.h"
+#include "tq_sample.h"
 
 using tq::fail;
 
@@ -134,29 +135,119 @@ extern "C" tq_status tq_kv_attend_workspace(const tq_kv_cache* cache, int64_t n,
   return tq::ok();
 }
 
+// What the attention calls have in common: the queries and where their results go.
+struct AttendCall {
+  const tq_kv_cache* cache;
+  int layer;
+  const int32_t *slots, *starts;
+  int64_t n;
+  tq::KvRows q;
+  int type;
+  int64_t total;
+  int heads;
+  float scale;
+  void* out;
+  float* lse;
+  void* workspace;
+};
+
+static tq_status check_call(const char* fn, const AttendCall& c, tq::KvView& kv) {
+  TRY(view(fn, c.cache, kv));
+  TRY(check_layer(fn, kv, c.layer));
+  TRY(check_attend(fn, kv, c.n, c.total, c.heads));
+  if (c.type != TQ_BF16 && c.type != TQ_FP16)
+    return fail(TQ_EINVAL, "%s: type %d: queries are TQ_BF16 or TQ_FP16", fn, c.type);
+  if (!std::isfinite(c.scale)) return fail(TQ_EINVAL, "%s: scale is not finite", fn);
+  return TQ_OK;
+}
+
+// (`none`: there is nothing to do)
+static tq_status check_arrays(const char* fn, const AttendCall& c, bool& none) {
+  none = c.total == 0;
+  if (none) return TQ_OK;
+  if (c.n == 0) return fail(TQ_EINVAL, "%s: total=%lld queries of no sequence", fn, (long long)c.total);
+  TRY(check_index(fn, c.slots, c.starts));
+  TRY(check_rows(fn, "q", c.q, c.type));
+  if (!c.out || !tq::aligned16(c.out)) return fail(TQ_EINVAL, "%s: out must be 16-byte aligned", fn);
+  if (!aligned(c.lse, 4)) return fail(TQ_EINVAL, "%s: lse must be 4-byte aligned", fn);
+  return TQ_OK;
+}
+
+static tq_status attend(const char* fn, const AttendCall& c, int window, size_t ws_bytes, bool all, void* stream) {
+  tq::KvView kv;
+  bool none;
+  TRY(check_call(fn, c, kv));
+  if (window < 0) return fail(TQ_EINVAL, "%s: window=%d is negative", fn, window);
+  TRY(check_arrays(fn, c, none));
+  if (none) return tq::ok();
+  TRY(check_workspace(fn, c.workspace, ws_bytes, tq::kv_attend_needs(kv, c.n, c.total, c.heads)));
+  const cudaError_t e =
+      tq::launch_kv_attend(kv, c.layer, c.slots, c.starts, c.n, c.q, c.type, c.total, c.heads, c.scale, window, c.out,
+                           c.lse, c.workspace, static_cast<cudaStream_t>(stream), all);
+  return e == cudaSuccess ? tq::ok() : cuda_fail(fn, e);
+}
+
 extern "C" tq_status tq_kv_attend(const tq_kv_cache* cache, int layer, const int32_t* slots, const int32_t* starts,
                                   int64_t n, const void* q, int type, int64_t total, int heads,
                                   int64_t q_token_stride, int64_t q_head_stride, float scale, int window, void* out,
                                   float* lse, void* workspace, size_t ws_bytes, void* stream) {
-  const char* fn = "tq_kv_attend";
+  return attend("tq_kv_attend", {cache, layer, slots, starts, n, {q, q_token_stride, q_head_stride}, type, total, heads,
+                                 scale, out, lse, workspace},
+                window, ws_bytes, false, stream);
+}
+
+extern "C" tq_status tq_kv_cross(const tq_kv_cache* cache, int layer, const int32_t* slots, const int32_t* starts,
+                                 int64_t n, const void* q, int type, int64_t total, int heads, int64_t q_token_stride,
+                                 int64_t q_head_stride, float scale, void* out, float* lse, void* workspace,
+                                 size_t ws_bytes, void* stream) {
+  return attend("tq_kv_cross", {cache, layer, slots, starts, n, {q, q_token_stride, q_head_stride}, type, total, heads,
+                                scale, out, lse, workspace},
+                0, ws_bytes, true, stream);
+}
+
+extern "C" tq_status tq_kv_share(const tq_kv_cache* cache, const int32_t* slots, const int32_t* starts, int64_t n,
+                                 int32_t* plan, void* stream) {
+  const char* fn = "tq_kv_share";
   tq::KvView kv;
   TRY(view(fn, cache, kv));
-  TRY(check_layer(fn, kv, layer));
-  TRY(check_attend(fn, kv, n, total, heads));
-  if (type != TQ_BF16 && type != TQ_FP16)
-    return fail(TQ_EINVAL, "%s: type %d: queries are TQ_BF16 or TQ_FP16", fn, type);
-  if (!std::isfinite(scale)) return fail(TQ_EINVAL, "%s: scale is not finite", fn);
-  if (window < 0) return fail(TQ_EINVAL, "%s: window=%d is negative", fn, window);
-  if (total == 0) return tq::ok();
-  if (n == 0) return fail(TQ_EINVAL, "%s: total=%lld queries of no sequence", fn, (long long)total);
+  TRY(check_entries(fn, kv, n));
+  if (n == 0) return tq::ok();
   TRY(check_index(fn, slots, starts));
-  const tq::KvRows rows = {q, q_token_stride, q_head_stride};
-  TRY(check_rows(fn, "q", rows, type));
-  if (!out || !tq::aligned16(out)) return fail(TQ_EINVAL, "%s: out must be 16-byte aligned", fn);
-  if (!aligned(lse, 4)) return fail(TQ_EINVAL, "%s: lse must be 4-byte aligned", fn);
-  TRY(check_workspace(fn, workspace, ws_bytes, tq::kv_attend_needs(kv, n, total, heads)));
-  const cudaError_t e = tq::launch_kv_attend(kv, layer, slots, starts, n, rows, type, total, heads, scale, window, out,
-                                             lse, workspace, static_cast<cudaStream_t>(stream));
+  if (!plan || !aligned(plan, 4)) return fail(TQ_EINVAL, "%s: plan must be 4-byte aligned and not NULL", fn);
+  const cudaError_t e = tq::launch_kv_share(kv, slots, starts, n, plan, static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? tq::ok() : cuda_fail(fn, e);
+}
+
+extern "C" tq_status tq_kv_attend_shared_workspace(const tq_kv_cache* cache, int64_t n, int64_t total, int heads,
+                                                   size_t* bytes) {
+  const char* fn = "tq_kv_attend_shared_workspace";
+  tq::KvView kv;
+  if (!bytes) return fail(TQ_EINVAL, "%s: NULL bytes", fn);
+  TRY(view(fn, cache, kv));
+  TRY(check_attend(fn, kv, n, total, heads));
+  *bytes = tq::kv_shared_workspace(kv, n, total, heads);
+  return tq::ok();
+}
+
+extern "C" tq_status tq_kv_attend_shared(const tq_kv_cache* cache, int layer, const int32_t* slots,
+                                         const int32_t* starts, const int32_t* plan, int64_t n, int64_t groups,
+                                         const void* q, int type, int64_t total, int heads, int64_t q_token_stride,
+                                         int64_t q_head_stride, float scale, void* out, float* lse, void* workspace,
+                                         size_t ws_bytes, void* stream) {
+  const char* fn = "tq_kv_attend_shared";
+  const AttendCall c = {cache, layer, slots, starts, n,   {q, q_token_stride, q_head_stride}, type, total, heads,
+                        scale, out,   lse,   workspace};
+  tq::KvView kv;
+  bool none;
+  TRY(check_call(fn, c, kv));
+  TRY(check_arrays(fn, c, none));
+  if (none) return tq::ok();
+  if (groups < 1 || groups > n)
+    return fail(TQ_EINVAL, "%s: groups=%lld outside [1, n=%lld]", fn, (long long)groups, (long long)n);
+  if (!plan || !aligned(plan, 4)) return fail(TQ_EINVAL, "%s: plan must be 4-byte aligned and not NULL", fn);
+  TRY(check_workspace(fn, workspace, ws_bytes, tq::kv_shared_workspace(kv, n, total, heads)));
+  const cudaError_t e = tq::launch_kv_attend_shared(kv, layer, slots, starts, plan, n, groups, c.q, type, total, heads,
+                                                    scale, out, lse, workspace, static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? tq::ok() : cuda_fail(fn, e);
 }
 
@@ -278,5 +369,43 @@ extern "C" tq_status tq_verify_drafts(const void* target, const void* draft, int
   TRY(check_workspace(fn, workspace, ws_bytes, tq::verify_workspace(n, vocab)));
   const cudaError_t e = tq::launch_verify(target, draft, type, drafts, draft_lens, uniforms, noise, n, t, vocab,
                                           tokens, accepted, workspace, static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? tq::ok() : cuda_fail(fn, e);
+}
+
+static tq_status check_sample(const char* fn, int64_t n, int64_t vocab) {
+  if (n < 0 || n > 65535) return fail(TQ_EINVAL, "%s: n=%lld outside [0, 65535]", fn, (long long)n);
+  if (vocab < 1 || vocab > (1 << 24))
+    return fail(TQ_EINVAL, "%s: vocab=%lld outside [1, 2^24]", fn, (long long)vocab);
+  return TQ_OK;
+}
+
+extern "C" tq_status tq_sample_workspace(int64_t n, int64_t vocab, size_t* bytes) {
+  const char* fn = "tq_sample_workspace";
+  if (!bytes) return fail(TQ_EINVAL, "%s: NULL bytes", fn);
+  TRY(check_sample(fn, n, vocab));
+  *bytes = tq::sample_workspace(n, vocab);
+  return tq::ok();
+}
+
+extern "C" tq_status tq_sample(const void* logits, int type, int64_t logits_stride, const float* noise,
+                               int64_t noise_stride, int64_t n, int vocab, const float* temperature,
+                               const int32_t* top_k, const float* top_p, const float* min_p, int32_t* tokens,
+                               float* logprobs, void* workspace, size_t ws_bytes, void* stream) {
+  const char* fn = "tq_sample";
+  TRY(check_sample(fn, n, vocab));
+  if (type != TQ_BF16 && type != TQ_FP16 && type != TQ_FP32) return fail(TQ_EINVAL, "%s: unknown type %d", fn, type);
+  if (logits_stride < 0 || noise_stride < 0 || logits_stride > INT32_MAX || noise_stride > INT32_MAX)
+    return fail(TQ_EINVAL, "%s: strides outside [0, 2^31-1]", fn);
+  if (n == 0) return tq::ok();
+  if (!logits || !noise || !tokens) return fail(TQ_EINVAL, "%s: NULL device pointer", fn);
+  if (!aligned(logits, type == TQ_FP32 ? 4 : 2))
+    return fail(TQ_EINVAL, "%s: the logits must be aligned to their elements", fn);
+  for (const void* p : {(const void*)noise, (const void*)temperature, (const void*)top_k, (const void*)top_p,
+                        (const void*)min_p, (const void*)tokens, (const void*)logprobs})
+    if (!aligned(p, 4)) return fail(TQ_EINVAL, "%s: arrays must be 4-byte aligned", fn);
+  TRY(check_workspace(fn, workspace, ws_bytes, tq::sample_workspace(n, vocab)));
+  const cudaError_t e = tq::launch_sample(logits, type, logits_stride, noise, noise_stride, n, vocab, temperature,
+                                          top_k, top_p, min_p, tokens, logprobs, workspace,
+                                          static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? tq::ok() : cuda_fail(fn, e);
 }

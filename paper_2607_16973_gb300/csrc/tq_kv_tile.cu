@@ -41,6 +41,7 @@
 // TFLOP/s, 0.33 of the measured rate.  Up to 128 rows the converters bound it: 255 MB of codes in
 // 154 us.
 #include <algorithm>
+#include <cstddef>
 
 #include "tq_kv_attend.cuh"
 #include "tq_tc.cuh"
@@ -63,7 +64,7 @@ template <int D>
 struct TileSmem {
   static constexpr int Q = 128 * D * 2;     // one row tile
   static constexpr int K = TOKENS * D * 2;  // one stage
-  static constexpr int q = 0, k = q + 2 * Q, v = k + 2 * K, rest = v + 2 * K, total = rest + 16384 + 1024;
+  static constexpr int q = 0, k = q + 2 * Q, v = k + 2 * K, rest = v + 2 * K, total = rest + 18432 + 1024;
 };
 
 struct TileShared {  // behind the operands
@@ -71,14 +72,15 @@ struct TileShared {  // behind the operands
   Run run;
   // of a tile's blocks: K's scale, log2 of V's, 1 / V's; a block without tokens, or
   // one that cannot be read, has 0, -inf, 0
-  float scales[SCALE_RING][3][8];
+  alignas(16) float scales[SCALE_RING][3][8];  // (read four at a time)
   float row_m[2][128], row_l[2][128];  // what the softmax ends with
   float unscale[256];  // factor of a row's scores, in log2 units
   uint64_t q_full[2], k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_full[2], fin;
   uint32_t tmem;
   int abort_flag, err;
 };
-static_assert(sizeof(TileShared) <= 16384, "shared memory behind the operands");
+static_assert(offsetof(TileShared, scales) % 16 == 0, "scales are read four at a time");
+static_assert(sizeof(TileShared) <= 18432, "shared memory behind the operands");
 
 __host__ __device__ constexpr uint32_t tile_idesc(int n) {
   return (1u << 4) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
@@ -289,7 +291,7 @@ __global__ __launch_bounds__(TILE_THREADS, 1) void k_kv_tile(AttendArgs a) {
       float m = -INFINITY, l = 0.0f;
       bool ok = all_wait(sh.q_full + rt, segments & 1, abort_flag, err, 6);
       const float unscale = sh.unscale[rt * 128 + row];
-      const int place = real ? max(-1, sq.len - sq.count + r / a.group) : -1;
+      const int place = real ? max(-1, dense(a) ? sq.len - 1 : sq.len - sq.count + r / a.group) : -1;
       // what the first warp issues for the four
       const bool issuer = (warp & 3) == 0;
       const uint32_t tm = __shfl_sync(FULL, tmem, 0), sm0 = __shfl_sync(FULL, smem_u32(sm), 0);
@@ -335,7 +337,7 @@ __global__ __launch_bounds__(TILE_THREADS, 1) void k_kv_tile(AttendArgs a) {
           const int t0 = (first + j) * TOKENS;
           // columns [lo, hi) are seen; they are looked at only where some row does not see them
           // all.  (lo may wrap around only for hi <= 0, where nothing is seen whatever it is.)
-          const int hi = place - t0 + 1, lo = a.window ? (int)((unsigned)hi - (unsigned)a.window) : 0;
+          const int hi = place - t0 + 1, lo = max(sq.from - t0, a.window ? (int)((unsigned)hi - (unsigned)a.window) : 0);
           const bool edge = __any_sync(FULL, real && (hi < TOKENS || lo > 0));
           // Half of S at a time (64 columns, 4 blocks): the second half's maximum, the
           // first half's, its weights, and the second half read again for its.  P goes
@@ -648,8 +650,11 @@ __global__ __launch_bounds__(TILE_THREADS, 1) void k_kv_tile(AttendArgs a) {
       l = l * keep0 + sh.row_l[1][row] * keep1;
     }
     if (some && (two || w == 0)) {
-      const float inv = l > 0.0f ? 1.0f / l : 0.0f;
       const int64_t at = real ? out_row(a, sq.token, head, r) : 0;
+      const bool sums = a.sees == KvSees::SHARED;
+      const int from = real && seg.whole ? sq.from : 0;
+      const Both both = join_shared(a, D, at, from, m, l);
+      const float inv = l > 0.0f ? 1.0f / l : 0.0f;
       float* part = part_of<D, P::ROWS>(a, seg);
       const int prow = rt * 128 + row;
 #pragma unroll 1
@@ -662,7 +667,16 @@ __global__ __launch_bounds__(TILE_THREADS, 1) void k_kv_tile(AttendArgs a) {
             x[i] = __float_as_uint(__uint_as_float(x[i]) * keep0 + other[(c + i) * 128 + row] * keep1);
         }
         if (!real) continue;
-        if (seg.whole) {
+        if (seg.whole && !sums) {
+          if (from > 0) {
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+              const float4 z = *reinterpret_cast<const float4*>(a.sums + at * D + c + i);
+              const float y[4] = {z.x, z.y, z.z, z.w};
+#pragma unroll
+              for (int e = 0; e < 4; ++e) x[i + e] = __float_as_uint(__uint_as_float(x[i + e]) * both.own + y[e] * both.shared);
+            }
+          }
           union {
             T e[16];
             uint4 v[2];
@@ -673,12 +687,17 @@ __global__ __launch_bounds__(TILE_THREADS, 1) void k_kv_tile(AttendArgs a) {
           o[0] = y.v[0];
           o[1] = y.v[1];
         } else {
-          uint4* o = reinterpret_cast<uint4*>(part + prow * D + c);
+          uint4* o = reinterpret_cast<uint4*>(seg.whole ? a.sums + at * D + c : part + prow * D + c);
 #pragma unroll
           for (int i = 0; i < 4; ++i) o[i] = make_uint4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
         }
       }
-      if (real && seg.whole && a.lse) a.lse[at] = lse_of(m, l);
+      if (real && seg.whole && sums) {
+        *sums_m(a, D, at) = m;
+        *sums_l(a, D, at) = l;
+      } else if (real && seg.whole && a.lse) {
+        a.lse[at] = lse_of(m, l);
+      }
       if (real && !seg.whole) {
         part[P::ROWS * D + prow] = m;
         part[P::ROWS * (D + 1) + prow] = l;

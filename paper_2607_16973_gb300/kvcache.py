@@ -221,6 +221,14 @@ class KVCache:
         default; window 0, or the tokens that a query sees.  Returns out
         [tokens, heads, head_dim], or (out, lse float32 [tokens, heads]) with
         `return_lse`."""
+        head, tail, result = self._attend(slots, starts, q, out, lse, return_lse, workspace, stream,
+                                          "tq_kv_attend_workspace")
+        check(self._lib.tq_kv_attend(self._handle, layer, *head, self._dim ** -0.5 if scale is None else scale,
+                                     min(window, INT_MAX), *tail))
+        return result
+
+    def _attend(self, slots, starts, q, out, lse, return_lse, workspace, stream, need: str):
+        """What the attention calls have in common: arguments up to the queries' strides, those from `out` on, results."""
         ps, pt, n = self._entries(slots, starts, "slots", "starts", stream, 1)
         if q.dim() != 3:
             raise ValueError(f"q must be [tokens, heads, {self._dim}]")
@@ -242,11 +250,55 @@ class KVCache:
         elif return_lse:
             lse = _empty((total, heads), self._f32, q.device, stream)
             lp = lse.data_ptr()
-        workspace, wp, wb = self._workspace(workspace, stream, "tq_kv_attend_workspace", n, total, heads)
-        check(self._lib.tq_kv_attend(self._handle, layer, ps, pt, n, qp, qt, total, heads, q0, q1,
-                                     dim ** -0.5 if scale is None else scale, min(window, INT_MAX), op, lp, wp, wb,
-                                     _stream(stream)))
-        return (out, lse) if return_lse else out
+        workspace, wp, wb = self._workspace(workspace, stream, need, n, total, heads)
+        return ((ps, pt, n, qp, qt, total, heads, q0, q1), (op, lp, wp, wb, _stream(stream)),
+                (out, lse) if return_lse else out)
+
+    def cross_attention(self, layer: int, slots, starts, q, scale: float | None = None, out=None, lse=None,
+                        return_lse: bool = False, workspace=None, stream=None):
+        """tq_kv_cross: attention of queries over all tokens that the slots hold,
+        whatever the queries' number and place (a reader over encoded passages);
+        arguments, workspace (`attention_workspace`) and results as for
+        `attention`."""
+        head, tail, result = self._attend(slots, starts, q, out, lse, return_lse, workspace, stream,
+                                          "tq_kv_attend_workspace")
+        check(self._lib.tq_kv_cross(self._handle, layer, *head, self._dim ** -0.5 if scale is None else scale, *tail))
+        return result
+
+    def share(self, slots, starts, plan=None, stream=None):
+        """tq_kv_share: which neighbouring requests hold the same first pages:
+        plan int32 [3, n], for each request its group's first request, how many
+        there are, and the tokens that they share before their new ones."""
+        ps, pt, n = self._entries(slots, starts, "slots", "starts", stream, 1)
+        self._used(stream, plan)
+        if plan is None:
+            plan = _empty((3, n), self._i32, self._device, stream)
+        elif plan.shape != (3, n):
+            raise ValueError(f"plan must be {(3, n)}")
+        check(self._lib.tq_kv_share(self._handle, ps, pt, n, _ptr(plan, "plan", self._i32), _stream(stream)))
+        return plan
+
+    def shared_attention_workspace(self, n: int, total: int, heads: int) -> int:
+        """tq_kv_attend_shared_workspace: device bytes for up to `total` queries of up to n requests and `heads` heads."""
+        return self._need("tq_kv_attend_shared_workspace", n, total, heads)
+
+    def shared_attention(self, layer: int, slots, starts, plan, q, groups: int | None = None,
+                         scale: float | None = None, out=None, lse=None, return_lse: bool = False, workspace=None,
+                         stream=None):
+        """tq_kv_attend_shared: `attention` (without a window) where the tokens that
+        the requests of a group share are read once for all its queries; `plan`
+        from `share`.  groups: groups and single requests of the plan (None: taken
+        as n), which the choice of a kernel goes by."""
+        if plan.shape != (3, slots.numel()):
+            raise ValueError(f"plan must be {(3, slots.numel())}")
+        self._used(stream, plan)
+        plan = _ptr(plan, "plan", self._i32)
+        head, tail, result = self._attend(slots, starts, q, out, lse, return_lse, workspace, stream,
+                                          "tq_kv_attend_shared_workspace")
+        ps, pt, n, *queries = head
+        check(self._lib.tq_kv_attend_shared(self._handle, layer, ps, pt, plan, n, n if groups is None else groups,
+                                            *queries, self._dim ** -0.5 if scale is None else scale, *tail))
+        return result
 
     def fork(self, dst, src, stream=None) -> None:
         """tq_kv_fork: slots dst hold what slots src hold, in the same pages."""
@@ -328,4 +380,54 @@ def verify_drafts(target_probs, drafts, uniforms, noise, draft_probs=None, draft
 def _verify_need(n: int, vocab: int) -> int:
     need = C.c_size_t()
     check(load().tq_verify_drafts_workspace(n, vocab, C.byref(need)))
+    return max(need.value, 16)
+
+
+def sample_tokens(logits, noise, temperature=None, top_k=None, top_p=None, min_p=None, tokens=None, logprobs=None,
+                  return_logprobs=False, workspace=None, stream=None):
+    """tq_sample: the next token of each row of logits, from given random numbers.
+
+    logits [n, vocab] float32, bfloat16 or float16 and noise float32 [n, vocab],
+    exponentially distributed, with any row stride; temperature, top_p, min_p float32
+    [n] and top_k int32 [n] on the device, or None: off (temperature 1).  Returns
+    tokens int32 [n], or (tokens, logprobs float32 [n]: at temperature 1, over all
+    tokens) with `return_logprobs`."""
+    torch = _torch()
+    types, i32, f32, dev = _types(), torch.int32, torch.float32, logits.device
+    if logits.dim() != 2 or noise.shape != logits.shape:
+        raise ValueError("logits and noise must both be [n, vocab]")
+    n, vocab = logits.shape
+    for t, name, kinds in ((logits, "logits", tuple(types)), (noise, "noise", (f32,))):
+        if t.dtype not in kinds or not t.is_cuda:
+            _dev_ptr(t, name, kinds, contiguous=False)
+        if t.stride(1) != 1 and vocab > 1:
+            raise ValueError(f"{name}: the elements of a row must lie side by side")
+
+    def ptr(x, name, kind):
+        if x is None:
+            return None
+        if x.shape != (n,):
+            raise ValueError(f"{name} must be {(n,)}, got {tuple(x.shape)}")
+        return _ptr(x, name, kind)
+
+    settings = (ptr(temperature, "temperature", f32), ptr(top_k, "top_k", i32), ptr(top_p, "top_p", f32),
+                ptr(min_p, "min_p", f32))
+    _used(stream, logits, noise, temperature, top_k, top_p, min_p, tokens, logprobs, workspace)
+    if tokens is None:
+        tokens = _empty(n, i32, dev, stream)
+    if logprobs is None and return_logprobs:
+        logprobs = _empty(n, f32, dev, stream)
+    if workspace is None:
+        workspace = _empty(_sample_need(n, vocab), torch.uint8, dev, stream)
+    check(load().tq_sample(logits.data_ptr(), types[logits.dtype], logits.stride(0), noise.data_ptr(), noise.stride(0),
+                           n, vocab, *settings, ptr(tokens, "tokens", i32), ptr(logprobs, "logprobs", f32),
+                           _dev_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size(),
+                           _stream(stream)))
+    return (tokens, logprobs) if return_logprobs else tokens
+
+
+@functools.lru_cache(maxsize=4096)
+def _sample_need(n: int, vocab: int) -> int:
+    need = C.c_size_t()
+    check(load().tq_sample_workspace(n, vocab, C.byref(need)))
     return max(need.value, 16)
