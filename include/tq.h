@@ -764,8 +764,8 @@ tq_status tq_verify_drafts(const void* target, const void* draft, int type,
  *   logits   device [n][vocab], `type` TQ_FP32, TQ_BF16 or TQ_FP16, rows logits_stride
  *            elements apart (any alignment of the elements' own size).  -INFINITY masks
  *            a token; NaN counts as -INFINITY, +INFINITY as the largest float
- *   noise    device [n][vocab] float32 > 0 and finite, exponentially distributed, rows
- *            noise_stride elements apart
+ *   noise    device [n][vocab] float32, exponentially distributed, rows noise_stride
+ *            elements apart; what is below 2^-126, or NaN, counts as 2^-126
  *   temperature, top_k, top_p, min_p  device [n] each, nullable (1, 0, 1, 0)
  *   tokens   device out [n] int32
  *   logprobs device out [n] float32 (nullable): x_token - ln sum_v e^(x_v), at
