@@ -48,12 +48,12 @@ __device__ __forceinline__ float ex2f(float x) {
   return y;
 }
 
-// A logit: NaN counts as -inf, +inf as the largest float; -0 as 0.
-__device__ __forceinline__ float logit(float x) { return fminf(fmaxf(x, -INFINITY), 3.402823466e38f) + 0.0f; }
+// A logit: NaN counts as -inf, +inf as the largest float.
+__device__ __forceinline__ float logit(float x) { return fminf(fmaxf(x, -INFINITY), 3.402823466e38f); }
 
 // Floats as unsigned integers in their order.
 __device__ __forceinline__ uint32_t ordered(float x) {
-  const uint32_t u = __float_as_uint(x);
+  const uint32_t u = __float_as_uint(x + 0.0f);  // (-0 is 0)
   return u ^ ((uint32_t)((int)u >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float unordered(uint32_t u) {
@@ -140,7 +140,7 @@ struct Places {
   int n;
   __device__ __forceinline__ int pieces() const { return n; }
   __device__ __forceinline__ int load(int g, float (&x)[1]) const {
-    const uint64_t place = __ldcg(p + g);
+    const uint64_t place = p[g];
     x[0] = value_of(place);
     return token_of(place);
   }
@@ -442,11 +442,14 @@ struct Race {
   }
   __device__ __forceinline__ void enter(float x, int v) { enter(x, v, weigh(x)); }
   __device__ __forceinline__ void enter(float x, int v, float w) { enter(x, v, w, noise[v]); }
+  // Whether min-p lets a token of about weight w race: in 64 bits next to its border.
+  __device__ __forceinline__ bool keeps(float x, float w) const {
+    if (w > s.min_p * (1.0f + 0x1p-18f)) return true;
+    return w > 0.0f && w >= s.min_p * (1.0f - 0x1p-18f) && weight(x) >= (double)s.min_p;
+  }
   __device__ __forceinline__ void enter(float x, int v, float w, float e) {
     const uint64_t place = place_of(x, v);
-    if (w < s.min_p * (1.0f + 0x1p-18f) || w == 0.0f) {  // (next to the border: in 64 bits)
-      if (place != first && (w < s.min_p * (1.0f - 0x1p-18f) || w == 0.0f || weight(x) < (double)s.min_p)) return;
-    }
+    if (place != first && !keeps(x, w)) return;
     const float q = w / number(e);
     if (winner) {
       if (!(q >= best * NEAR)) return;
@@ -511,6 +514,13 @@ __device__ int cut_list(const Setting& s, const Weigh& weigh, int n, Shared& sh)
 __device__ __forceinline__ float least_value(const Setting& s, float top, uint64_t sum, int vocab) {
   const float least = (1.0f - s.top_p) * ((float)sum / FIXED) / (float)vocab;
   return fmaxf(top + logf(least) * s.temperature * 1.0001f - 1e-3f, -3.0e38f);
+}
+
+// What tokens below are ruled out by min-p (> 0).
+__device__ __forceinline__ float least_kept(const Setting& s, float top) {
+  float x = top + (logf(s.min_p) - 1e-3f) * s.temperature;
+  x -= fabsf(x) * 0x1p-21f;
+  return x < top ? x : -INFINITY;
 }
 
 // A row by one block of N threads, whatever its settings.
@@ -657,35 +667,34 @@ __global__ __launch_bounds__(N) void k_sample_row(SampleArgs a) {
 
 // ---- a row by several blocks ------------------------------------------------
 //
-// k_sample_parts: a block per PART tokens, read once: its largest, its sums, and what
-// tells where the row's cut lies: the largest of every 64 tokens (small k), or the
-// weights of 1,024 steps of 1/32 of x / T (top-p; steps at fixed places, so that parts
-// which do not know of one another's largest add up).  The row's last block says which
-// step or bound that is.
-// k_sample_race: the same blocks again: what lies above the step races at once and is
-// summed, what lies in it (or above the bound) goes to the row's list, which its last
-// block cuts and races, and joins with the parts' winners.  A list that is too long, and
-// what fits neither form (large k), is left to whole_row there.
-constexpr int SPLIT = 256, EACH = 16, PART = SPLIT * EACH;
-constexpr int GROUP = 64, GROUPS = PART / GROUP;
+// k_sample_parts: a block per part of 256 x JP pieces of 16 bytes, read once and held as
+// they are: its largest, its sums, and what tells where the row's cut lies: the largest of
+// every 64 tokens (small k), or the weights of 1,024 steps of 1/32 of x / T (top-p; steps at
+// fixed places, so that parts which do not know of one another's largest add up).
+// k_sample_cut: a block per row joins the parts and finds that step, or a bound of k values.
+// k_sample_race: the parts again, from L2: what lies above the step races at once and is
+// summed, what lies in it (or above the bound) goes to the row's list.
+// k_sample_finish: a block per row cuts the list, races it, and joins the parts' winners.
+// A list that is too long, and what fits neither form (large k, infinities), is left to
+// whole_row there.
+constexpr int SPLIT = 256;
+constexpr int GROUP = 64;              // tokens
 constexpr int STEPS = 1024;            // of 1/32: weights down to e^-32 of a part's largest
-constexpr float STEP_ONE = 524288.0f;  // weight at a step's upper end, as an integer: PART of them fit
-constexpr int MOST_K = 512, MOST_LISTED = 4096, MOST_PARTS = 128;
+constexpr float STEP_ONE = 524288.0f;  // weight at a step's upper end, as an integer: 2^13 of them fit
+constexpr float ROUND = 12582912.0f;   // 1.5 * 2^23: what is added to it is rounded to an integer, in its low bits
+constexpr float MOST_STEP = 1e6f;      // steps' numbers up to which that holds, and leaves bits behind the point
+constexpr int MOST_K = 512, MOST_LISTED = 4096, MOST_PARTS = SPLIT;
 constexpr int MOST_ROWS = 512, MOST_BLOCKS = 16384;  // of a launch: what the workspace is for
+constexpr int FEW_BLOCKS = 304;        // with less of 8 pieces a thread, 2 a thread
 
 enum class Mode : int { DONE, ALONE, BOUND, CUT };
 
 struct RowRecord {
-  // zero at the start
-  unsigned arrived, raced, listed;
-  unsigned unused;
-  uint64_t above;       // weight above the step
-  // from the first kernel's last block
   uint64_t first, sum1, sum;
   Mode mode;
-  float bound;          // BOUND
+  float bound;          // BOUND: the list's least value.  CUT: nothing below it is kept or listed
   int step;             // CUT: the list's step; what lies above it is kept, what lies below is not
-  int unused2;
+  unsigned listed;      // (0 until the race)
 };
 struct PartRecord {
   uint64_t first;
@@ -693,7 +702,7 @@ struct PartRecord {
 };
 struct PartWinner {
   uint64_t place;
-  float best;
+  float best, above;    // its quotient; the part's weight above the step
 };
 
 struct SplitArgs {
@@ -703,67 +712,143 @@ struct SplitArgs {
   RowRecord* rows;
   PartRecord* part;
   PartWinner* winner;
-  float* groups;     // [blocks][GROUPS]
+  float* groups;     // [blocks][SPLIT]
   uint32_t* steps;   // [blocks][STEPS]
   uint64_t* list;    // [rows][MOST_LISTED]
 };
 
-// Step of x: floor(32 x / T), which grows with x.
-__device__ __forceinline__ float steps_per(float temperature) { return fminf(32.0f / temperature, 1e30f); }
-__device__ __forceinline__ int step_of(float x, float per) { return (int)floorf(fminf(fmaxf(x * per, -1e9f), 1e9f)); }
-// Steps of b below a (no less than -1: they may be 2^31 apart).
-__device__ __forceinline__ int steps_below(int a, int b) { return (int)max(-1ll, min((long long)STEPS, (long long)a - b)); }
-
-template <typename T>
-__device__ __forceinline__ void load_part(const Row<T>& row, int part, float (&x)[EACH], int (&v)[EACH / Row<T>::E]) {
-  constexpr int E = Row<T>::E;
-#pragma unroll
-  for (int j = 0; j < EACH / E; ++j) {
-    float y[E];
-    const int g = part * (PART / E) + j * SPLIT + threadIdx.x;
-    v[j] = g * E - row.lead;
-    if (g < row.pieces()) {
-      row.load(g, y);
-    } else {
-#pragma unroll
-      for (int i = 0; i < E; ++i) y[i] = -INFINITY;
-    }
-#pragma unroll
-    for (int i = 0; i < E; ++i) x[j * E + i] = y[i];
+// 16 bytes of a row as they lie in memory.
+template <typename T> struct Packed;
+template <> struct Packed<float> {
+  static constexpr uint32_t MASKED = 0xff800000u;
+  static __device__ __forceinline__ uint32_t largest(uint32_t a, uint32_t b) {
+    return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
   }
+  static __device__ __forceinline__ float top(uint32_t a) { return __uint_as_float(a); }
+  static __device__ __forceinline__ float at(const uint4& u, int i) {
+    return __uint_as_float(i == 0 ? u.x : i == 1 ? u.y : i == 2 ? u.z : u.w);
+  }
+};
+template <typename T2, typename T, uint32_t MASK> struct Packed16 {
+  static constexpr uint32_t MASKED = MASK;
+  static __device__ __forceinline__ uint32_t largest(uint32_t a, uint32_t b) {
+    T2 x, y;
+    memcpy(&x, &a, 4);
+    memcpy(&y, &b, 4);
+    x = __hmax2(x, y);
+    memcpy(&a, &x, 4);
+    return a;
+  }
+  static __device__ __forceinline__ float at(uint32_t w, int i) {
+    const uint16_t h = (uint16_t)(i ? w >> 16 : w);
+    T x;
+    memcpy(&x, &h, 2);
+    return to_float(x);
+  }
+  static __device__ __forceinline__ float top(uint32_t a) { return fmaxf(at(a, 0), at(a, 1)); }
+  static __device__ __forceinline__ float at(const uint4& u, int i) {
+    return at(i < 2 ? u.x : i < 4 ? u.y : i < 6 ? u.z : u.w, i & 1);
+  }
+};
+template <> struct Packed<__nv_bfloat16> : Packed16<__nv_bfloat162, __nv_bfloat16, 0xff80ff80u> {
+  // (the upper half of the float)
+  static __device__ __forceinline__ float at(uint32_t w, int i) { return __uint_as_float(i ? w & 0xffff0000u : w << 16); }
+  static __device__ __forceinline__ float top(uint32_t a) { return fmaxf(at(a, 0), at(a, 1)); }
+  static __device__ __forceinline__ float at(const uint4& u, int i) {
+    return at(i < 2 ? u.x : i < 4 ? u.y : i < 6 ? u.z : u.w, i & 1);
+  }
+};
+template <> struct Packed<__half> : Packed16<__half2, __half, 0xfc00fc00u> {};
+
+// Piece g of a row, NaN and what is not the row's as -inf.
+template <typename T>
+__device__ __forceinline__ uint4 load_raw(const Row<T>& row, int g) {
+  using P = Packed<T>;
+  constexpr int E = Row<T>::E;
+  uint4 u = make_uint4(P::MASKED, P::MASKED, P::MASKED, P::MASKED);
+  const int v = g * E - row.lead;
+  if (v >= 0 && v + E <= row.n) {
+    u = *reinterpret_cast<const uint4*>(row.p + v);
+  } else if (v < row.n) {
+    union {
+      uint4 u;
+      T e[E];
+    } x;
+    x.u = u;
+#pragma unroll
+    for (int i = 0; i < E; ++i)
+      if (v + i >= 0 && v + i < row.n) x.e[i] = row.p[v + i];
+    u = x.u;
+  }
+  return u;
+}
+template <typename T>
+__device__ __forceinline__ void mask_nan(uint4& u) {
+  using P = Packed<T>;
+  u.x = P::largest(u.x, P::MASKED), u.y = P::largest(u.y, P::MASKED);
+  u.z = P::largest(u.z, P::MASKED), u.w = P::largest(u.w, P::MASKED);
+}
+// What follows converts the pieces again rather than keep 64 floats from before.
+template <int JP>
+__device__ __forceinline__ void hold(uint4 (&u)[JP]) {
+#pragma unroll
+  for (int j = 0; j < JP; ++j) asm volatile("" : "+r"(u[j].x), "+r"(u[j].y), "+r"(u[j].z), "+r"(u[j].w));
+}
+template <typename T>
+__device__ __forceinline__ uint32_t piece_top(const uint4& u) {
+  using P = Packed<T>;
+  return P::largest(P::largest(u.x, u.y), P::largest(u.z, u.w));
 }
 
-__device__ __forceinline__ float block_sum(float x, Scratch& s) {
+// Number of the step that x is in, which grows with x: 32 x / T, rounded.  (Up to MOST_STEP.)
+__device__ __forceinline__ float steps_per(float temperature) { return fminf(32.0f / temperature, 1e30f); }
+__device__ __forceinline__ int step_of(float x, float per) {
+  return __float_as_int(__fadd_rn(__fmul_rn(x, per), ROUND)) - __float_as_int(ROUND);
+}
+
+__device__ __forceinline__ float warp_sum(float x) {
 #pragma unroll
   for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(FULL, x, o);
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) s.words[threadIdx.x >> 5] = __float_as_uint(x);
-  __syncthreads();
-  x = __uint_as_float((uint32_t)s.words[threadIdx.x & (SPLIT / 32 - 1)]);
-#pragma unroll
-  for (int o = SPLIT / 64; o; o >>= 1) x += __shfl_xor_sync(FULL, x, o);
   return x;
 }
-
-// True in every thread of the block that arrives last of `parts`; what the others wrote
-// in front of it is then visible.
-__device__ __forceinline__ bool last_of(unsigned* counter, int parts, Shared& sh) {
+// The block's largest x >= 0; y becomes its sum.
+__device__ __forceinline__ float block_most(float x, float& y, Scratch& s) {
+  x = __uint_as_float(__reduce_max_sync(FULL, __float_as_uint(x)));
+  y = warp_sum(y);
+  if ((threadIdx.x & 31) == 0) s.words[threadIdx.x >> 5] = (uint64_t)__float_as_uint(x) << 32 | __float_as_uint(y);
   __syncthreads();
-  if (threadIdx.x == 0) {
-    __threadfence();
-    sh.bin = (int)atomicAdd(counter, 1u) == parts - 1;
-    __threadfence();
+  x = y = 0.0f;
+#pragma unroll
+  for (int w = 0; w < SPLIT / 32; ++w) {
+    x = fmaxf(x, __uint_as_float((uint32_t)(s.words[w] >> 32)));
+    y += __uint_as_float((uint32_t)s.words[w]);
   }
+  return x;
+}
+__device__ __forceinline__ void block_sums(float& x, float& y, Scratch& s) {
+  x = warp_sum(x);
+  y = warp_sum(y);
   __syncthreads();
-  return sh.bin;
+  if ((threadIdx.x & 31) == 0) s.words[threadIdx.x >> 5] = (uint64_t)__float_as_uint(x) << 32 | __float_as_uint(y);
+  __syncthreads();
+  x = y = 0.0f;
+#pragma unroll
+  for (int w = 0; w < SPLIT / 32; ++w) {
+    x += __uint_as_float((uint32_t)(s.words[w] >> 32));
+    y += __uint_as_float((uint32_t)s.words[w]);
+  }
 }
 
-// The row's record, by the last block of k_sample_parts.
-template <typename T>
-__device__ void settle_row(const SplitArgs& q, int64_t r, RowRecord& rec, Shared& sh) {
+// The row's record; groups: of a part.  A block per row.
+__global__ __launch_bounds__(SPLIT) void k_sample_cut(SplitArgs q, int groups_of_part) {
+  __shared__ Shared sh;
   const SampleArgs& a = q.a;
+  const int64_t r = q.row0 + blockIdx.x, block0 = blockIdx.x * (int64_t)q.parts;
+  RowRecord& rec = q.rows[blockIdx.x];
+  griddep_launch_dependents();
   const Setting s = setting_of(a, r);
-  const PartRecord* part = q.part + blockIdx.y * (int64_t)q.parts;
+  griddep_wait();
+  const PartRecord* part = q.part + block0;
   const int t = threadIdx.x;
   PartRecord mine = {0, 0.0f, 0.0f};  // (parts <= threads)
   if (t < q.parts) {
@@ -772,41 +857,44 @@ __device__ void settle_row(const SplitArgs& q, int64_t r, RowRecord& rec, Shared
     mine.sum = __ldcg(&part[t].sum);
   }
   const uint64_t first = block_max<SPLIT>(mine.first, sh.scratch);
-  if (first == 0) {
+  const float top = first ? value_of(first) : 0.0f, m = mine.first ? value_of(mine.first) : 0.0f;
+  if (first == 0 || top == INFINITY) {
     if (t == 0) {
-      finish(a, r, 0, 0.0f, 0);
-      rec.mode = Mode::DONE;
+      if (first == 0) finish(a, r, 0, 0.0f, 0);
+      rec.mode = first ? Mode::ALONE : Mode::DONE;
+      rec.first = first;
     }
     return;
   }
-  const float top = value_of(first), m = value_of(mine.first);
   const Weigh plain = weigh_of(top, 1.0f), weigh = weigh_of(top, s.hot ? s.temperature : 1.0f);
   const uint64_t sum1 = block_sum<SPLIT>(mine.first ? fixed(mine.sum1 * plain(m)) : 0, sh.scratch);
   const uint64_t sum = block_sum<SPLIT>(mine.first ? fixed(mine.sum * weigh(m)) : 0, sh.scratch);
+  const float per = steps_per(s.temperature);
   Mode mode = Mode::DONE;
   float bound = -INFINITY;
-  int step = -2000000000;
+  int step = INT_MIN;
   if (!s.hot) {
     if (t == 0) finish(a, r, first, top, sum1);
   } else if (s.k < a.vocab) {
     mode = Mode::ALONE;
     if (s.k <= MOST_K) {
-      // the least value that k groups reach, by a histogram of their largest
-      const float* groups = q.groups + blockIdx.y * (int64_t)q.parts * GROUPS;
-      const int n = q.parts * GROUPS;
+      // a value that k groups' largest reach, by a histogram of them
+      const float* groups = q.groups + block0 * SPLIT;
+      const int n = q.parts * groups_of_part;
+      auto group = [&](int i) { return __ldcg(groups + (int64_t)(i / groups_of_part) * SPLIT + i % groups_of_part); };
       uint32_t lo = 0xffffffffu;
       for (int i = t; i < n; i += SPLIT) {
-        const float x = __ldcg(groups + i);
+        const float x = group(i);
         if (x > -INFINITY) lo = min(lo, ordered(x));
       }
       const float low = unordered(~(uint32_t)block_max<SPLIT>((uint64_t)~lo, sh.scratch));
-      const float per = top > low ? (BINS - 1) / (top - low) : 0.0f;
+      const float bins_per = top > low ? (BINS - 1) / (top - low) : 0.0f;
       for (int i = t; i < BINS; i += SPLIT) sh.bins[i] = 0;
       if (t == 0) sh.listed = -1;
       __syncthreads();
-      auto bin_of = [&](float x) { return (int)fminf((top - x) * per, (float)(BINS - 1)); };
+      auto bin_of = [&](float x) { return (int)fminf((top - x) * bins_per, (float)(BINS - 1)); };
       for (int i = t; i < n; i += SPLIT) {
-        const float x = __ldcg(groups + i);
+        const float x = group(i);
         if (x > -INFINITY) atomicAdd(&sh.bins[bin_of(x)], 1u);
       }
       __syncthreads();
@@ -825,53 +913,57 @@ __device__ void settle_row(const SplitArgs& q, int64_t r, RowRecord& rec, Shared
       if (bin >= 0) {  // (else fewer groups than k)
         uint32_t least = 0xffffffffu;
         for (int i = t; i < n; i += SPLIT) {
-          const float x = __ldcg(groups + i);
+          const float x = group(i);
           if (x > -INFINITY && bin_of(x) <= bin) least = min(least, ordered(x));
         }
         bound = unordered(~(uint32_t)block_max<SPLIT>((uint64_t)~least, sh.scratch));
         mode = Mode::BOUND;
       }
     }
-  } else if (s.top_p < 1.0f && !(fabsf(top) * steps_per(s.temperature) < 1e6f)) {
-    mode = Mode::ALONE;  // (float32 holds too few bits behind a step's number)
+  } else if (!(s.top_p < 1.0f)) {
+    mode = Mode::CUT;  // (of nothing: all race that min-p lets)
+    if (s.min_p > 0.0f) bound = least_kept(s, top);
+  } else if (!(fabsf(top) * per < MOST_STEP)) {
+    mode = Mode::ALONE;  // (a step's number is too large)
   } else {
     mode = Mode::CUT;
-    if (s.top_p < 1.0f) {
-      // the steps' weights from the row's largest down, 4 of them a thread, relative to that
-      const float per = steps_per(s.temperature);
-      const int highest = step_of(top, per), at = t * (STEPS / SPLIT);
-      uint64_t w[STEPS / SPLIT] = {0, 0, 0, 0};
-      static_assert(STEPS / SPLIT == 4, "steps of a thread");
-      if (t < q.parts) sh.bins[t] = mine.first ? steps_below(highest, step_of(m, per)) : STEPS;
-      __syncthreads();
-      const uint32_t* steps = q.steps + blockIdx.y * (int64_t)q.parts * STEPS;
+    // the steps' weights from the row's largest down, 4 of them a thread, relative to that
+    const int highest = step_of(top, per), at = t * (STEPS / SPLIT);
+    uint64_t w[4] = {0, 0, 0, 0};
+    static_assert(STEPS / SPLIT == 4, "steps of a thread");
+    int shift = STEPS;  // of this part's steps; STEPS: it has none that count
+    if (mine.first && (top - m) * per < (float)STEPS) shift = highest - step_of(m, per);
+    sh.bins[t] = shift;
+    __syncthreads();
+    const uint32_t* steps = q.steps + block0 * STEPS;
 #pragma unroll 4
-      for (int p = 0; p < q.parts; ++p) {
-        const int from = at - (int)sh.bins[p];
+    for (int p = 0; p < q.parts; ++p) {
+      const int from = at - (int)sh.bins[p];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (from + i >= 0) w[i] += __ldcg(steps + (int64_t)p * STEPS + from + i);
-      }
-      uint64_t some = 0, all;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        // weight at the step's upper end; at most 1 in the largest's own step, up to rounding
-        const float up = ((float)(highest - at - i + 1) - top * per) * (1.0f / 32.0f);
-        w[i] = (uint64_t)((float)w[i] * (FIXED / STEP_ONE) * ex2f(fminf(up * LOG2E, 1.0f)));
-        some += w[i];
-      }
-      const uint64_t want = part_of(s.top_p, sum);
-      if (t == 0) sh.listed = -1;
-      uint64_t upto = block_scan<SPLIT>(some, sh.scratch, all);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (w[i] && upto < want && upto + w[i] >= want) sh.listed = at + i;
-        upto += w[i];
-      }
-      __syncthreads();
-      // (none: all but what is e^-32 of the largest, or the parts' sums rounded apart)
-      step = highest - (sh.listed < 0 ? STEPS : sh.listed);
+      for (int i = 0; i < 4; ++i)
+        if (from + i >= 0) w[i] += __ldcg(steps + (int64_t)p * STEPS + from + i);
     }
+    uint64_t some = 0, all;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      // the weight at the step's upper end: about 1 in the largest's own step
+      const float up = ((float)(highest - at - i) + 0.5f - top * per) * (1.0f / 32.0f);
+      w[i] = (uint64_t)((float)w[i] * (FIXED / STEP_ONE) * ex2f(up * LOG2E));
+      some += w[i];
+    }
+    const uint64_t want = part_of(s.top_p, sum);
+    if (t == 0) sh.listed = -1;
+    uint64_t upto = block_scan<SPLIT>(some, sh.scratch, all);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (w[i] && upto < want && upto + w[i] >= want) sh.listed = at + i;
+      upto += w[i];
+    }
+    __syncthreads();
+    // (none: all but what is e^-32 of the largest, or the parts' sums rounded apart)
+    step = highest - (sh.listed < 0 ? STEPS - 1 : sh.listed);
+    bound = ((float)step - 0.51f) / per;
+    bound -= fabsf(bound) * 0x1p-21f;
   }
   if (t == 0) {
     rec.first = first;
@@ -880,185 +972,561 @@ __device__ void settle_row(const SplitArgs& q, int64_t r, RowRecord& rec, Shared
     rec.mode = mode;
     rec.bound = bound;
     rec.step = step;
+    rec.listed = 0;
   }
 }
 
-template <typename T>
+template <typename T, int JP>
 __global__ __launch_bounds__(SPLIT, 4) void k_sample_parts(SplitArgs q) {
-  constexpr int E = Row<T>::E;
-  __shared__ Shared sh;
+  using P = Packed<T>;
+  constexpr int E = Row<T>::E, LANES = GROUP / (JP * E);  // of a group
+  __shared__ struct {
+    uint32_t bins[STEPS];
+    Scratch scratch;
+    uint32_t low;
+  } sh;
   const SampleArgs& a = q.a;
   const int64_t r = q.row0 + blockIdx.y, block = blockIdx.y * (int64_t)q.parts + blockIdx.x;
   const Row<T> row(a.logits, a.logits_stride, r, a.vocab);
-  const int t = threadIdx.x;
+  const int t = threadIdx.x, g0 = blockIdx.x * (SPLIT * JP) + t;
   griddep_launch_dependents();
-  float x[EACH];
-  int v[EACH / E];
-  load_part(row, blockIdx.x, x, v);
+  uint4 raw[JP];
+#pragma unroll
+  for (int j = 0; j < JP; ++j) raw[j] = load_raw(row, g0 + j * SPLIT);
   const Setting s = setting_of(a, r);
   const bool cut = s.hot && s.k == a.vocab && s.top_p < 1.0f, few = s.hot && s.k < a.vocab && s.k <= MOST_K;
-
-  float m = x[0];
+  uint32_t most = P::MASKED;
 #pragma unroll
-  for (int i = 1; i < EACH; ++i) m = fmaxf(m, x[i]);
+  for (int j = 0; j < JP; ++j) {
+    mask_nan<T>(raw[j]);
+    most = P::largest(most, piece_top<T>(raw[j]));
+  }
+  const float mine = P::top(most);
+  hold(raw);
   if (few) {
-    float y = fmaxf(m, __shfl_xor_sync(FULL, m, 1));
-    y = fmaxf(y, __shfl_xor_sync(FULL, y, 2));
-    if ((t & 3) == 0) q.groups[block * GROUPS + t / 4] = y;
+    float y = mine;
+#pragma unroll
+    for (int o = 1; o < LANES; o <<= 1) y = fmaxf(y, __shfl_xor_sync(FULL, y, o));
+    if (t % LANES == 0) q.groups[block * SPLIT + t / LANES] = y;
   }
   if (cut)
     for (int i = t; i < STEPS; i += SPLIT) sh.bins[i] = 0;
-  int at = a.vocab;
+  // the block's largest, then its lowest token
+  const uint32_t high = __reduce_max_sync(FULL, ordered(mine));
+  if ((t & 31) == 0) sh.scratch.words[t >> 5] = high;
+  if (t == 0) sh.low = 0xffffffffu;
+  __syncthreads();
+  uint32_t high_u = 0;
 #pragma unroll
-  for (int i = EACH - 1; i >= 0; --i)
-    if (x[i] == m) at = v[i / E] + i % E;
-  const uint64_t first = block_max<SPLIT>(m > -INFINITY ? place_of(m, at) : 0, sh.scratch);
-  m = first ? value_of(first) : 0.0f;
+  for (int w = 0; w < SPLIT / 32; ++w) high_u = max(high_u, (uint32_t)sh.scratch.words[w]);
+  const float m = unordered(high_u);
   float sum1 = 0.0f, sum = 0.0f;
+  if (m > -INFINITY) {  // (uniform)
+    if (mine == m) {
+      int at = INT_MAX;
 #pragma unroll
-  for (int i = 0; i < EACH; ++i) sum1 += ex2f((x[i] - m) * LOG2E);
-  sum1 = block_sum(sum1, sh.scratch);
-  if (cut) {
-    const Weigh weigh = weigh_of(m, s.temperature);
-    const float per = steps_per(s.temperature);
-    const int highest = step_of(m, per);
+      for (int j = 0; j < JP; ++j)
 #pragma unroll
-    for (int i = 0; i < EACH; ++i)
-      if (x[i] > -INFINITY) {
-        sum += weigh(x[i]);
-        const int step = step_of(x[i], per), slot = steps_below(highest, step);
-        // (a product that rounds up to the step's end, or past it where x is huge, is held at 1)
-        const float up = fminf((x[i] * per - (float)(step + 1)) * (LOG2E / 32.0f), 0.0f);
-        if (slot >= 0 && slot < STEPS) atomicAdd(&sh.bins[slot], __float2uint_rn(STEP_ONE * ex2f(up)));
+        for (int i = 0; i < E; ++i)
+          if (P::at(raw[j], i) == m) at = min(at, (g0 + j * SPLIT) * E - row.lead + i);
+      atomicMin(&sh.low, (uint32_t)at);
+    }
+    hold(raw);
+#pragma unroll
+    for (int j = 0; j < JP; ++j) {
+      float y[E];
+#pragma unroll
+      for (int i = 0; i < E; ++i) y[i] = ex2f((P::at(raw[j], i) - m) * LOG2E);
+#pragma unroll
+      for (int o = 1; o < E; o <<= 1)
+#pragma unroll
+        for (int i = 0; i < E; i += 2 * o) y[i] += y[i + o];
+      sum1 += y[0];
+    }
+    if (cut) {
+      const float per = steps_per(s.temperature), c = weigh_of(m, s.temperature).hi;
+      const bool steps = fabsf(m) * per < MOST_STEP;  // (else the row is done by a block alone, or this part is far below it)
+      const int highest = steps ? step_of(m, per) : 0;
+      const float least = m - (STEPS + 8) / per;
+      hold(raw);
+#pragma unroll
+      for (int j = 0; j < JP; ++j) {
+        if (P::top(piece_top<T>(raw[j])) < least) continue;
+        float y = 0.0f;
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+          const float x = P::at(raw[j], i);
+          y += x > -INFINITY ? ex2f((x - m) * c) : 0.0f;
+          if (x >= least && steps) {
+            const int step = step_of(x, per), slot = highest - step;
+            const float up = (__fmul_rn(x, per) - ((float)step + 0.5f)) * (LOG2E / 32.0f);
+            const uint32_t w = __float_as_uint(fmaf(ex2f(up), STEP_ONE, ROUND)) - __float_as_uint(ROUND);
+            if (slot < STEPS) atomicAdd(&sh.bins[slot], w);
+          }
+        }
+        sum += y;
       }
-    sum = block_sum(sum, sh.scratch);  // (a barrier behind the steps too)
+    }
+  }
+  block_sums(sum1, sum, sh.scratch);  // (a barrier behind the steps too)
+  if (cut)
     for (int i = t; i < STEPS / 4; i += SPLIT)
       reinterpret_cast<uint4*>(q.steps + block * STEPS)[i] = reinterpret_cast<const uint4*>(sh.bins)[i];
-  }
-  if (t == 0) q.part[block] = {first, sum1, sum};
-  RowRecord& rec = q.rows[blockIdx.y];
-  __threadfence();
-  if (last_of(&rec.arrived, q.parts, sh)) settle_row<T>(q, r, rec, sh);
+  if (t == 0) q.part[block] = {m > -INFINITY ? place_of(m, (int)sh.low) : 0, sum1, sum};
 }
 
-// The rest of a row, by the last block of k_sample_race.
+// The noise of E tokens from v on, or 1 where there is none; wide: pieces begin at every 16
+// bytes of the noise too, as they do where its rows lie as the logits' do.
+template <int E>
+__device__ __forceinline__ void noise_of(const float* noise, bool wide, int v, int n, float (&e)[E]) {
+  if (wide && v >= 0 && v + E <= n) {
+#pragma unroll
+    for (int i = 0; i < E; i += 4) {
+      const float4 f = __ldg(reinterpret_cast<const float4*>(noise + v + i));
+      e[i] = f.x, e[i + 1] = f.y, e[i + 2] = f.z, e[i + 3] = f.w;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < E; ++i) e[i] = v + i >= 0 && v + i < n ? noise[v + i] : 1.0f;
+  }
+}
+// Races those of the piece from v on that lie above the step and whose quotient is about `high`.
 template <typename T>
-__device__ void settle_race(const SplitArgs& q, int64_t r, const RowRecord& rec, const Setting& s, const Weigh& weigh,
-                            Shared& sh) {
-  const SampleArgs& a = q.a;
-  const int t = threadIdx.x, listed = (int)__ldcg(&rec.listed);
-  const uint64_t* list = q.list + blockIdx.y * (int64_t)MOST_LISTED;
-  Race race = {s, weigh, a.noise + r * a.noise_stride, rec.first};
-  bool alone = listed > MOST_LISTED || (rec.mode == Mode::BOUND && listed > LIST);
-  if (!alone && rec.mode == Mode::BOUND) {
-    for (int i = t; i < listed; i += SPLIT) sh.list[i] = __ldcg(list + i);
-    sort_list<SPLIT>(sh, listed);
-    const int n = cut_list<SPLIT>(s, weigh, listed, sh);
-    for (int i = t; i < n; i += SPLIT) race.enter(value_of(sh.list[i]), token_of(sh.list[i]));
-  } else if (!alone && rec.mode == Mode::CUT) {
-    if (listed) {
-      const uint64_t want = part_of(s.top_p, rec.sum), front = __ldcg(&rec.above);
-      uint64_t lo = ~0ull, hi = 0;
-      for (int i = t; i < listed; i += SPLIT) {
-        const uint64_t x = __ldcg(list + i);
-        lo = min((unsigned long long)lo, (unsigned long long)x);
-        hi = max((unsigned long long)hi, (unsigned long long)x);
-      }
-      lo = ~block_max<SPLIT>(~lo, sh.scratch);
-      hi = block_max<SPLIT>(hi, sh.scratch);
-      const Places places = {list, listed};
-      const uint64_t cut = find_cut<SPLIT, false>(places, weigh, 0, front, want, 0x1p31f / ((float)rec.sum / FIXED),
-                                                  value_of(lo), value_of(hi), sh);
-      alone = cut == 0;
-      if (!alone)
-        for (int i = t; i < listed; i += SPLIT) {
-          const uint64_t x = __ldcg(list + i);
-          if (x >= cut) race.enter(value_of(x), token_of(x));
-        }
-    }
-    if (!alone && t < q.parts) {
-      const PartWinner* w = q.winner + blockIdx.y * (int64_t)q.parts + t;
-      const uint64_t place = __ldcg(&w->place);
-      const float best = __ldcg(&w->best);
-      if (place && (!race.winner || !(best < race.best * NEAR))) {
-        if (!race.winner || best * NEAR > race.best || race.better(place, race.winner) == place) {
-          race.best = best;
-          race.winner = place;
-        }
-      }
-    }
+__device__ __noinline__ void race_again(Race& race, const Row<T>& row, int v, float bound, int step, float per, float c,
+                                        float high) {
+  for (int i = 0; i < Row<T>::E; ++i) {
+    if (v + i < 0 || v + i >= row.n) continue;
+    const float x = fmaxf(to_float(row.p[v + i]), -INFINITY);
+    if (!(x >= bound) || x == -INFINITY || (step != INT_MIN && step_of(x, per) <= step)) continue;
+    const float w = ex2f((x - race.weigh.top) * c), e = race.noise[v + i];
+    if (__fdividef(w, Race::number(e)) >= high * (1.0f - 0x1p-15f)) race.enter(x, v + i, race.weigh(x), e);
   }
-  if (alone) {  // (uniform)
-    whole_row<SPLIT, T>(a, r, sh);
-    return;
-  }
-  float best;
-  const uint64_t winner = block_winner<SPLIT>(race, sh, best);
-  if (t == 0) finish(a, r, winner, weigh.top, rec.sum1);
 }
 
-template <typename T>
-__global__ __launch_bounds__(SPLIT, 3) void k_sample_race(SplitArgs q) {
+// The cut that lies among the listed places; front: weight in front of them, want: what
+// the cut is at, total: all weight.  0 where it does not lie among them after all (the
+// steps' weights are rounded; these are not), or cannot be told.
+template <int N>
+__device__ uint64_t cut_places(const Places& places, const Weigh& weigh, uint64_t front, uint64_t want, uint64_t total,
+                               Shared& sh) {
+  uint64_t lo = ~0ull, hi = 0, sum = 0;
+  for (int i = threadIdx.x; i < places.n; i += N) {
+    const uint64_t x = places.p[i];
+    lo = min((unsigned long long)lo, (unsigned long long)x);
+    hi = max((unsigned long long)hi, (unsigned long long)x);
+    sum += fixed(weigh(value_of(x)));
+  }
+  lo = ~block_max<N>(~lo, sh.scratch);
+  hi = block_max<N>(hi, sh.scratch);
+  sum = block_sum<N>(sum, sh.scratch);
+  if (front >= want || front + sum < want) return 0;
+  return find_cut<N, false>(places, weigh, 0, front, want, 0x1p31f / ((float)total / FIXED), value_of(lo), value_of(hi), sh);
+}
+
+constexpr int STAGE = 1024;  // places that a block brings to the list at most
+
+template <typename T, int JP>
+__global__ __launch_bounds__(SPLIT, 4) void k_sample_race(SplitArgs q) {
+  using P = Packed<T>;
   constexpr int E = Row<T>::E;
-  __shared__ Shared sh;
+  __shared__ struct {
+    uint64_t list[STAGE];
+    Scratch scratch;
+    uint64_t winner[SPLIT / 32];
+    int listed, candidates, to;
+    uint64_t place[SPLIT];
+  } sh;
   const SampleArgs& a = q.a;
   const int64_t r = q.row0 + blockIdx.y, block = blockIdx.y * (int64_t)q.parts + blockIdx.x;
   const Row<T> row(a.logits, a.logits_stride, r, a.vocab);
-  const int t = threadIdx.x;
-  float x[EACH];
-  int v[EACH / E];
-  load_part(row, blockIdx.x, x, v);
+  const int t = threadIdx.x, g0 = blockIdx.x * (SPLIT * JP) + t;
+  griddep_launch_dependents();
   const Setting s = setting_of(a, r);
+  uint4 raw[JP];
+#pragma unroll
+  for (int j = 0; j < JP; ++j) raw[j] = load_raw(row, g0 + j * SPLIT);
+  if (t == 0) sh.listed = sh.candidates = 0;
   griddep_wait();
   RowRecord& rec = q.rows[blockIdx.y];
   const Mode mode = rec.mode;
-  if (mode == Mode::DONE) return;
-  if (mode == Mode::ALONE) {
-    if (blockIdx.x == 0) whole_row<SPLIT, T>(a, r, sh);
-    return;
-  }
-  const Weigh weigh = weigh_of(value_of(rec.first), s.temperature);
-  uint64_t* list = q.list + blockIdx.y * (int64_t)MOST_LISTED;
+  if (mode == Mode::DONE || mode == Mode::ALONE) return;
+  const float bound = rec.bound;
+  __syncthreads();
   auto append = [&](float y, int token) {
-    const unsigned to = atomicAdd(&rec.listed, 1u);
-    if (to < MOST_LISTED) list[to] = place_of(y, token);
+    const int to = atomicAdd(&sh.listed, 1);
+    if (to < STAGE) sh.list[to] = place_of(y, token);
   };
+#pragma unroll
+  for (int j = 0; j < JP; ++j) mask_nan<T>(raw[j]);
+  hold(raw);
   if (mode == Mode::BOUND) {
-    const float bound = rec.bound;
 #pragma unroll
-    for (int i = 0; i < EACH; ++i)
-      if (x[i] >= bound) append(x[i], v[i / E] + i % E);
-  } else {
-    const float per = steps_per(s.temperature);
-    const int step = rec.step;
-    Race race = {s, weigh, a.noise + r * a.noise_stride, rec.first};
-    float above = 0.0f;
+    for (int j = 0; j < JP; ++j)
+      if (P::top(piece_top<T>(raw[j])) >= bound) {
 #pragma unroll
-    for (int i = 0; i < EACH; ++i)
-      if (x[i] > -INFINITY) {
-        const int mine = step_of(x[i], per);
-        if (mine > step) {
-          const float w = weigh(x[i]);
-          above += w;
-          race.enter(x[i], v[i / E] + i % E, w);
-        } else if (mine == step) {
-          append(x[i], v[i / E] + i % E);
+        for (int i = 0; i < E; ++i) {
+          const float x = P::at(raw[j], i);
+          if (x >= bound) append(x, (g0 + j * SPLIT) * E - row.lead + i);
         }
       }
-    above = block_sum(above, sh.scratch);
-    float best;
-    const uint64_t winner = block_winner<SPLIT>(race, sh, best);
+    __syncthreads();
+  } else {
+    const Weigh weigh = weigh_of(value_of(rec.first), s.temperature);
+    const float per = steps_per(s.temperature), c = weigh.hi, top = weigh.top;
+    const int step = rec.step;
+    const float* noise = a.noise + r * a.noise_stride;
+    const bool wide = ((uintptr_t)(noise - row.lead) & 15) == 0;
+    Race race = {s, weigh, noise, rec.first};
+    // a product of float32's functions, 2^-17 off at most, first: its largest over the block
+    // says whom to race
+    float above = 0.0f, most = 0.0f;
+    auto needed = [&](int j) {
+      const float highest = P::top(piece_top<T>(raw[j]));
+      return highest >= bound && highest > -INFINITY;
+    };
+#pragma unroll
+    for (int j = 0; j < JP; ++j) {
+      const int v = (g0 + j * SPLIT) * E - row.lead;
+      if (v >= 0 && needed(j)) asm volatile("prefetch.global.L2 [%0];" ::"l"(noise + v));
+    }
+    hold(raw);
+#pragma unroll
+    for (int j0 = 0; j0 < JP; j0 += 2) {
+      float e[2][E];
+#pragma unroll
+      for (int j = j0; j < j0 + 2; ++j)
+        if (needed(j)) noise_of<E>(noise, wide, (g0 + j * SPLIT) * E - row.lead, row.n, e[j - j0]);
+#pragma unroll
+      for (int j = j0; j < j0 + 2; ++j) {
+        if (!needed(j)) continue;
+        const int v = (g0 + j * SPLIT) * E - row.lead;
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+          const float x = P::at(raw[j], i);
+          const int mine = step == INT_MIN ? 0 : x >= bound ? step_of(x, per) : INT_MIN;
+          if (mine > step) {
+            const float w = ex2f((x - top) * c);
+            above += w;
+            if (race.keeps(x, w)) most = fmaxf(most, __fdividef(w, Race::number(e[j - j0][i])));
+          } else if (mine == step) {
+            append(x, v + i);
+          }
+        }
+      }
+    }
+    hold(raw);
+    const float high = block_most(most, above, sh.scratch);  // (and the sum of the weights)
+    if (most > 0.0f && most >= high * (1.0f - 0x1p-15f)) {
+#pragma unroll 1
+      for (int j = 0; j < JP; ++j) race_again<T>(race, row, (g0 + j * SPLIT) * E - row.lead, bound, step, per, c, high);
+      if (race.winner) sh.place[atomicAdd(&sh.candidates, 1)] = race.winner;
+    }
+    __syncthreads();
     if (t == 0) {
-      q.winner[block] = {winner, best};
-      if (above > 0.0f) atomicAdd((unsigned long long*)&rec.above, (unsigned long long)fixed(above));
+      uint64_t w = sh.candidates ? sh.place[0] : 0;
+      for (int i = 1; i < sh.candidates; ++i) w = race.better(w, sh.place[i]);
+      q.winner[block] = {w, high, above};
     }
   }
-  __threadfence();
-  if (last_of(&rec.raced, q.parts, sh)) settle_race<T>(q, r, rec, s, weigh, sh);
+  // the list, behind what other blocks bring
+  const int n = sh.listed;
+  if (n == 0) return;
+  if (t == 0) sh.to = (int)min(atomicAdd(&rec.listed, (unsigned)(n > STAGE ? MOST_LISTED + 1 : n)), (unsigned)MOST_LISTED + 1);
+  __syncthreads();
+  uint64_t* list = q.list + blockIdx.y * (int64_t)MOST_LISTED;
+  for (int i = t; i < min(n, STAGE); i += SPLIT)
+    if (sh.to + i < MOST_LISTED) list[sh.to + i] = sh.list[i];
 }
 
-// Parts of a row (one more piece than it has, where it begins within one).
-int64_t parts_of(int64_t vocab) { return (vocab + 7 + PART - 1) / PART; }
+// The rest of a row: the list's cut and its race, the parts' winners.  A block per row.
+template <typename T>
+__global__ __launch_bounds__(SPLIT) void k_sample_finish(SplitArgs q) {
+  __shared__ Shared sh;
+  const SampleArgs& a = q.a;
+  const int64_t r = q.row0 + blockIdx.x;
+  const int t = threadIdx.x;
+  const Setting s = setting_of(a, r);
+  griddep_wait();
+  const RowRecord rec = q.rows[blockIdx.x];
+  if (rec.mode == Mode::DONE) return;
+  const int listed = (int)rec.listed;
+  if (rec.mode == Mode::ALONE || listed > (rec.mode == Mode::BOUND ? LIST : MOST_LISTED)) {
+    whole_row<SPLIT, T>(a, r, sh);
+    return;
+  }
+  const uint64_t* list = q.list + blockIdx.x * (int64_t)MOST_LISTED;
+  const Weigh weigh = weigh_of(value_of(rec.first), s.temperature);
+  Race race = {s, weigh, a.noise + r * a.noise_stride, rec.first};
+  if (rec.mode == Mode::BOUND) {
+    for (int i = t; i < listed; i += SPLIT) sh.list[i] = list[i];
+    sort_list<SPLIT>(sh, listed);
+    const int n = cut_list<SPLIT>(s, weigh, listed, sh);
+    for (int i = t; i < n; i += SPLIT) race.enter(value_of(sh.list[i]), token_of(sh.list[i]));
+  } else {
+    PartWinner w = {0, 0.0f, 0.0f};
+    if (t < q.parts) w = q.winner[blockIdx.x * (int64_t)q.parts + t];
+    if (w.place) {
+      race.best = w.best;
+      race.winner = w.place;
+    }
+    if (listed) {
+      const uint64_t want = part_of(s.top_p, rec.sum), front = block_sum<SPLIT>(fixed(w.above), sh.scratch);
+      const uint64_t cut = cut_places<SPLIT>({list, listed}, weigh, front, want, rec.sum, sh);
+      if (cut == 0) {  // (uniform)
+        whole_row<SPLIT, T>(a, r, sh);
+        return;
+      }
+      for (int i = t; i < listed; i += SPLIT) {
+        const uint64_t x = list[i];
+        if (x >= cut) race.enter(value_of(x), token_of(x));
+      }
+    }
+  }
+  float best;
+  const uint64_t winner = block_winner<SPLIT>(race, sh, best);
+  if (t == 0) finish(a, r, winner ? winner : rec.first, weigh.top, rec.sum1);  // (none: every quotient is 0)
+}
+
+// ---- a row of up to 8 pieces a thread by one block, held in registers --------
+//
+// The four kernels' steps in one: no round trip over memory in between.
+constexpr int ONE = 1024;
+constexpr float ONE_UNIT = 32768.0f;  // as STEP_ONE: 2^16 of them fit
+struct OneShared {
+  Shared sh;
+  uint64_t places[LIST];
+  uint32_t steps[STEPS];
+  float most[ONE / 32], sums[2][ONE / 32];
+};
+
+template <typename T, int JP>
+__global__ __launch_bounds__(ONE) void k_sample_one(SampleArgs a) {
+  using P = Packed<T>;
+  constexpr int E = Row<T>::E;
+  extern __shared__ unsigned char raw_smem[];
+  OneShared& one = *reinterpret_cast<OneShared*>(raw_smem);
+  Shared& sh = one.sh;
+  const int64_t r = blockIdx.x;
+  const Row<T> row(a.logits, a.logits_stride, r, a.vocab);
+  const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
+  uint4 raw[JP];
+#pragma unroll
+  for (int j = 0; j < JP; ++j) raw[j] = load_raw(row, t + j * ONE);
+  const Setting s = setting_of(a, r);
+  const bool cut = s.hot && s.k == a.vocab && s.top_p < 1.0f;
+  const float* noise = a.noise + r * a.noise_stride;
+  uint32_t packed = P::MASKED;
+#pragma unroll
+  for (int j = 0; j < JP; ++j) {
+    mask_nan<T>(raw[j]);
+    packed = P::largest(packed, piece_top<T>(raw[j]));
+  }
+  const float mine = P::top(packed);
+  hold(raw);
+  if (t < STEPS) one.steps[t] = 0;
+  for (int i = t; i < BINS; i += ONE) sh.bins[i] = 0;
+  // the row's largest and smallest thread's largest, then the lowest token
+  const uint32_t high = __reduce_max_sync(FULL, ordered(mine));
+  const uint32_t low = __reduce_max_sync(FULL, mine > -INFINITY ? ~ordered(mine) : 0u);
+  if (lane == 0) sh.scratch.words[warp] = (uint64_t)high << 32 | low;
+  if (t == 0) {
+    sh.low = 0xffffffffu;
+    sh.listed = sh.candidates = 0;
+    sh.bin = -1;
+  }
+  __syncthreads();
+  const uint64_t word = sh.scratch.words[lane];
+  const float top = unordered(__reduce_max_sync(FULL, (uint32_t)(word >> 32)));
+  const float least_top = unordered(~__reduce_max_sync(FULL, (uint32_t)word));
+  if (top == -INFINITY) {
+    if (t == 0) finish(a, r, 0, 0.0f, 0);
+    return;
+  }
+  const float per = steps_per(s.temperature);
+  const bool alone = top == INFINITY || (s.hot && (s.k < a.vocab ? s.k > MOST_K : s.top_p < 1.0f && !(fabsf(top) * per < MOST_STEP)));
+  if (alone) {  // (uniform)
+    __syncthreads();
+    whole_row<ONE, T>(a, r, sh);
+    return;
+  }
+  const Weigh weigh = weigh_of(top, s.hot ? s.temperature : 1.0f);
+  const float c = weigh.hi;
+  if (mine == top) {
+    int at = INT_MAX;
+#pragma unroll
+    for (int j = 0; j < JP; ++j)
+#pragma unroll
+      for (int i = 0; i < E; ++i)
+        if (P::at(raw[j], i) == top) at = min(at, (t + j * ONE) * E - row.lead + i);
+    atomicMin(&sh.low, (uint32_t)at);
+  }
+  hold(raw);
+  float sum1 = 0.0f, sum = 0.0f;
+#pragma unroll
+  for (int j = 0; j < JP; ++j) {
+    float y[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) y[i] = ex2f((P::at(raw[j], i) - top) * LOG2E);
+#pragma unroll
+    for (int o = 1; o < E; o <<= 1)
+#pragma unroll
+      for (int i = 0; i < E; i += 2 * o) y[i] += y[i + o];
+    sum1 += y[0];
+  }
+  hold(raw);
+  const int highest = cut ? step_of(top, per) : 0;
+  if (cut) {
+    const float least = top - (STEPS + 8) / per;
+#pragma unroll
+    for (int j = 0; j < JP; ++j) {
+      if (P::top(piece_top<T>(raw[j])) < least) continue;
+      float y = 0.0f;
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        const float x = P::at(raw[j], i);
+        if (x >= least) {
+          y += ex2f((x - top) * c);
+          const int step = step_of(x, per), slot = highest - step;
+          const float up = (__fmul_rn(x, per) - ((float)step + 0.5f)) * (LOG2E / 32.0f);
+          const uint32_t w = __float_as_uint(fmaf(ex2f(up), ONE_UNIT, ROUND)) - __float_as_uint(ROUND);
+          if (slot < STEPS) atomicAdd(&one.steps[slot], w);
+        }
+      }
+      sum += y;
+    }
+  } else if (s.hot && s.k < a.vocab && mine > -INFINITY) {
+    // how many threads' largest lie in each of equal steps
+    const float bins_per = top > least_top ? (BINS - 1) / (top - least_top) : 0.0f;
+    atomicAdd(&sh.bins[(int)fminf((top - mine) * bins_per, (float)(BINS - 1))], 1u);
+  }
+  sum1 = warp_sum(sum1);
+  sum = warp_sum(sum);
+  if (lane == 0) {
+    one.sums[0][warp] = sum1;
+    one.sums[1][warp] = sum;
+  }
+  __syncthreads();
+  const uint64_t total1 = fixed(warp_sum(one.sums[0][lane])), total = fixed(warp_sum(one.sums[1][lane]));
+  const uint64_t first = place_of(top, (int)sh.low);
+  if (!s.hot) {
+    if (t == 0) finish(a, r, first, top, total1);
+    return;
+  }
+  Race race = {s, weigh, noise, first};
+  auto append = [&](float y, int token) {
+    const int to = atomicAdd(&sh.listed, 1);
+    if (to < LIST) one.places[to] = place_of(y, token);
+  };
+  if (s.k < a.vocab) {
+    // ---- the values that k threads' largest reach, sorted
+    uint64_t all;
+    const uint64_t some = sh.bins[2 * t] + sh.bins[2 * t + 1], upto = block_scan<ONE>(some, sh.scratch, all);
+    if (upto < (uint64_t)s.k && upto + some >= (uint64_t)s.k) sh.bin = upto + sh.bins[2 * t] >= (uint64_t)s.k ? 2 * t : 2 * t + 1;
+    __syncthreads();
+    const int bin = sh.bin;
+    if (bin < 0) {  // (fewer threads with tokens than k)
+      whole_row<ONE, T>(a, r, sh);
+      return;
+    }
+    const float bins_per = top > least_top ? (BINS - 1) / (top - least_top) : 0.0f;
+#pragma unroll
+    for (int j = 0; j < JP; ++j)
+      if (P::top(piece_top<T>(raw[j])) > -INFINITY) {
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+          const float x = P::at(raw[j], i);
+          if (x > -INFINITY && (int)fminf((top - x) * bins_per, (float)(BINS - 1)) <= bin)
+            append(x, (t + j * ONE) * E - row.lead + i);
+        }
+      }
+    __syncthreads();
+    const int n = sh.listed;
+    __syncthreads();
+    if (n > LIST) {
+      whole_row<ONE, T>(a, r, sh);
+      return;
+    }
+    for (int i = t; i < n; i += ONE) sh.list[i] = one.places[i];
+    sort_list<ONE>(sh, n);
+    const int kept = cut_list<ONE>(s, weigh, n, sh);
+    for (int i = t; i < kept; i += ONE) race.enter(value_of(sh.list[i]), token_of(sh.list[i]));
+  } else {
+    // ---- what lies above the step that top-p's cut is in; what lies in it
+    int step = INT_MIN;
+    float bound = -INFINITY;
+    const uint64_t want = cut ? part_of(s.top_p, total) : 0;
+    if (cut) {
+      const float up = ((float)(highest - t) + 0.5f - top * per) * (1.0f / 32.0f);
+      const uint64_t w = (uint64_t)((float)one.steps[t] * (FIXED / ONE_UNIT) * ex2f(up * LOG2E));
+      uint64_t all;
+      const uint64_t upto = block_scan<ONE>(w, sh.scratch, all);
+      if (w && upto < want && upto + w >= want) sh.bin = t;
+      __syncthreads();
+      step = highest - (sh.bin < 0 ? STEPS - 1 : sh.bin);
+      bound = ((float)step - 0.51f) / per;
+      bound -= fabsf(bound) * 0x1p-21f;
+    } else if (s.min_p > 0.0f) {
+      bound = least_kept(s, top);
+    }
+    const bool wide = ((uintptr_t)(noise - row.lead) & 15) == 0;
+    float above = 0.0f, most = 0.0f;
+#pragma unroll
+    for (int j = 0; j < JP; ++j) {
+      const float here = P::top(piece_top<T>(raw[j]));
+      if (!(here >= bound) || here == -INFINITY) continue;
+      const int v = (t + j * ONE) * E - row.lead;
+      float e[E];
+      noise_of<E>(noise, wide, v, row.n, e);
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        const float x = P::at(raw[j], i);
+        const int at = step == INT_MIN ? 0 : x >= bound ? step_of(x, per) : INT_MIN;
+        if (at > step) {
+          const float w = ex2f((x - top) * c);
+          above += w;
+          if (race.keeps(x, w)) most = fmaxf(most, __fdividef(w, Race::number(e[i])));
+        } else if (at == step) {
+          append(x, v + i);
+        }
+      }
+    }
+    const float warp_most = __uint_as_float(__reduce_max_sync(FULL, __float_as_uint(most)));
+    above = warp_sum(above);
+    if (lane == 0) {
+      one.most[warp] = warp_most;
+      one.sums[0][warp] = above;
+    }
+    __syncthreads();
+    const float high_q = __uint_as_float(__reduce_max_sync(FULL, __float_as_uint(one.most[lane])));
+    if (most > 0.0f && most >= high_q * (1.0f - 0x1p-15f)) {
+#pragma unroll 1
+      for (int j = 0; j < JP; ++j) race_again<T>(race, row, (t + j * ONE) * E - row.lead, bound, step, per, c, high_q);
+    }
+    const int listed = sh.listed;
+    if (listed) {
+      const uint64_t front = fixed(warp_sum(one.sums[0][lane]));
+      const uint64_t at = listed <= LIST ? cut_places<ONE>({one.places, listed}, weigh, front, want, total, sh) : 0;
+      if (at == 0) {  // (uniform)
+        __syncthreads();
+        whole_row<ONE, T>(a, r, sh);
+        return;
+      }
+      for (int i = t; i < listed; i += ONE) {
+        const uint64_t x = one.places[i];
+        if (x >= at) race.enter(value_of(x), token_of(x));
+      }
+    }
+  }
+  float best;
+  const uint64_t winner = block_winner<ONE>(race, sh, best);
+  if (t == 0) finish(a, r, winner ? winner : first, top, total1);
+}
+
+// Parts of a row of pieces of E tokens, JP of them a thread (and one more piece than it
+// has, where it begins within one).
+int64_t parts_of(int64_t vocab, int each, int jp) {
+  return (vocab + each - 1 + (int64_t)SPLIT * jp * each - 1) / ((int64_t)SPLIT * jp * each);
+}
 
 size_t round_up(size_t x) { return (x + 255) / 256 * 256; }
 
@@ -1070,23 +1538,38 @@ Sizes sizes_of(int64_t rows, int64_t blocks) {
   z.rows = round_up(rows * sizeof(RowRecord));
   z.part = round_up(blocks * sizeof(PartRecord));
   z.winner = round_up(blocks * sizeof(PartWinner));
-  z.groups = round_up(blocks * GROUPS * sizeof(float));
+  z.groups = round_up(blocks * SPLIT * sizeof(float));
   z.steps = round_up(blocks * STEPS * sizeof(uint32_t));
   z.list = round_up(rows * MOST_LISTED * sizeof(uint64_t));
   z.total = z.rows + z.part + z.winner + z.groups + z.steps + z.list;
   return z;
 }
 
+template <typename T, int JP>
+cudaError_t one_block(const SampleArgs& a, int64_t n, cudaStream_t s) {
+  auto* kernel = k_sample_one<T, JP>;
+  const cudaError_t e = set_max_dynamic_smem(reinterpret_cast<const void*>(kernel), sizeof(OneShared));
+  if (e != cudaSuccess) return e;
+  kernel<<<(unsigned)n, ONE, sizeof(OneShared), s>>>(a);
+  return cudaGetLastError();
+}
+
 template <typename T>
 cudaError_t sample(const SampleArgs& a, int64_t n, void* workspace, cudaStream_t s) {
-  const int64_t parts = parts_of(a.vocab);
-  if (parts == 1 || parts > MOST_PARTS) {
-    if (parts == 1)
-      k_sample_row<256, T><<<(unsigned)n, 256, 0, s>>>(a);
-    else
-      k_sample_row<1024, T><<<(unsigned)n, 1024, 0, s>>>(a);
+  constexpr int E = Row<T>::E;
+  const int64_t wide = parts_of(a.vocab, E, 8), narrow = parts_of(a.vocab, E, 2);
+  const int64_t pieces = (a.vocab + 2 * E - 2) / E;  // (and one more, where a row begins within one)
+  if (pieces <= 256) {
+    k_sample_row<256, T><<<(unsigned)n, 256, 0, s>>>(a);
     return cudaGetLastError();
   }
+  if (pieces <= 8 * ONE) return pieces <= 2 * ONE ? one_block<T, 2>(a, n, s) : pieces <= 4 * ONE ? one_block<T, 4>(a, n, s) : one_block<T, 8>(a, n, s);
+  if (wide > MOST_PARTS) {
+    k_sample_row<1024, T><<<(unsigned)n, 1024, 0, s>>>(a);
+    return cudaGetLastError();
+  }
+  const bool few = n * wide < FEW_BLOCKS && narrow <= MOST_PARTS;
+  const int64_t parts = few ? narrow : wide;
   const int64_t rows = std::min<int64_t>({n, MOST_ROWS, MOST_BLOCKS / parts});
   const Sizes z = sizes_of(rows, rows * parts);
   char* p = static_cast<char*>(workspace);
@@ -1099,25 +1582,28 @@ cudaError_t sample(const SampleArgs& a, int64_t n, void* workspace, cudaStream_t
   q.groups = reinterpret_cast<float*>(p), p += z.groups;
   q.steps = reinterpret_cast<uint32_t*>(p), p += z.steps;
   q.list = reinterpret_cast<uint64_t*>(p);
+  const int jp = few ? 2 : 8;
   for (q.row0 = 0; q.row0 < n; q.row0 += rows) {
-    const dim3 grid((unsigned)parts, (unsigned)std::min(rows, n - q.row0));
-    cudaError_t e = cudaMemsetAsync(q.rows, 0, grid.y * sizeof(RowRecord), s);
+    const dim3 grid((unsigned)parts, (unsigned)std::min(rows, n - q.row0)), per_row(grid.y), block(SPLIT);
+    (few ? k_sample_parts<T, 2> : k_sample_parts<T, 8>)<<<grid, block, 0, s>>>(q);
+    cudaError_t e = cudaGetLastError();
+    if (e == cudaSuccess) e = launch_maybe_pdl(true, k_sample_cut, per_row, block, 0, s, q, SPLIT * jp * E / GROUP);
+    if (e == cudaSuccess) e = launch_maybe_pdl(true, few ? k_sample_race<T, 2> : k_sample_race<T, 8>, grid, block, 0, s, q);
+    if (e == cudaSuccess) e = launch_maybe_pdl(true, k_sample_finish<T>, per_row, block, 0, s, q);
     if (e != cudaSuccess) return e;
-    k_sample_parts<T><<<grid, SPLIT, 0, s>>>(q);
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
-    if ((e = launch_maybe_pdl(true, k_sample_race<T>, grid, dim3(SPLIT), 0, s, q)) != cudaSuccess) return e;
   }
   return cudaSuccess;
 }
 
 }  // namespace
 
-// Enough for every smaller call too: of as many rows as a launch takes, or as many blocks.
+// Enough for every smaller call too, whatever the type: rows of a launch, and the blocks
+// that either form has of float32.
 size_t sample_workspace(int64_t n, int64_t vocab) {
-  const int64_t parts = std::min<int64_t>(parts_of(vocab), MOST_PARTS);
-  if (n == 0 || parts == 1) return 0;
-  const int64_t rows = std::min<int64_t>(n, MOST_ROWS);
-  return sizes_of(rows, std::min<int64_t>(rows * parts, MOST_BLOCKS)).total;
+  if (n == 0 || parts_of(vocab, 4, 2) == 1) return 0;
+  const int64_t wide = std::min<int64_t>(parts_of(vocab, 4, 8), MOST_PARTS), rows = std::min<int64_t>(n, MOST_ROWS);
+  const int64_t few = std::min<int64_t>(n * parts_of(vocab, 4, 2), 4 * FEW_BLOCKS + rows);
+  return sizes_of(rows, std::max(std::min<int64_t>(rows * wide, MOST_BLOCKS), few)).total;
 }
 
 cudaError_t launch_sample(const void* logits, int type, int64_t logits_stride, const float* noise, int64_t noise_stride,
