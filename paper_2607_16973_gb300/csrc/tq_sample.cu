@@ -429,9 +429,11 @@ struct Race {
 
   // (no quotient is negative, NaN or infinite, whatever the noise)
   static __device__ __forceinline__ float number(float e) { return fmaxf(e, 0x1p-126f); }
-  __device__ __forceinline__ double weight(float x) const {
-    return exp(((double)x - (double)weigh.top) / (double)s.temperature);
+  // (rarely asked, and long: not inlined where a row's tokens go by)
+  static __device__ __noinline__ double exact(float x, float top, float temperature) {
+    return exp(((double)x - (double)top) / (double)temperature);
   }
+  __device__ __forceinline__ double weight(float x) const { return exact(x, weigh.top, s.temperature); }
   __device__ __forceinline__ double quotient(uint64_t place) const {
     return weight(value_of(place)) / (double)number(noise[token_of(place)]);
   }
@@ -1090,16 +1092,23 @@ __device__ __forceinline__ void noise_of(const float* noise, bool wide, int v, i
     for (int i = 0; i < E; ++i) e[i] = v + i >= 0 && v + i < n ? noise[v + i] : 1.0f;
   }
 }
-// Races those of the piece from v on that lie above the step and whose quotient is about `high`.
-template <typename T>
-__device__ __noinline__ void race_again(Race& race, const Row<T>& row, int v, float bound, int step, float per, float c,
-                                        float high) {
-  for (int i = 0; i < Row<T>::E; ++i) {
-    if (v + i < 0 || v + i >= row.n) continue;
-    const float x = fmaxf(to_float(row.p[v + i]), -INFINITY);
-    if (!(x >= bound) || x == -INFINITY || (step != INT_MIN && step_of(x, per) <= step)) continue;
-    const float w = ex2f((x - race.weigh.top) * c), e = race.noise[v + i];
-    if (__fdividef(w, Race::number(e)) >= high * (1.0f - 0x1p-15f)) race.enter(x, v + i, race.weigh(x), e);
+// Races the tokens above the step whose quotient is about `high`: those of the pieces
+// first + j * THREADS of each lane that has one (`mine`).  By a whole warp, a token a lane.
+template <typename T, int JP, int THREADS>
+__device__ __noinline__ void race_again(Race& race, const Row<T>& row, bool mine, int first, float bound, int step, float per,
+                                        float c, float high) {
+  constexpr int E = Row<T>::E;
+  for (unsigned left = __ballot_sync(FULL, mine); left; left &= left - 1) {
+    const int g0 = __shfl_sync(FULL, first, __ffs(left) - 1);
+#pragma unroll 1
+    for (int k = threadIdx.x & 31; k < JP * E; k += 32) {
+      const int v = (g0 + k / E * THREADS) * E - row.lead + k % E;
+      if (v < 0 || v >= row.n) continue;
+      const float x = fmaxf(to_float(row.p[v]), -INFINITY);
+      if (!(x >= bound) || x == -INFINITY || (step != INT_MIN && step_of(x, per) <= step)) continue;
+      const float w = ex2f((x - race.weigh.top) * c), e = race.noise[v];
+      if (__fdividef(w, Race::number(e)) >= high * (1.0f - 0x1p-15f)) race.enter(x, v, race.weigh(x), e);
+    }
   }
 }
 
@@ -1132,7 +1141,6 @@ __global__ __launch_bounds__(SPLIT, 4) void k_sample_race(SplitArgs q) {
   __shared__ struct {
     uint64_t list[STAGE];
     Scratch scratch;
-    uint64_t winner[SPLIT / 32];
     int listed, candidates, to;
     uint64_t place[SPLIT];
   } sh;
@@ -1142,10 +1150,9 @@ __global__ __launch_bounds__(SPLIT, 4) void k_sample_race(SplitArgs q) {
   const int t = threadIdx.x, g0 = blockIdx.x * (SPLIT * JP) + t;
   griddep_launch_dependents();
   const Setting s = setting_of(a, r);
-  uint4 raw[JP];
-#pragma unroll
-  for (int j = 0; j < JP; ++j) raw[j] = load_raw(row, g0 + j * SPLIT);
   if (t == 0) sh.listed = sh.candidates = 0;
+  // (one piece at a time, the next on its way: unrolled, the code is more than the SM's caches hold)
+  uint4 next = load_raw(row, g0);
   griddep_wait();
   RowRecord& rec = q.rows[blockIdx.y];
   const Mode mode = rec.mode;
@@ -1156,19 +1163,18 @@ __global__ __launch_bounds__(SPLIT, 4) void k_sample_race(SplitArgs q) {
     const int to = atomicAdd(&sh.listed, 1);
     if (to < STAGE) sh.list[to] = place_of(y, token);
   };
-#pragma unroll
-  for (int j = 0; j < JP; ++j) mask_nan<T>(raw[j]);
-  hold(raw);
   if (mode == Mode::BOUND) {
+#pragma unroll 1
+    for (int j = 0; j < JP; ++j) {
+      uint4 u = next;
+      if (j + 1 < JP) next = load_raw(row, g0 + (j + 1) * SPLIT);
+      mask_nan<T>(u);
+      if (P::top(piece_top<T>(u)) >= bound) {
 #pragma unroll
-    for (int j = 0; j < JP; ++j)
-      if (P::top(piece_top<T>(raw[j])) >= bound) {
-#pragma unroll
-        for (int i = 0; i < E; ++i) {
-          const float x = P::at(raw[j], i);
-          if (x >= bound) append(x, (g0 + j * SPLIT) * E - row.lead + i);
-        }
+        for (int i = 0; i < E; ++i)
+          if (P::at(u, i) >= bound) append(P::at(u, i), (g0 + j * SPLIT) * E - row.lead + i);
       }
+    }
     __syncthreads();
   } else {
     const Weigh weigh = weigh_of(value_of(rec.first), s.temperature);
@@ -1178,49 +1184,48 @@ __global__ __launch_bounds__(SPLIT, 4) void k_sample_race(SplitArgs q) {
     const bool wide = ((uintptr_t)(noise - row.lead) & 15) == 0;
     Race race = {s, weigh, noise, rec.first};
     // a product of float32's functions, 2^-17 off at most, first: its largest over the block
-    // says whom to race
-    float above = 0.0f, most = 0.0f;
-    auto needed = [&](int j) {
-      const float highest = P::top(piece_top<T>(raw[j]));
-      return highest >= bound && highest > -INFINITY;
+    // says whom to race.  A piece is weighed while the noise of the next one, which is asked
+    // for where some token of it matters, and the one behind are on their way.
+    float above = 0.0f, most = 0.0f, e0[E], e1[E];
+    uint4 u0 = next, u1;
+    bool need0, need1 = false;
+    auto ask = [&](uint4& u, int j, float (&e)[E]) {
+      mask_nan<T>(u);
+      const float highest = P::top(piece_top<T>(u));
+      const bool need = highest >= bound && highest > -INFINITY;
+      if (need) noise_of<E>(noise, wide, (g0 + j * SPLIT) * E - row.lead, row.n, e);
+      return need;
     };
-#pragma unroll
+    if (JP > 1) next = load_raw(row, g0 + SPLIT);
+    need0 = ask(u0, 0, e0);
+#pragma unroll 1
     for (int j = 0; j < JP; ++j) {
-      const int v = (g0 + j * SPLIT) * E - row.lead;
-      if (v >= 0 && needed(j)) asm volatile("prefetch.global.L2 [%0];" ::"l"(noise + v));
-    }
-    hold(raw);
-#pragma unroll
-    for (int j0 = 0; j0 < JP; j0 += 2) {
-      float e[2][E];
-#pragma unroll
-      for (int j = j0; j < j0 + 2; ++j)
-        if (needed(j)) noise_of<E>(noise, wide, (g0 + j * SPLIT) * E - row.lead, row.n, e[j - j0]);
-#pragma unroll
-      for (int j = j0; j < j0 + 2; ++j) {
-        if (!needed(j)) continue;
-        const int v = (g0 + j * SPLIT) * E - row.lead;
+      u1 = next;
+      if (j + 2 < JP) next = load_raw(row, g0 + (j + 2) * SPLIT);
+      need1 = j + 1 < JP && ask(u1, j + 1, e1);
+      if (need0) {
 #pragma unroll
         for (int i = 0; i < E; ++i) {
-          const float x = P::at(raw[j], i);
+          const float x = P::at(u0, i);
           const int mine = step == INT_MIN ? 0 : x >= bound ? step_of(x, per) : INT_MIN;
           if (mine > step) {
             const float w = ex2f((x - top) * c);
             above += w;
-            if (race.keeps(x, w)) most = fmaxf(most, __fdividef(w, Race::number(e[j - j0][i])));
+            if (race.keeps(x, w)) most = fmaxf(most, __fdividef(w, Race::number(e0[i])));
           } else if (mine == step) {
-            append(x, v + i);
+            append(x, (g0 + j * SPLIT) * E - row.lead + i);
           }
         }
       }
+      u0 = u1;
+      need0 = need1;
+#pragma unroll
+      for (int i = 0; i < E; ++i) e0[i] = e1[i];
     }
-    hold(raw);
     const float high = block_most(most, above, sh.scratch);  // (and the sum of the weights)
-    if (most > 0.0f && most >= high * (1.0f - 0x1p-15f)) {
-#pragma unroll 1
-      for (int j = 0; j < JP; ++j) race_again<T>(race, row, (g0 + j * SPLIT) * E - row.lead, bound, step, per, c, high);
-      if (race.winner) sh.place[atomicAdd(&sh.candidates, 1)] = race.winner;
-    }
+    const bool mine = most > 0.0f && most >= high * (1.0f - 0x1p-15f);
+    if (__any_sync(FULL, mine)) race_again<T, JP, SPLIT>(race, row, mine, g0, bound, step, per, c, high);
+    if (race.winner) sh.place[atomicAdd(&sh.candidates, 1)] = race.winner;
     __syncthreads();
     if (t == 0) {
       uint64_t w = sh.candidates ? sh.place[0] : 0;
@@ -1498,10 +1503,8 @@ __global__ __launch_bounds__(ONE) void k_sample_one(SampleArgs a) {
     }
     __syncthreads();
     const float high_q = __uint_as_float(__reduce_max_sync(FULL, __float_as_uint(one.most[lane])));
-    if (most > 0.0f && most >= high_q * (1.0f - 0x1p-15f)) {
-#pragma unroll 1
-      for (int j = 0; j < JP; ++j) race_again<T>(race, row, (t + j * ONE) * E - row.lead, bound, step, per, c, high_q);
-    }
+    const bool ahead = most > 0.0f && most >= high_q * (1.0f - 0x1p-15f);
+    if (__any_sync(FULL, ahead)) race_again<T, JP, ONE>(race, row, ahead, t, bound, step, per, c, high_q);
     const int listed = sh.listed;
     if (listed) {
       const uint64_t front = fixed(warp_sum(one.sums[0][lane]));
