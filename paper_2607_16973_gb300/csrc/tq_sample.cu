@@ -262,14 +262,14 @@ __device__ uint64_t find_cut(const Source& row, const Weigh& weigh, uint64_t kep
     const uint64_t rest = want > front ? want - front : 0;
     const uint64_t need = BY_COUNT ? rest : (uint64_t)((float)rest * (scale / FIXED));
     uint64_t mine = 0, all;
-#pragma unroll
+#pragma unroll 1
     for (int i = 0; i < BINS / N; ++i) {
       const int b = threadIdx.x * (BINS / N) + i;
       mine += sh.bins[b];
     }
     if (threadIdx.x == 0) sh.bin = -1;
     uint64_t upto = block_scan<N>(mine, sh.scratch, all);
-#pragma unroll
+#pragma unroll 1
     for (int i = 0; i < BINS / N; ++i) {
       const int b = threadIdx.x * (BINS / N) + i;
       const uint64_t here = sh.bins[b];
@@ -330,19 +330,17 @@ __device__ uint64_t find_cut(const Source& row, const Weigh& weigh, uint64_t kep
       // sorted: the last of them with too little in front of it
       sort_list<N>(sh, listed);
       if (threadIdx.x == 0) sh.cut = sh.list[0];
-      uint64_t here[LIST / N], sum = 0;
-#pragma unroll
-      for (int i = 0; i < LIST / N; ++i) {
-        const int at = threadIdx.x * (LIST / N) + i;
-        here[i] = at < listed ? (BY_COUNT ? 1 : fixed(weigh(value_of(sh.list[at])))) : 0;
-        sum += here[i];
-      }
+      const int each = (listed + N - 1) / N, from = threadIdx.x * each, to = min(listed, from + each);
+      auto here = [&](int at) { return BY_COUNT ? (uint64_t)1 : fixed(weigh(value_of(sh.list[at]))); };
+      uint64_t sum = 0;
+#pragma unroll 1
+      for (int at = from; at < to; ++at) sum += here(at);
       uint64_t before = front + block_scan<N>(sum, sh.scratch, all);
-#pragma unroll
-      for (int i = 0; i < LIST / N; ++i) {
-        const int at = threadIdx.x * (LIST / N) + i;
-        if (at < listed && before < want && (before + here[i] >= want || at == listed - 1)) sh.cut = sh.list[at];
-        before += here[i];
+#pragma unroll 1
+      for (int at = from; at < to; ++at) {
+        const uint64_t x = here(at);
+        if (before < want && (before + x >= want || at == listed - 1)) sh.cut = sh.list[at];
+        before += x;
       }
       __syncthreads();
       const uint64_t cut = sh.cut;
@@ -493,21 +491,18 @@ template <int N>
 __device__ int cut_list(const Setting& s, const Weigh& weigh, int n, Shared& sh) {
   n = min(n, s.k);
   if (!(s.top_p < 1.0f)) return n;
-  uint64_t here[LIST / N], part = 0, sum;
-#pragma unroll
-  for (int i = 0; i < LIST / N; ++i) {
-    const int e = threadIdx.x * (LIST / N) + i;
-    here[i] = e < n ? fixed(weigh(value_of(sh.list[e]))) : 0;
-    part += here[i];
-  }
+  // a thread takes some neighbours.  (Rolled: code that runs once costs more to fetch than to run.)
+  const int each = (n + N - 1) / N, from = threadIdx.x * each, to = min(n, from + each);
+  uint64_t part = 0, sum;
+#pragma unroll 1
+  for (int e = from; e < to; ++e) part += fixed(weigh(value_of(sh.list[e])));
   uint64_t before = block_scan<N>(part, sh.scratch, sum);
   const uint64_t want = part_of(s.top_p, sum);
   int count = 0;
-#pragma unroll
-  for (int i = 0; i < LIST / N; ++i) {
-    const int e = threadIdx.x * (LIST / N) + i;
-    if (e < n && (e == 0 || before < want)) ++count;
-    before += here[i];
+#pragma unroll 1
+  for (int e = from; e < to; ++e) {
+    count += e == 0 || before < want;
+    before += fixed(weigh(value_of(sh.list[e])));
   }
   return (int)block_sum<N>((uint64_t)count, sh.scratch);
 }
@@ -901,10 +896,10 @@ __global__ __launch_bounds__(SPLIT) void k_sample_cut(SplitArgs q, int groups_of
       }
       __syncthreads();
       uint64_t some = 0, all;
-#pragma unroll
+#pragma unroll 1
       for (int i = 0; i < BINS / SPLIT; ++i) some += sh.bins[t * (BINS / SPLIT) + i];
       uint64_t upto = block_scan<SPLIT>(some, sh.scratch, all);
-#pragma unroll
+#pragma unroll 1
       for (int i = 0; i < BINS / SPLIT; ++i) {
         const unsigned here = sh.bins[t * (BINS / SPLIT) + i];
         if (upto < (uint64_t)s.k && upto + here >= (uint64_t)s.k) sh.listed = t * (BINS / SPLIT) + i;
