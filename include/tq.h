@@ -765,7 +765,7 @@ tq_status tq_verify_drafts(const void* target, const void* draft, int type,
  *            elements apart (any alignment of the elements' own size).  -INFINITY masks
  *            a token; NaN counts as -INFINITY, +INFINITY as the largest float
  *   noise    device [n][vocab] float32, exponentially distributed, rows noise_stride
- *            elements apart; what is below 2^-126, or NaN, counts as 2^-126
+ *            elements apart; taken as 2^-126 where it is less or NaN, as 2^20 where it is more
  *   temperature, top_k, top_p, min_p  device [n] each, nullable (1, 0, 1, 0)
  *   tokens   device out [n] int32
  *   logprobs device out [n] float32 (nullable): x_token - ln sum_v e^(x_v), at
@@ -778,7 +778,8 @@ tq_status tq_verify_drafts(const void* target, const void* draft, int type,
  * them (all for top_p >= 1); of those, the ones with w >= min_p; the first always. The
  * token is the kept one with the largest w / noise, the lowest of equals. A
  * temperature that is 0, negative or NaN keeps the first alone, and so does a top_p or
- * min_p of NaN. A row without a token that is not masked gives token 0 and -INFINITY.
+ * min_p of NaN; one above 1e30 counts as 1e30. A row without a token that is not
+ * masked gives token 0 and -INFINITY.
  * The answer is that of these definitions in 64 bits but for tokens whose weight, or
  * the weight in front of them, is within 2^-20 of a border, and weights below
  * 2^-126, which count as 0. n in [0, 65535], vocab in [1, 2^24].

@@ -16,6 +16,19 @@
 //
 // Quotients are taken in float32; those within 2^-18 of the largest are compared again
 // in 64 bits, so that the token is that of exact arithmetic.
+//
+// Three forms.  Rows of up to 256 pieces of 16 bytes, and rows beyond 256 parts, by a block
+// that reads them again for every step (whole_row).  Rows of up to 8 pieces for each of
+// 1,024 threads by a block that holds them in registers (k_sample_one).  Longer ones in
+// parts, by four kernels.
+//
+// Bound: HBM for the parts' first reading; the rest is the chain of a row's steps and, for
+// code that runs once a launch, its fetching.  256 rows of 128,000 bf16 logits with settings
+// of all kinds (65.5 MB, and 16 to 20 MB of noise): 106 us on a GB300, of which the first
+// reading 31, the cuts 12, the race 51, the lists 20.  48 rows of 100,003 float32, flat, top-p
+// 0.9: 56 us (14, 11, 24, 14).  One row of 32,000: 18 us, 22 a call.  (A block per row
+// throughout: 236, 138 and 25 us; the settling steps in the last block of each kernel
+// instead of kernels of their own: 225 and 81.)
 #include <algorithm>
 
 #include "tq_kv.cuh"
@@ -204,10 +217,25 @@ struct Shared {
   int candidates;
 };
 
-// Sorts the first n (at most LIST) places of the list, largest first; n is padded to a
-// power of two with zeros.
+// Sorts the first n (at most LIST) places of the list, largest first: few of them by
+// counting those in front of each, more by a bitonic network, n padded to a power of
+// two with zeros.  (100 places in a block of 1,024 threads: 28 steps of the network with
+// their barriers, or 100 reads of shared memory by four warps.)
 template <int N>
 __device__ void sort_list(Shared& sh, int n) {
+  if (n <= 256) {
+    static_assert(N >= 256, "a thread for each");
+    __syncthreads();
+    const uint64_t mine = threadIdx.x < n ? sh.list[threadIdx.x] : 0;
+    int front = 0;
+    if ((int)(threadIdx.x & ~31u) < n)
+#pragma unroll 4
+      for (int i = 0; i < n; ++i) front += sh.list[i] > mine;
+    __syncthreads();
+    if (threadIdx.x < n) sh.list[front] = mine;
+    __syncthreads();
+    return;
+  }
   int size = 2;
   while (size < n) size <<= 1;
   for (int i = n + threadIdx.x; i < size; i += N) sh.list[i] = 0;
@@ -409,6 +437,7 @@ struct Setting {
 __device__ __forceinline__ Setting setting_of(const SampleArgs& a, int64_t r) {
   Setting s;
   s.temperature = a.temperature ? a.temperature[r] : 1.0f;
+  if (s.temperature > 1e30f) s.temperature = 1e30f;  // (infinite: products with masked values would be NaN)
   s.top_p = a.top_p ? a.top_p[r] : 1.0f;
   s.min_p = a.min_p ? a.min_p[r] : 0.0f;
   const int k = a.top_k ? a.top_k[r] : 0;
@@ -425,8 +454,8 @@ struct Race {
   float best = 0.0f;
   uint64_t winner = 0;   // 0: none yet
 
-  // (no quotient is negative, NaN or infinite, whatever the noise)
-  static __device__ __forceinline__ float number(float e) { return fmaxf(e, 0x1p-126f); }
+  // (no quotient is negative, NaN, infinite or, for a weight above 2^-100, zero, whatever the noise)
+  static __device__ __forceinline__ float number(float e) { return fminf(fmaxf(e, 0x1p-126f), 0x1p20f); }
   // (rarely asked, and long: not inlined where a row's tokens go by)
   static __device__ __noinline__ double exact(float x, float top, float temperature) {
     return exp(((double)x - (double)top) / (double)temperature);
@@ -1146,8 +1175,9 @@ __global__ __launch_bounds__(SPLIT, 4) void k_sample_race(SplitArgs q) {
   griddep_launch_dependents();
   const Setting s = setting_of(a, r);
   if (t == 0) sh.listed = sh.candidates = 0;
-  // (one piece at a time, the next on its way: unrolled, the code is more than the SM's caches hold)
-  uint4 next = load_raw(row, g0);
+  uint4 raw[JP];
+#pragma unroll
+  for (int j = 0; j < JP; ++j) raw[j] = load_raw(row, g0 + j * SPLIT);
   griddep_wait();
   RowRecord& rec = q.rows[blockIdx.y];
   const Mode mode = rec.mode;
@@ -1159,16 +1189,19 @@ __global__ __launch_bounds__(SPLIT, 4) void k_sample_race(SplitArgs q) {
     if (to < STAGE) sh.list[to] = place_of(y, token);
   };
   if (mode == Mode::BOUND) {
-#pragma unroll 1
-    for (int j = 0; j < JP; ++j) {
-      uint4 u = next;
-      if (j + 1 < JP) next = load_raw(row, g0 + (j + 1) * SPLIT);
-      mask_nan<T>(u);
-      if (P::top(piece_top<T>(u)) >= bound) {
+    unsigned here = 0;  // pieces that have some
 #pragma unroll
-        for (int i = 0; i < E; ++i)
-          if (P::at(u, i) >= bound) append(P::at(u, i), (g0 + j * SPLIT) * E - row.lead + i);
-      }
+    for (int j = 0; j < JP; ++j) {
+      mask_nan<T>(raw[j]);
+      here |= (unsigned)(P::top(piece_top<T>(raw[j])) >= bound) << j;
+    }
+    for (; here; here &= here - 1) {  // (read again: few of them)
+      const int j = __ffs(here) - 1;
+      uint4 u = load_raw(row, g0 + j * SPLIT);
+      mask_nan<T>(u);
+#pragma unroll
+      for (int i = 0; i < E; ++i)
+        if (P::at(u, i) >= bound) append(P::at(u, i), (g0 + j * SPLIT) * E - row.lead + i);
     }
     __syncthreads();
   } else {
@@ -1181,8 +1214,9 @@ __global__ __launch_bounds__(SPLIT, 4) void k_sample_race(SplitArgs q) {
     // a product of float32's functions, 2^-17 off at most, first: its largest over the block
     // says whom to race.  A piece is weighed while the noise of the next one, which is asked
     // for where some token of it matters, and the one behind are on their way.
+    // (A piece at a time, read from L2 again: unrolled, the code is more than the SM's caches hold.)
     float above = 0.0f, most = 0.0f, e0[E], e1[E];
-    uint4 u0 = next, u1;
+    uint4 u0 = raw[0], u1, next;
     bool need0, need1 = false;
     auto ask = [&](uint4& u, int j, float (&e)[E]) {
       mask_nan<T>(u);
@@ -1191,7 +1225,7 @@ __global__ __launch_bounds__(SPLIT, 4) void k_sample_race(SplitArgs q) {
       if (need) noise_of<E>(noise, wide, (g0 + j * SPLIT) * E - row.lead, row.n, e);
       return need;
     };
-    if (JP > 1) next = load_raw(row, g0 + SPLIT);
+    next = raw[1];
     need0 = ask(u0, 0, e0);
 #pragma unroll 1
     for (int j = 0; j < JP; ++j) {
@@ -1429,9 +1463,10 @@ __global__ __launch_bounds__(ONE) void k_sample_one(SampleArgs a) {
       return;
     }
     const float bins_per = top > least_top ? (BINS - 1) / (top - least_top) : 0.0f;
+    const float reach = bins_per > 0.0f ? top - (bin + 2) / bins_per : -INFINITY;  // (a little below the bin's end)
 #pragma unroll
     for (int j = 0; j < JP; ++j)
-      if (P::top(piece_top<T>(raw[j])) > -INFINITY) {
+      if (P::top(piece_top<T>(raw[j])) >= reach && P::top(piece_top<T>(raw[j])) > -INFINITY) {
 #pragma unroll
         for (int i = 0; i < E; ++i) {
           const float x = P::at(raw[j], i);

@@ -1,5 +1,6 @@
-"""The 8-bit key-value cache of the generator behind the index, and the
-verification of its drafts: tq_kv_* and tq_verify_drafts of include/tq.h.
+"""The 8-bit key-value cache of the generator behind the index, the verification
+of its drafts and the sampling of its tokens: tq_kv_*, tq_verify_drafts and
+tq_sample of include/tq.h.
 
 A retrieved passage is prompted once, its keys and values stay in pages of
 8-bit codes (one scale for every 16 tokens and head), and each request that
@@ -12,7 +13,15 @@ retrieves it forks those pages.  One decoding step of a batch is
     tokens, accepted = tq.verify_drafts(...)           # where some were drafts
     cache.truncate(slots, lens)                        # rejected ones go
 
-with slots, counts and lengths on the device: nothing in it waits for the host,
+Where requests of a batch were forked from one passage and stand side by side,
+
+    plan = cache.share(slots, starts)                                # once a step
+    o = cache.shared_attention(layer, slots, starts, plan, q, groups)
+
+reads what they share once for all of them; `cross_attention` lets queries from
+elsewhere see all that a slot holds; `sample_tokens` draws from logits.
+
+All that with slots, counts and lengths on the device: nothing in it waits for the host,
 and the same calls can be captured into a CUDA graph.  `check()` reports what a
 call could not carry out.
 """

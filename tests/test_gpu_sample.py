@@ -116,6 +116,19 @@ def test_settings_that_are_not_numbers_keep_the_first(cuda_lib):
     assert cuda_lib.sample_tokens(x, noise, min_p=x.new_tensor([nan, 2.0, 1.0, float("inf")])).tolist() == first
 
 
+@pytest.mark.parametrize("vocab", [700, 20_000, 150_000])
+@pytest.mark.parametrize("type", ["float32", "float16"])
+def test_an_infinite_temperature(cuda_lib, vocab, type):
+    """All tokens that are not masked weigh the same."""
+    x, noise = rows(3, vocab, type, seed=24)
+    x[1, 5::7] = -float("inf")
+    x[2, : vocab - 3] = -float("inf")
+    for t in (float("inf"), 1e35, 1e30):
+        check(cuda_lib, x, noise, temperature=[t] * 3, top_p=[0.5] * 3)
+        check(cuda_lib, x, noise, temperature=[t] * 3, top_k=[9] * 3, min_p=[0.5] * 3)
+        check(cuda_lib, x, noise, temperature=[t] * 3)
+
+
 def test_values_far_apart(cuda_lib):
     """Clusters of values many powers of two apart, in denormal steps too: the search for a cut goes on in the bits."""
     torch = __import__("torch")
@@ -188,3 +201,45 @@ def test_two_graphs(cuda_lib):
         for graph, out in graphs:
             graph.replay()
             assert out.equal(want)
+
+
+@pytest.mark.parametrize("type,vocab", [("bfloat16", 65_528), ("bfloat16", 65_529), ("float32", 32_765), ("float32", 32_766),
+                                        ("float16", 2041), ("float16", 2042), ("bfloat16", 4_300_001), ("float32", 2_200_003)])
+def test_vocabularies_at_the_forms_ends(cuda_lib, type, vocab):
+    """Either side of where a row is taken by another form, and beyond the most parts of a row; rows that begin off 16 bytes."""
+    n = 3 if vocab < 10 ** 6 else 1
+    x, noise = rows(n, vocab, type, seed=vocab, likely=9, stride=1)
+    check(cuda_lib, x, noise, temperature=[0.9] * n, top_p=[0.95] * n)
+    check(cuda_lib, x, noise, top_k=[64] * n, top_p=[0.95] * n)
+
+
+@pytest.mark.parametrize("type", ["float32", "bfloat16"])
+def test_more_rows_than_a_launch_takes(cuda_lib, type):
+    """A batch gives what its parts give; its workspace serves them."""
+    torch = __import__("torch")
+    n, vocab = 530, 70_000
+    x, noise = rows(n, vocab, type, seed=21, likely=9)
+    g = torch.Generator(device="cuda").manual_seed(22)
+    p = 0.5 + 0.5 * torch.rand(n, device="cuda", generator=g)
+    k = torch.randint(0, 3, (n,), device="cuda", generator=g, dtype=torch.int32) * 30
+    from paper_2607_16973_gb300.kvcache import _sample_need
+    ws = torch.empty(_sample_need(n, vocab), dtype=torch.uint8, device="cuda")
+    tokens, logprobs = cuda_lib.sample_tokens(x, noise, top_p=p, top_k=k, workspace=ws, return_logprobs=True)
+    for a, b in ((0, 1), (1, 40), (40, 300), (300, 530)):
+        some = cuda_lib.sample_tokens(x[a:b], noise[a:b], top_p=p[a:b], top_k=k[a:b], workspace=ws, return_logprobs=True)
+        assert some[0].equal(tokens[a:b])
+        assert (some[1] - logprobs[a:b]).abs().max() <= 2.0 ** -20  # (sums in another order, and float32's rounding below 16)
+    check(cuda_lib, x[525:], noise[525:], top_p=p[525:].tolist(), top_k=k[525:].tolist())
+
+
+@pytest.mark.parametrize("vocab", [3000, 100_000])
+def test_noise_that_is_none(cuda_lib, vocab):
+    """Zeros, negative numbers, NaN and infinities are taken as the ends of what counts: here all alike."""
+    torch = __import__("torch")
+    x, noise = rows(4, vocab, seed=23)
+    noise[0] = 0.0
+    noise[1] = -1.0
+    noise[2] = float("nan")
+    noise[3] = float("inf")
+    for settings in (dict(), dict(top_p=x.new_full((4,), 0.9)), dict(top_k=torch.full((4,), 20, dtype=torch.int32, device="cuda"))):
+        assert cuda_lib.sample_tokens(x, noise, **settings).tolist() == x.argmax(1).tolist()
