@@ -401,6 +401,7 @@ __device__ __forceinline__ Both join_shared(const AttendArgs& a, int dim, int64_
 // kept): what a query that sees nothing gets.  (Asked by every block it was 1 us
 // of every call: they start where the attention's blocks end.)
 constexpr int PAD = 16;
+constexpr int FEW = 8, FEW_ROWS = 4;  // (a lane for each part of each row)
 constexpr int join_warps(int dim) { return dim == 256 ? 4 : 8; }  // (their sums take 32 KB of shared memory)
 template <typename T, int D, int ROWS>
 __global__ __launch_bounds__(join_warps(D) * 32) void k_kv_join(AttendArgs a) {
@@ -427,11 +428,88 @@ __global__ __launch_bounds__(join_warps(D) * 32) void k_kv_join(AttendArgs a) {
   }
   griddep_wait();
   const Split sp = a.splits[blockIdx.x - PAD];
-  const int row0 = blockIdx.y * 8;
-  if (sp.first < 0 || sp.row0 + row0 >= sp.rows) return;
+  if (sp.first < 0) return;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int live = min(8, sp.rows - sp.row0 - row0);
   auto part = [&](int x) { return a.parts + ((int64_t)x * 2 + (x == sp.first)) * (ROWS * (D + 2)); };
+  // A joined row's sums to the output, or to where the requests' own side finds them.
+  auto finish = [&](int row, float top, float sum, float (&y)[E]) {
+    const int64_t at = out_row(a, sp.token, sp.head, sp.row0 + row);
+    if (a.sees == KvSees::SHARED) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) a.sums[at * D + lane * E + e] = y[e];
+      if (lane == 0) {
+        *sums_m(a, D, at) = top;
+        *sums_l(a, D, at) = sum;
+      }
+      return;
+    }
+    const Both f = join_shared(a, D, at, sp.from, top, sum);
+    const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+    T* out = static_cast<T*>(a.out) + at * D + lane * E;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      if (sp.from > 0) y[e] = y[e] * f.own + a.sums[at * D + lane * E + e] * f.shared;
+      out[e] = from_float<T>(y[e] * inv);
+    }
+    if (a.lse && lane == 0) a.lse[at] = lse_of(top, sum);
+  };
+  const int n = sp.last - sp.first + 1;
+  if (n <= FEW) {
+    // Few parts: a warp joins FEW_ROWS rows by itself, in the same order.  (As below, 1,200 rows
+    // over 7 sequences took 35 us, most of it the parts' one load, a barrier and idle warps.)
+    const int first = (blockIdx.y * JOIN_WARPS + warp) * FEW_ROWS;
+    if (sp.row0 + first >= sp.rows || first >= ROWS) return;
+    const int live = min(FEW_ROWS, min(ROWS - first, sp.rows - sp.row0 - first));
+    // lane: a row's (m, l) in one of the parts
+    const int row = lane / FEW, x = lane % FEW;
+    float m = -INFINITY, l = 0.0f;
+    if (row < live && x < n) {
+      m = part(sp.first + x)[ROWS * D + first + row];
+      l = part(sp.first + x)[ROWS * (D + 1) + first + row];
+    }
+    float top = m;
+#pragma unroll
+    for (int w = 1; w < FEW; w <<= 1) top = fmaxf(top, __shfl_sync(FULL, top, lane ^ w));
+    const float f = top > -INFINITY ? ex2(m - top) : 1.0f;  // (1: sums of 0, or NaN)
+    float y[FEW_ROWS][E], sum[FEW_ROWS];
+#pragma unroll
+    for (int r = 0; r < FEW_ROWS; ++r) {
+      sum[r] = 0.0f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) y[r][e] = 0.0f;
+    }
+    for (int x = 0; x < n; ++x) {
+      const float* p = part(sp.first + x) + first * D + lane * E;
+      union {
+        Vec v[V];
+        float f[E];
+      } z[FEW_ROWS];
+#pragma unroll
+      for (int r = 0; r < FEW_ROWS; ++r)
+        if (r < live) {
+#pragma unroll
+          for (int v = 0; v < V; ++v) z[r].v[v] = *reinterpret_cast<const Vec*>(p + r * D + v * (int)(sizeof(Vec) / 4));
+        }
+#pragma unroll
+      for (int r = 0; r < FEW_ROWS; ++r) {
+        const float fr = __shfl_sync(FULL, f, r * FEW + x), lr = __shfl_sync(FULL, l, r * FEW + x);
+        sum[r] += fr * lr;
+        if (r < live) {
+#pragma unroll
+          for (int e = 0; e < E; ++e) y[r][e] += fr * z[r].f[e];
+        }
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < FEW_ROWS; ++r) {
+      const float top_r = __shfl_sync(FULL, top, r * FEW);
+      if (r < live) finish(first + r, top_r, sum[r], y[r]);
+    }
+    return;
+  }
+  const int row0 = blockIdx.y * 8;
+  if (sp.row0 + row0 >= sp.rows) return;
+  const int live = min(8, sp.rows - sp.row0 - row0);
   float o[8][E], m[8], l[8];
 #pragma unroll
   for (int r = 0; r < 8; ++r) {
@@ -488,25 +566,7 @@ __global__ __launch_bounds__(join_warps(D) * 32) void k_kv_join(AttendArgs a) {
 #pragma unroll
       for (int e = 0; e < E; ++e) y[e] += f * sh_o[x][r][lane * E + e];
     }
-    const int64_t at = out_row(a, sp.token, sp.head, sp.row0 + row0 + r);
-    if (a.sees == KvSees::SHARED) {
-#pragma unroll
-      for (int e = 0; e < E; ++e) a.sums[at * D + lane * E + e] = y[e];
-      if (lane == 0) {
-        *sums_m(a, D, at) = top;
-        *sums_l(a, D, at) = sum;
-      }
-      continue;
-    }
-    const Both f = join_shared(a, D, at, sp.from, top, sum);
-    const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
-    T* out = static_cast<T*>(a.out) + at * D + lane * E;
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      if (sp.from > 0) y[e] = y[e] * f.own + a.sums[at * D + lane * E + e] * f.shared;
-      out[e] = from_float<T>(y[e] * inv);
-    }
-    if (a.lse && lane == 0) a.lse[at] = lse_of(top, sum);
+    finish(row0 + r, top, sum, y);
   }
 }
 
