@@ -1137,8 +1137,9 @@ __device__ __noinline__ void race_again(Race& race, const Row<T>& row, bool mine
 }
 
 // The cut that lies among the listed places; front: weight in front of them, want: what
-// the cut is at, total: all weight.  0 where it does not lie among them after all (the
-// steps' weights are rounded; these are not), or cannot be told.
+// the cut is at, total: all weight.  The step was found with rounded weights, and in one
+// row of some thousands the cut lies right beside it: up to 2^-20 away it is taken at the
+// step's end.  0 where it is further off, or cannot be told.
 template <int N>
 __device__ uint64_t cut_places(const Places& places, const Weigh& weigh, uint64_t front, uint64_t want, uint64_t total,
                                Shared& sh) {
@@ -1152,7 +1153,8 @@ __device__ uint64_t cut_places(const Places& places, const Weigh& weigh, uint64_
   lo = ~block_max<N>(~lo, sh.scratch);
   hi = block_max<N>(hi, sh.scratch);
   sum = block_sum<N>(sum, sh.scratch);
-  if (front >= want || front + sum < want) return 0;
+  if (front >= want) return front - want <= want >> 20 ? ~0ull : 0;
+  if (front + sum < want) return want - (front + sum) <= want >> 20 ? lo : 0;
   return find_cut<N, false>(places, weigh, 0, front, want, 0x1p31f / ((float)total / FIXED), value_of(lo), value_of(hi), sh);
 }
 

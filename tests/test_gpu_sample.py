@@ -243,3 +243,16 @@ def test_noise_that_is_none(cuda_lib, vocab):
     noise[3] = float("inf")
     for settings in (dict(), dict(top_p=x.new_full((4,), 0.9)), dict(top_k=torch.full((4,), 20, dtype=torch.int32, device="cuda"))):
         assert cuda_lib.sample_tokens(x, noise, **settings).tolist() == x.argmax(1).tolist()
+
+
+@pytest.mark.parametrize("vocab", [20_000, 130_000])
+def test_cuts_beside_a_step(cuda_lib, vocab):
+    """Values on two levels, each with half of the weight but for some 2^-22: the cut of top-p 0.5 lies between them, closer
+    than a step's weights are rounded."""
+    torch = __import__("torch")
+    x = torch.zeros(6, vocab, device="cuda")
+    few = vocab // 50
+    for i, off in enumerate((0.0, 2.0 ** -22, -2.0 ** -22, 2.0 ** -21, -2.0 ** -21, 1e-3)):
+        x[i, :few] = float(np.log((vocab - few) / few * (1 + off)))
+    noise = rows(6, vocab, seed=31)[1]
+    check(cuda_lib, x, noise, top_p=[0.5] * 6)
