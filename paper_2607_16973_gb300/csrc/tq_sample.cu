@@ -1397,12 +1397,13 @@ __global__ __launch_bounds__(ONE) void k_sample_one(SampleArgs a) {
     atomicMin(&sh.low, (uint32_t)at);
   }
   hold(raw);
+  const Weigh plain = weigh_of(top, 1.0f);  // (to 2^-22: a lone row's log-probability shows it)
   float sum1 = 0.0f, sum = 0.0f;
 #pragma unroll
   for (int j = 0; j < JP; ++j) {
     float y[E];
 #pragma unroll
-    for (int i = 0; i < E; ++i) y[i] = ex2f((P::at(raw[j], i) - top) * LOG2E);
+    for (int i = 0; i < E; ++i) y[i] = plain(P::at(raw[j], i));
 #pragma unroll
     for (int o = 1; o < E; o <<= 1)
 #pragma unroll
