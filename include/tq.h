@@ -781,8 +781,9 @@ tq_status tq_verify_drafts(const void* target, const void* draft, int type,
  * min_p of NaN; one above 1e30 counts as 1e30. A row without a token that is not
  * masked gives token 0 and -INFINITY.
  * The answer is that of these definitions in 64 bits but for tokens whose weight, or
- * the weight in front of them, is within 2^-20 (relative) of a border, and weights
- * below 2^-126, which count as 0. n in [0, 65535], vocab in [1, 2^24].
+ * the weight in front of them, is within 2^-20 (relative; vocab * 2^-40 where that is
+ * more) of a border, and weights below 2^-126, which count as 0. n in [0, 65535],
+ * vocab in [1, 2^24].
  */
 tq_status tq_sample_workspace(int64_t n, int64_t vocab, size_t* bytes);
 tq_status tq_sample(const void* logits, int type, int64_t logits_stride,

@@ -258,10 +258,14 @@ __device__ void sort_list(Shared& sh, int n) {
 // less than `want` of the weight (in fixed point) in front of them.  The prefix has one
 // token at least; `want` is less than what all of them have.
 // front: what of them lies above `high`.  0 where more than LIST tokens of a list have one value.
+// Weights are added up as what `want` counts, to the last bit: with bins of 2^-31 of all weight,
+// 128,000 equal tokens came out 2^-16 too light, and tokens of 2^-33 as nothing.
 template <int N, bool BY_COUNT, typename Source>
 __device__ uint64_t find_cut(const Source& row, const Weigh& weigh, uint64_t kept, uint64_t front, uint64_t want,
-                             float scale, float low, float high, Shared& sh) {
+                             float low, float high, Shared& sh) {
   constexpr int E = Source::E;
+  uint32_t* more = reinterpret_cast<uint32_t*>(sh.list);  // the upper halves of the bins' weights, until the list is made
+  static_assert(BINS * sizeof(uint32_t) <= sizeof(sh.list), "room for them");
   for (int level = 0;; ++level) {
     // a histogram of the tokens with low <= x <= high: equal steps of x, then of x as an
     // ordered integer, so that every further level parts the smallest from the largest
@@ -271,85 +275,93 @@ __device__ uint64_t find_cut(const Source& row, const Weigh& weigh, uint64_t kep
     auto bin_of = [&](float x) {
       return level ? (int)((high_u - ordered(x)) >> shift) : (int)fminf((high - x) * step, (float)(BINS - 1));
     };
-    for (int i = threadIdx.x; i < BINS; i += N) sh.bins[i] = 0;
+    for (int i = threadIdx.x; i < BINS; i += N) {
+      sh.bins[i] = 0;
+      if (!BY_COUNT) more[i] = 0;
+    }
     __syncthreads();
+    int held = 0;  // a thread's tokens in a row that share a bin go there together
+    uint64_t some = 0;
+    auto put = [&] {
+      if (some == 0) return;
+      const uint32_t part = (uint32_t)some, old = atomicAdd(&sh.bins[held], part);
+      const uint32_t up = (uint32_t)(some >> 32) + (old + part < old);
+      if (!BY_COUNT && up) atomicAdd(&more[held], up);
+      some = 0;
+    };
     for (int g = threadIdx.x; g < row.pieces(); g += N) {
       float x[E];
       const int v = row.load(g, x);
 #pragma unroll
       for (int i = 0; i < E; ++i)
         if (x[i] >= low && x[i] <= high && place_of(x[i], v + i) >= kept) {
-          if (BY_COUNT)
-            atomicAdd(&sh.bins[bin_of(x[i])], 1u);
-          else
-            atomicAdd(&sh.bins[bin_of(x[i])], __float2uint_rn(weigh(x[i]) * scale));
+          const int b = bin_of(x[i]);
+          if (b != held) put();
+          held = b;
+          some += BY_COUNT ? 1 : fixed(weigh(x[i]));
         }
     }
+    put();
     __syncthreads();
     // the first bin that reaches what is wanted
-    const uint64_t rest = want > front ? want - front : 0;
-    const uint64_t need = BY_COUNT ? rest : (uint64_t)((float)rest * (scale / FIXED));
+    const uint64_t need = want > front ? want - front : 0;
+    auto bin_sum = [&](int b) { return (BY_COUNT ? 0 : (uint64_t)more[b] << 32) | sh.bins[b]; };
     uint64_t mine = 0, all;
 #pragma unroll 1
-    for (int i = 0; i < BINS / N; ++i) {
-      const int b = threadIdx.x * (BINS / N) + i;
-      mine += sh.bins[b];
+    for (int i = 0; i < BINS / N; ++i) mine += bin_sum(threadIdx.x * (BINS / N) + i);
+    if (threadIdx.x == 0) {
+      sh.bin = -1;
+      sh.taken = 0;
     }
-    if (threadIdx.x == 0) sh.bin = -1;
     uint64_t upto = block_scan<N>(mine, sh.scratch, all);
 #pragma unroll 1
     for (int i = 0; i < BINS / N; ++i) {
       const int b = threadIdx.x * (BINS / N) + i;
-      const uint64_t here = sh.bins[b];
-      if (here && upto < need && upto + here >= need) sh.bin = b;
+      const uint64_t here = bin_sum(b);
+      if (here && upto < need && upto + here >= need) {
+        sh.bin = b;
+        sh.taken = upto;
+      }
       upto += here;
     }
     __syncthreads();
     int bin = sh.bin;
-    if (bin < 0) {  // (rounded weights fall short, or nothing is needed): the last bin that has any, or the first
+    uint64_t before_bin = sh.taken;
+    if (bin < 0) {  // (sums of several weights are rounded apart, or nothing is needed): the last bin that has any, or the first
       int last = -1, first = BINS;
       for (int i = threadIdx.x; i < BINS; i += N)
-        if (sh.bins[i]) last = max(last, i), first = min(first, i);
+        if (bin_sum(i)) last = max(last, i), first = min(first, i);
       last = (int)block_max<N>((uint64_t)(last + 1), sh.scratch) - 1;
       first = BINS - (int)block_max<N>((uint64_t)(BINS - first), sh.scratch);
       bin = need ? max(last, 0) : first < BINS ? first : 0;
+      if (need) before_bin = all - bin_sum(bin);
     }
-    // its tokens to the list, their extremes; exactly what lies in front of them
+    front += before_bin;
+    // its tokens to the list, their extremes
     if (threadIdx.x == 0) {
       sh.listed = 0;
       sh.low = 0xffffffffu;
       sh.high = 0;
     }
     __syncthreads();
-    uint64_t above = 0;
     uint32_t lo = 0xffffffffu, hi = 0;
     for (int g = threadIdx.x; g < row.pieces(); g += N) {
       float x[E];
       const int v = row.load(g, x);
-      float sum = 0.0f;
 #pragma unroll
       for (int i = 0; i < E; ++i)
-        if (x[i] >= low && x[i] <= high && place_of(x[i], v + i) >= kept) {
-          const int b = bin_of(x[i]);
-          if (b < bin) {
-            if (BY_COUNT)
-              ++above;
-            else
-              sum += weigh(x[i]);
-          } else if (b == bin) {
-            const int at = atomicAdd(&sh.listed, 1);
-            if (at < LIST) sh.list[at] = place_of(x[i], v + i);
-            lo = min(lo, ordered(x[i]));
-            hi = max(hi, ordered(x[i]));
-          }
+        if (x[i] >= low && x[i] <= high && place_of(x[i], v + i) >= kept && bin_of(x[i]) == bin) {
+          const int at = atomicAdd(&sh.listed, 1);
+          if (at < LIST) sh.list[at] = place_of(x[i], v + i);
+          lo = min(lo, ordered(x[i]));
+          hi = max(hi, ordered(x[i]));
         }
-      if (!BY_COUNT) above += fixed(sum);
     }
     if (lo <= hi) {
       atomicMin(&sh.low, lo);
       atomicMax(&sh.high, hi);
     }
-    front += block_sum<N>(above, sh.scratch);
+    __syncthreads();
     const int listed = sh.listed;
     if (listed == 0) return kept;  // (nothing is kept at all)
     low = unordered(sh.low);
@@ -645,7 +657,7 @@ __device__ __noinline__ void whole_row(const SampleArgs& a, int64_t r, Shared& s
       count = block_sum<N>(count, sh.scratch);
       lo = ~(uint32_t)block_max<N>((uint64_t)~lo, sh.scratch);
       if (count > (uint64_t)s.k) {
-        kept = find_cut<N, true>(row, weigh, kept, 0, s.k, 0.0f, unordered(lo), top, sh);
+        kept = find_cut<N, true>(row, weigh, kept, 0, s.k, unordered(lo), top, sh);
         uint64_t part = 0;
         for (int g = threadIdx.x; g < row.pieces(); g += N) {
           float x[E], y = 0.0f;
@@ -661,8 +673,7 @@ __device__ __noinline__ void whole_row(const SampleArgs& a, int64_t r, Shared& s
   if (!listed && s.top_p < 1.0f) {
     const uint64_t want = part_of(s.top_p, sum);
     if (want < sum) {
-      const uint64_t cut = find_cut<N, false>(row, weigh, kept, 0, want, 0x1p31f / ((float)sum / FIXED),
-                                              least_value(s, top, sum, a.vocab), top, sh);
+      const uint64_t cut = find_cut<N, false>(row, weigh, kept, 0, want, least_value(s, top, sum, a.vocab), top, sh);
       kept = cut > kept ? cut : kept;
     }
   }
@@ -1137,12 +1148,11 @@ __device__ __noinline__ void race_again(Race& race, const Row<T>& row, bool mine
 }
 
 // The cut that lies among the listed places; front: weight in front of them, want: what
-// the cut is at, total: all weight.  The step was found with rounded weights, and in one
+// the cut is at.  The step was found with rounded weights, and in one
 // row of some thousands the cut lies right beside it: up to 2^-20 away it is taken at the
 // step's end.  0 where it is further off, or cannot be told.
 template <int N>
-__device__ uint64_t cut_places(const Places& places, const Weigh& weigh, uint64_t front, uint64_t want, uint64_t total,
-                               Shared& sh) {
+__device__ uint64_t cut_places(const Places& places, const Weigh& weigh, uint64_t front, uint64_t want, Shared& sh) {
   uint64_t lo = ~0ull, hi = 0, sum = 0;
   for (int i = threadIdx.x; i < places.n; i += N) {
     const uint64_t x = places.p[i];
@@ -1155,7 +1165,7 @@ __device__ uint64_t cut_places(const Places& places, const Weigh& weigh, uint64_
   sum = block_sum<N>(sum, sh.scratch);
   if (front >= want) return front - want <= want >> 20 ? ~0ull : 0;
   if (front + sum < want) return want - (front + sum) <= want >> 20 ? lo : 0;
-  return find_cut<N, false>(places, weigh, 0, front, want, 0x1p31f / ((float)total / FIXED), value_of(lo), value_of(hi), sh);
+  return find_cut<N, false>(places, weigh, 0, front, want, value_of(lo), value_of(hi), sh);
 }
 
 constexpr int STAGE = 1024;  // places that a block brings to the list at most
@@ -1307,7 +1317,7 @@ __global__ __launch_bounds__(SPLIT) void k_sample_finish(SplitArgs q) {
     }
     if (listed) {
       const uint64_t want = part_of(s.top_p, rec.sum), front = block_sum<SPLIT>(fixed(w.above), sh.scratch);
-      const uint64_t cut = cut_places<SPLIT>({list, listed}, weigh, front, want, rec.sum, sh);
+      const uint64_t cut = cut_places<SPLIT>({list, listed}, weigh, front, want, sh);
       if (cut == 0) {  // (uniform)
         whole_row<SPLIT, T>(a, r, sh);
         return;
@@ -1541,7 +1551,7 @@ __global__ __launch_bounds__(ONE) void k_sample_one(SampleArgs a) {
     const int listed = sh.listed;
     if (listed) {
       const uint64_t front = fixed(warp_sum(one.sums[0][lane]));
-      const uint64_t at = listed <= LIST ? cut_places<ONE>({one.places, listed}, weigh, front, want, total, sh) : 0;
+      const uint64_t at = listed <= LIST ? cut_places<ONE>({one.places, listed}, weigh, front, want, sh) : 0;
       if (at == 0) {  // (uniform)
         __syncthreads();
         whole_row<ONE, T>(a, r, sh);
