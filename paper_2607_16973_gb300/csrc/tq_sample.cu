@@ -717,7 +717,9 @@ __global__ __launch_bounds__(N) void k_sample_row(SampleArgs a) {
 constexpr int SPLIT = 256;
 constexpr int GROUP = 64;              // tokens
 constexpr int STEPS = 1024;            // of 1/32: weights down to e^-32 of a part's largest
-constexpr float STEP_ONE = 524288.0f;  // weight at a step's upper end, as an integer: 2^13 of them fit
+// The weight at a step's upper end as an integer: a part of `tokens` brings 2^31 at most, even
+// where all of them lie at one step's end, so no step wraps; and 2^22 at most, what ROUND holds.
+constexpr float unit_of(int tokens) { return (float)((1u << 31) / tokens); }
 constexpr float ROUND = 12582912.0f;   // 1.5 * 2^23: what is added to it is rounded to an integer, in its low bits
 constexpr float MOST_STEP = 1e6f;      // steps' numbers up to which that holds, and leaves bits behind the point
 constexpr int MOST_K = 512, MOST_LISTED = 4096, MOST_PARTS = SPLIT;
@@ -876,8 +878,8 @@ __device__ __forceinline__ void block_sums(float& x, float& y, Scratch& s) {
   }
 }
 
-// The row's record; groups: of a part.  A block per row.
-__global__ __launch_bounds__(SPLIT) void k_sample_cut(SplitArgs q, int groups_of_part) {
+// The row's record; groups: of a part; unit: of its steps' weights.  A block per row.
+__global__ __launch_bounds__(SPLIT) void k_sample_cut(SplitArgs q, int groups_of_part, float unit) {
   __shared__ Shared sh;
   const SampleArgs& a = q.a;
   const int64_t r = q.row0 + blockIdx.x, block0 = blockIdx.x * (int64_t)q.parts;
@@ -985,7 +987,7 @@ __global__ __launch_bounds__(SPLIT) void k_sample_cut(SplitArgs q, int groups_of
     for (int i = 0; i < 4; ++i) {
       // the weight at the step's upper end: about 1 in the largest's own step
       const float up = ((float)(highest - at - i) + 0.5f - top * per) * (1.0f / 32.0f);
-      w[i] = (uint64_t)((float)w[i] * (FIXED / STEP_ONE) * ex2f(up * LOG2E));
+      w[i] = (uint64_t)((float)w[i] * (FIXED / unit) * ex2f(up * LOG2E));
       some += w[i];
     }
     const uint64_t want = part_of(s.top_p, sum);
@@ -1017,6 +1019,8 @@ template <typename T, int JP>
 __global__ __launch_bounds__(SPLIT, 4) void k_sample_parts(SplitArgs q) {
   using P = Packed<T>;
   constexpr int E = Row<T>::E, LANES = GROUP / (JP * E);  // of a group
+  constexpr float UNIT = unit_of(SPLIT * JP * E);
+  static_assert(UNIT >= 0x1p16f && UNIT <= 0x1p22f, "weights to 2^-17, sums to 2^31");
   __shared__ struct {
     uint32_t bins[STEPS];
     Scratch scratch;
@@ -1097,7 +1101,7 @@ __global__ __launch_bounds__(SPLIT, 4) void k_sample_parts(SplitArgs q) {
           if (x >= least && steps) {
             const int step = step_of(x, per), slot = highest - step;
             const float up = (__fmul_rn(x, per) - ((float)step + 0.5f)) * (LOG2E / 32.0f);
-            const uint32_t w = __float_as_uint(fmaf(ex2f(up), STEP_ONE, ROUND)) - __float_as_uint(ROUND);
+            const uint32_t w = __float_as_uint(fmaf(ex2f(up), UNIT, ROUND)) - __float_as_uint(ROUND);
             if (slot < STEPS) atomicAdd(&sh.bins[slot], w);
           }
         }
@@ -1337,7 +1341,6 @@ __global__ __launch_bounds__(SPLIT) void k_sample_finish(SplitArgs q) {
 //
 // The four kernels' steps in one: no round trip over memory in between.
 constexpr int ONE = 1024;
-constexpr float ONE_UNIT = 32768.0f;  // as STEP_ONE: 2^16 of them fit
 struct OneShared {
   Shared sh;
   uint64_t places[LIST];
@@ -1349,6 +1352,8 @@ template <typename T, int JP>
 __global__ __launch_bounds__(ONE) void k_sample_one(SampleArgs a) {
   using P = Packed<T>;
   constexpr int E = Row<T>::E;
+  constexpr float UNIT = unit_of(ONE * JP * E);
+  static_assert(UNIT >= 0x1p15f && UNIT <= 0x1p22f, "weights to 2^-16, sums to 2^31");
   extern __shared__ unsigned char raw_smem[];
   OneShared& one = *reinterpret_cast<OneShared*>(raw_smem);
   Shared& sh = one.sh;
@@ -1435,7 +1440,7 @@ __global__ __launch_bounds__(ONE) void k_sample_one(SampleArgs a) {
           y += ex2f((x - top) * c);
           const int step = step_of(x, per), slot = highest - step;
           const float up = (__fmul_rn(x, per) - ((float)step + 0.5f)) * (LOG2E / 32.0f);
-          const uint32_t w = __float_as_uint(fmaf(ex2f(up), ONE_UNIT, ROUND)) - __float_as_uint(ROUND);
+          const uint32_t w = __float_as_uint(fmaf(ex2f(up), UNIT, ROUND)) - __float_as_uint(ROUND);
           if (slot < STEPS) atomicAdd(&one.steps[slot], w);
         }
       }
@@ -1505,7 +1510,7 @@ __global__ __launch_bounds__(ONE) void k_sample_one(SampleArgs a) {
     const uint64_t want = cut ? part_of(s.top_p, total) : 0;
     if (cut) {
       const float up = ((float)(highest - t) + 0.5f - top * per) * (1.0f / 32.0f);
-      const uint64_t w = (uint64_t)((float)one.steps[t] * (FIXED / ONE_UNIT) * ex2f(up * LOG2E));
+      const uint64_t w = (uint64_t)((float)one.steps[t] * (FIXED / UNIT) * ex2f(up * LOG2E));
       uint64_t all;
       const uint64_t upto = block_scan<ONE>(w, sh.scratch, all);
       if (w && upto < want && upto + w >= want) sh.bin = t;
@@ -1633,7 +1638,8 @@ cudaError_t sample(const SampleArgs& a, int64_t n, void* workspace, cudaStream_t
     const dim3 grid((unsigned)parts, (unsigned)std::min(rows, n - q.row0)), per_row(grid.y), block(SPLIT);
     (few ? k_sample_parts<T, 2> : k_sample_parts<T, 8>)<<<grid, block, 0, s>>>(q);
     cudaError_t e = cudaGetLastError();
-    if (e == cudaSuccess) e = launch_maybe_pdl(true, k_sample_cut, per_row, block, 0, s, q, SPLIT * jp * E / GROUP);
+    if (e == cudaSuccess)
+      e = launch_maybe_pdl(true, k_sample_cut, per_row, block, 0, s, q, SPLIT * jp * E / GROUP, unit_of(SPLIT * jp * E));
     if (e == cudaSuccess) e = launch_maybe_pdl(true, few ? k_sample_race<T, 2> : k_sample_race<T, 8>, grid, block, 0, s, q);
     if (e == cudaSuccess) e = launch_maybe_pdl(true, k_sample_finish<T>, per_row, block, 0, s, q);
     if (e != cudaSuccess) return e;

@@ -1,0 +1,64 @@
+"""tq_sample on batches of as many rows as take the longest parts, and rows whose weight
+lies close together, against its definition in 64 bits."""
+import numpy as np
+import pytest
+
+from sampleref import sample
+from test_gpu_sample import SLACK, rows
+
+pytestmark = pytest.mark.gpu
+
+
+def check(tq, logits, noise, picked=None, **settings):
+    """As test_gpu_sample.check, for the rows `picked` of one call's answers."""
+    torch = __import__("torch")
+    kinds = {"temperature": torch.float32, "top_k": torch.int32, "top_p": torch.float32, "min_p": torch.float32}
+    given = {name: torch.tensor(x, dtype=kinds[name], device="cuda") for name, x in settings.items()}
+    tokens, logprobs = tq.sample_tokens(logits, noise, **given, return_logprobs=True)
+    values = {name: t.double().cpu().tolist() for name, t in given.items()}
+    for i in range(logits.shape[0]) if picked is None else picked:
+        s = {name: (int(v[i]) if name == "top_k" else v[i]) for name, v in values.items()}
+        x, e = logits[i].double().cpu().numpy(), noise[i].double().cpu().numpy()
+        want = [sample(x, e, **s, slack=slack) for slack in (0.0, SLACK, -SLACK)]
+        token, logprob = int(tokens[i]), float(logprobs[i])
+        assert token in [t for t, _ in want], (i, s, token, want)
+        ref = dict(want)[token]
+        assert logprob == ref or abs(logprob - ref) <= 2.0 ** -24 * abs(ref) + 2.0 ** -21, (i, s, logprob, ref)
+    return tokens
+
+
+def favour(logits, noise, temperature, top_p, behind):
+    """Noise that lets a token a little in front of the cut win, or one a little behind it that must not."""
+    torch = __import__("torch")
+    for i in range(logits.shape[0]):
+        x = logits[i].double()
+        order = torch.argsort(x, descending=True, stable=True)
+        w = torch.exp((x[order] - x[order[0]]) / temperature[i])
+        count = int((w.cumsum(0) - w < top_p[i] * w.sum()).sum())
+        at = min(len(order) - 1, count + len(order) // 1000) if behind[i] else max(0, count - 1 - len(order) // 1000)
+        noise[i, order[at]] = 2.0 ** -60
+
+
+@pytest.mark.parametrize("type,vocab", [("bfloat16", 128_000), ("float16", 128_000), ("float32", 100_003), ("float32", 128_000)])
+def test_rows_whose_weight_lies_in_few_steps(cuda_lib, type, vocab):
+    """Equal logits, all of them at a step's upper end, a small spread, high temperatures: a part's tokens all in a few of the
+    steps that the cut of top-p is found by."""
+    torch = __import__("torch")
+    n = 64
+    logits, noise = rows(n, vocab, type, seed=vocab, spread=1.0)
+    temperature, top_p, behind = [], [], []
+    for i in range(n):
+        kind = i % 6
+        if kind == 0:
+            logits[i] = 0.0
+        elif kind == 1:
+            logits[i] = 1 / 64
+        elif kind < 4:
+            logits[i] *= 0.01 * (kind - 1)
+        else:
+            logits[i] *= 2
+        temperature.append((1.0, 1.0, 1.0, 1.0, 100.0, float("inf"))[kind])
+        top_p.append((0.5, 0.9, 0.99999)[i // 6 % 3])
+        behind.append(i // 18 % 2 == 0)
+    favour(logits, noise, temperature, top_p, behind)
+    check(cuda_lib, logits, noise, picked=range(42), temperature=temperature, top_p=top_p)
