@@ -732,7 +732,7 @@ struct RowRecord {
   uint64_t first, sum1, sum;
   Mode mode;
   float bound;          // BOUND: the list's least value.  CUT: nothing below it is kept or listed
-  int step;             // CUT: the list's step; what lies above it is kept, what lies below is not
+  int step;             // CUT: the list's step; what lies above it is kept, what lies below is not.  INT_MIN: no cut
   unsigned listed;      // (0 until the race)
 };
 struct PartRecord {
@@ -999,7 +999,7 @@ __global__ __launch_bounds__(SPLIT) void k_sample_cut(SplitArgs q, int groups_of
       upto += w[i];
     }
     __syncthreads();
-    // (none: all but what is e^-32 of the largest, or the parts' sums rounded apart)
+    // (none: all but what is e^-32 of the largest, or the sums rounded apart, or a part without steps)
     step = highest - (sh.listed < 0 ? STEPS - 1 : sh.listed);
     bound = ((float)step - 0.51f) / per;
     bound -= fabsf(bound) * 0x1p-21f;
@@ -1151,10 +1151,10 @@ __device__ __noinline__ void race_again(Race& race, const Row<T>& row, bool mine
   }
 }
 
-// The cut that lies among the listed places; front: weight in front of them, want: what
-// the cut is at.  The step was found with rounded weights, and in one
-// row of some thousands the cut lies right beside it: up to 2^-20 away it is taken at the
-// step's end.  0 where it is further off, or cannot be told.
+// The cut that lies among the listed places (there may be none); front: weight in front of
+// them, want: what the cut is at.  The step was found with rounded weights, or none was, and
+// in one row of some thousands the cut lies right beside it: up to 2^-20 away it is taken at
+// the step's end.  0 where it is further off, or cannot be told: no step is trusted unseen.
 template <int N>
 __device__ uint64_t cut_places(const Places& places, const Weigh& weigh, uint64_t front, uint64_t want, Shared& sh) {
   uint64_t lo = ~0ull, hi = 0, sum = 0;
@@ -1319,7 +1319,7 @@ __global__ __launch_bounds__(SPLIT) void k_sample_finish(SplitArgs q) {
       race.best = w.best;
       race.winner = w.place;
     }
-    if (listed) {
+    if (rec.step != INT_MIN) {
       const uint64_t want = part_of(s.top_p, rec.sum), front = block_sum<SPLIT>(fixed(w.above), sh.scratch);
       const uint64_t cut = cut_places<SPLIT>({list, listed}, weigh, front, want, sh);
       if (cut == 0) {  // (uniform)
@@ -1554,7 +1554,7 @@ __global__ __launch_bounds__(ONE) void k_sample_one(SampleArgs a) {
     const bool ahead = most > 0.0f && most >= high_q * (1.0f - 0x1p-15f);
     if (__any_sync(FULL, ahead)) race_again<T, JP, ONE>(race, row, ahead, t, bound, step, per, c, high_q);
     const int listed = sh.listed;
-    if (listed) {
+    if (cut) {
       const uint64_t front = fixed(warp_sum(one.sums[0][lane]));
       const uint64_t at = listed <= LIST ? cut_places<ONE>({one.places, listed}, weigh, front, want, sh) : 0;
       if (at == 0) {  // (uniform)
