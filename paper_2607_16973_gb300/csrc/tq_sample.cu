@@ -14,7 +14,7 @@
 // threads bound the k-th value from below, and what lies above that bound is sorted at
 // once, cut, and raced.
 //
-// Quotients are taken in float32; those within 2^-18 of the largest are compared again
+// Quotients are taken in float32; those within 2^-16 of the largest are compared again
 // in 64 bits, so that the token is that of exact arithmetic.
 //
 // Three forms.  Rows of up to 256 pieces of 16 bytes, and rows beyond 256 parts, by a block
@@ -77,8 +77,9 @@ __device__ __forceinline__ uint64_t place_of(float x, int v) { return (uint64_t)
 __device__ __forceinline__ int token_of(uint64_t place) { return (int)~(uint32_t)place; }
 __device__ __forceinline__ float value_of(uint64_t place) { return unordered((uint32_t)(place >> 32)); }
 
-// Weight of a value: 2^((x - top) * (c_hi + c_lo)), about 2^-22 off; 0 below 2^-126 (and
-// for masked values, whatever the temperature).
+// Weight of a value: 2^((x - top) * (c_hi + c_lo)), about 2^-22 off, and for float32 values by
+// the rounding of x - top, which is 2^-24 of an exponent of up to 88: 2^-17.5.  0 below 2^-126
+// (and for masked values, whatever the temperature).
 struct Weigh {
   float top, hi, lo;
   __device__ __forceinline__ float operator()(float x) const {
@@ -438,8 +439,12 @@ __device__ uint64_t find_cut(const Source& row, const Weigh& weigh, uint64_t kep
   }
 }
 
-// The race among kept tokens: quotients in float32, those next to the best in 64 bits.
-constexpr float NEAR = 1.0f - 0x1p-18f;
+// The race among kept tokens: quotients in float32, those next to the best in 64 bits.  NEAR
+// holds two quotients' errors, each 2^-17.4 at most (the weight's, and the division's).
+constexpr float NEAR = 1.0f - 0x1p-16f;
+// The same for weights of one product, ex2f((x - top) * c): the difference, c and the product
+// are each 2^-24 off, of an exponent of up to 88, so the weight is by 2^-15.9 at most.
+constexpr float ABOUT = 0x1p-15f, NEAR_ABOUT = 1.0f - 0x1p-14f;
 
 struct Setting {
   float temperature, top_p, min_p;
@@ -485,8 +490,8 @@ struct Race {
   __device__ __forceinline__ void enter(float x, int v, float w) { enter(x, v, w, noise[v]); }
   // Whether min-p lets a token of about weight w race: in 64 bits next to its border.
   __device__ __forceinline__ bool keeps(float x, float w) const {
-    if (w > s.min_p * (1.0f + 0x1p-18f)) return true;
-    return w > 0.0f && w >= s.min_p * (1.0f - 0x1p-18f) && weight(x) >= (double)s.min_p;
+    if (w > s.min_p * (1.0f + ABOUT)) return true;
+    return w > 0.0f && w >= s.min_p * (1.0f - ABOUT) && weight(x) >= (double)s.min_p;
   }
   __device__ __forceinline__ void enter(float x, int v, float w, float e) {
     const uint64_t place = place_of(x, v);
@@ -1146,7 +1151,7 @@ __device__ __noinline__ void race_again(Race& race, const Row<T>& row, bool mine
       const float x = fmaxf(to_float(row.p[v]), -INFINITY);
       if (!(x >= bound) || x == -INFINITY || (step != INT_MIN && step_of(x, per) <= step)) continue;
       const float w = ex2f((x - race.weigh.top) * c), e = race.noise[v];
-      if (__fdividef(w, Race::number(e)) >= high * (1.0f - 0x1p-15f)) race.enter(x, v, race.weigh(x), e);
+      if (__fdividef(w, Race::number(e)) >= high * NEAR_ABOUT) race.enter(x, v, race.weigh(x), e);
     }
   }
 }
@@ -1227,8 +1232,8 @@ __global__ __launch_bounds__(SPLIT, 4) void k_sample_race(SplitArgs q) {
     const float* noise = a.noise + r * a.noise_stride;
     const bool wide = ((uintptr_t)(noise - row.lead) & 15) == 0;
     Race race = {s, weigh, noise, rec.first};
-    // a product of float32's functions, 2^-17 off at most, first: its largest over the block
-    // says whom to race.  A piece is weighed while the noise of the next one, which is asked
+    // weights of one product first (ABOUT): their largest quotient over the block says whom to
+    // race.  A piece is weighed while the noise of the next one, which is asked
     // for where some token of it matters, and the one behind are on their way.
     // (A piece at a time, read from L2 again: unrolled, the code is more than the SM's caches hold.)
     float above = 0.0f, most = 0.0f, e0[E], e1[E];
@@ -1268,14 +1273,15 @@ __global__ __launch_bounds__(SPLIT, 4) void k_sample_race(SplitArgs q) {
       for (int i = 0; i < E; ++i) e0[i] = e1[i];
     }
     const float high = block_most(most, above, sh.scratch);  // (and the sum of the weights)
-    const bool mine = most > 0.0f && most >= high * (1.0f - 0x1p-15f);
+    const bool mine = most > 0.0f && most >= high * NEAR_ABOUT;
     if (__any_sync(FULL, mine)) race_again<T, JP, SPLIT>(race, row, mine, g0, bound, step, per, c, high);
     if (race.winner) sh.place[atomicAdd(&sh.candidates, 1)] = race.winner;
     __syncthreads();
     if (t == 0) {
       uint64_t w = sh.candidates ? sh.place[0] : 0;
       for (int i = 1; i < sh.candidates; ++i) w = race.better(w, sh.place[i]);
-      q.winner[block] = {w, high, above};
+      // (its quotient as k_sample_finish takes the list's: `high` is not near enough)
+      q.winner[block] = {w, w ? race.weigh(value_of(w)) / Race::number(noise[token_of(w)]) : 0.0f, above};
     }
   }
   // the list, behind what other blocks bring
@@ -1551,7 +1557,7 @@ __global__ __launch_bounds__(ONE) void k_sample_one(SampleArgs a) {
     }
     __syncthreads();
     const float high_q = __uint_as_float(__reduce_max_sync(FULL, __float_as_uint(one.most[lane])));
-    const bool ahead = most > 0.0f && most >= high_q * (1.0f - 0x1p-15f);
+    const bool ahead = most > 0.0f && most >= high_q * NEAR_ABOUT;
     if (__any_sync(FULL, ahead)) race_again<T, JP, ONE>(race, row, ahead, t, bound, step, per, c, high_q);
     const int listed = sh.listed;
     if (cut) {

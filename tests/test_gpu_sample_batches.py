@@ -62,3 +62,54 @@ def test_rows_whose_weight_lies_in_few_steps(cuda_lib, type, vocab):
         behind.append(i // 18 % 2 == 0)
     favour(logits, noise, temperature, top_p, behind)
     check(cuda_lib, logits, noise, picked=range(42), temperature=temperature, top_p=top_p)
+
+
+@pytest.mark.parametrize("n,vocab", [(64, 100_003), (64, 20_000), (64, 900)])
+@pytest.mark.parametrize("temperature", [1.0, 1.3])
+def test_near_ties_of_tokens_far_below_the_first(cuda_lib, n, vocab, temperature):
+    """Two tokens of 2^-60 to 2^-110 whose noise makes their quotients alike to 2^-19, in different parts of the row: the one
+    that is ahead in 64 bits."""
+    torch = __import__("torch")
+    rng = np.random.default_rng(vocab)
+    logits, noise = rows(n, vocab, seed=vocab, spread=1.0)
+    noise.fill_(1.0)
+    x, e = logits.cpu().numpy(), noise.cpu().numpy()
+    want = []
+    for i in range(n):
+        a, b = (int(v) for v in rng.choice(vocab // 2 - 1, 2) + [0, vocab // 2])
+        x[i, [a, b]] = -rng.uniform(60, 110, 2) * np.log(2.0) * temperature
+        top = x[i].astype(np.float64).max()
+        w = np.exp((x[i, [a, b]].astype(np.float64) - top) / float(np.float32(temperature)))
+        e[i, [a, b]] = w * 2.0 ** -10 * [1, 1 + rng.choice([-1, 1]) * 2.0 ** -19]
+        want.append((a, b)[int(np.argmax(w / e[i, [a, b]].astype(np.float64)))])
+    logits.copy_(torch.from_numpy(x))
+    noise.copy_(torch.from_numpy(e))
+    t = torch.full((n,), temperature, device="cuda")
+    assert cuda_lib.sample_tokens(logits, noise, temperature=t).tolist() == want
+    assert cuda_lib.sample_tokens(logits, noise, temperature=t, min_p=torch.full((n,), 2.0 ** -125, device="cuda")).tolist() == want
+
+
+def test_a_border_of_min_p_far_below_the_first(cuda_lib):
+    """Tokens of 2^-100, some 2^-17 in front of min-p's border and some behind, with noise that lets them win: those in front
+    do, as if the others were not there."""
+    torch = __import__("torch")
+    n, vocab, temperature = 64, 100_003, 1.3
+    rng = np.random.default_rng(3)
+    logits, noise = rows(n, vocab, seed=3, spread=1.0)
+    noise.fill_(1.0)
+    x, e = logits.cpu().numpy(), noise.cpu().numpy()
+    min_p, want = np.empty(n, np.float32), []
+    for i in range(n):
+        a, b = (int(v) for v in rng.choice(vocab, 2, replace=False))
+        x[i, a] = -rng.uniform(90, 110) * np.log(2.0) * temperature
+        x[i, b] = np.nextafter(x[i, a], np.float32(-np.inf))
+        top = x[i].astype(np.float64).max()
+        w = np.exp((x[i, [a, b]].astype(np.float64) - top) / float(np.float32(temperature)))
+        min_p[i] = np.sqrt(w[0] * w[1])
+        assert w[0] > min_p[i] * (1 + 2.0 ** -20) and w[1] < min_p[i] * (1 - 2.0 ** -20)
+        e[i, a], e[i, b] = w[0] * 2.0 ** -10, w[1] * 2.0 ** -14
+        want.append(a)
+    logits.copy_(torch.from_numpy(x))
+    noise.copy_(torch.from_numpy(e))
+    t = torch.full((n,), temperature, device="cuda")
+    assert cuda_lib.sample_tokens(logits, noise, temperature=t, min_p=torch.from_numpy(min_p).cuda()).tolist() == want
