@@ -100,11 +100,22 @@ __device__ __forceinline__ Weigh weigh_of(float top, float temperature) {
 }
 __device__ __forceinline__ uint64_t fixed(float w) { return __float2ull_rn(w * FIXED); }
 
-// The least integer that is not below p * x, for p in (0, 1) and x below 2^63 (p to 2^-32):
-// 1 at least.
+// The least integer that is not below p * x, for p in (0, 1) and x of up to 2^63: 1 at least.
 __device__ __forceinline__ uint64_t part_of(float p, uint64_t x) {
-  const uint64_t m = (uint64_t)(uint32_t)__float2uint_rn(p * 4294967296.0f) << 32;
-  return max(1ull, (unsigned long long)(__umul64hi(x, m) + (x * m != 0)));
+  // p = m / 2^shift, the product hi * 2^64 + lo
+  const uint32_t u = __float_as_uint(p);
+  const uint64_t m = (u & 0x7fffffu) | (u >> 23 ? 0x800000u : 0u);
+  const int shift = 150 - max((int)(u >> 23), 1);  // 24 to 149
+  const uint64_t hi = __umul64hi(x, m), lo = x * m;
+  uint64_t whole, rest;
+  if (shift < 64) {
+    whole = hi << (64 - shift) | lo >> shift;
+    rest = lo << (64 - shift);
+  } else {
+    whole = shift == 64 ? hi : hi >> (shift - 64 < 63 ? shift - 64 : 63);  // (hi is below 2^24)
+    rest = 1;
+  }
+  return max(1ull, (unsigned long long)(whole + (rest != 0)));
 }
 // Logarithm of x / 2^39, x > 0: about 2^-25 off.
 __device__ __forceinline__ double log_fixed(uint64_t x) {

@@ -95,3 +95,15 @@ def test_values_on_either_side_of_where_steps_have_numbers(cuda_lib, vocab):
     noise[0, 9400] = noise[1, 9800] = 2.0 ** -60
     tokens = check(cuda_lib, logits, noise, temperature=[1e-3] * 2, top_p=[0.5] * 2)
     assert int(tokens[0]) == 9400 and int(tokens[1]) < 9500
+
+
+@pytest.mark.parametrize("place", [10, 300, 70_000])
+def test_a_small_top_p_of_many_tokens(cuda_lib, place):
+    """top-p a few float32 steps below what `place` of 10^6 equal tokens have: the one behind them stays out."""
+    vocab = 1_000_000
+    top_p = np.float32(place * (1 - 4e-6) / vocab)
+    assert place - 1 < float(top_p) * vocab < place * (1 - 2.0 ** -19)
+    logits, noise = row(vocab)
+    noise[0, place - 1] = noise[1, place] = 2.0 ** -60
+    tokens = check(cuda_lib, logits, noise, top_p=[float(top_p)] * 2)
+    assert int(tokens[0]) == place - 1 and int(tokens[1]) == 0
