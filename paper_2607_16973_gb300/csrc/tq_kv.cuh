@@ -36,9 +36,8 @@ __device__ __forceinline__ int64_t warp_last_not_above(int64_t n, int64_t x, F a
 
 // Sequence i of a call that brings tokens starts[i] .. starts[i+1] - 1 (its last
 // ones): false, with the status set, where the entry cannot be carried out.
-// Its tokens are seen from `from` on.
 struct KvSeq {
-  int slot, token, len, count, from;
+  int slot, token, len, count;
 };
 __device__ __forceinline__ bool kv_seq(const KvView& kv, const int32_t* __restrict__ slots,
                                        const int32_t* __restrict__ starts, int64_t i, int64_t total, bool clip,
@@ -47,7 +46,7 @@ __device__ __forceinline__ bool kv_seq(const KvView& kv, const int32_t* __restri
   q.slot = slots[i];
   q.token = a;
   q.count = b - a;
-  q.len = q.from = 0;
+  q.len = 0;
   if (a < 0 || b < a || b > total || q.slot < 0 || q.slot >= kv.c.slots) return false;
   q.len = kv.c.lens[q.slot];
   return q.len >= 0 && q.len <= kv.max_len && (clip || q.len >= q.count);

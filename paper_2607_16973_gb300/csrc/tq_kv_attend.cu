@@ -57,8 +57,8 @@ constexpr int AHEAD = 1;         // blocks of a warp on their way to L2 beyond t
 // over 1,031 tokens, 4: 11.6, 8: 12.8), and an item costs about as much as 16
 // beside its own: looking it up, its queries, its sums (128 ragged sequences: 138 us
 // counted as 4, 124 as 8, 114 as 16 to 32, 116 as 48).
-template <int NT>
-using StreamCut = Cut<8 * NT, kKvBlock, 16, 4>;
+template <int NT, bool CAUSAL>
+using StreamCut = Cut<8 * NT, kKvBlock, 16, 4, CAUSAL>;
 
 // Two pairs of fp16 values from the four codes of a word: every code is exact.
 template <int CODES>
@@ -109,13 +109,13 @@ struct Piece {  // what a lane loads of a row: K pieces of 16 bytes, V pieces of
 // Blocks of threads per SM, by the registers that the accumulators leave.
 constexpr int per_sm(int dim, int nt) { return dim == 256 ? 2 : nt == 1 ? 4 : 3; }
 
-template <typename T, int D, int CODES, int NT>
+template <typename T, int D, int CODES, int NT, bool CAUSAL>
 __global__ __launch_bounds__(THREADS, per_sm(D, NT)) void k_kv_attend(AttendArgs a) {
-  using P = StreamCut<NT>;
+  using P = StreamCut<NT, CAUSAL>;
   constexpr int ROWS = P::ROWS;
   constexpr int KP = Piece<D>::K, VP = Piece<D>::V, VW = Piece<D>::VW;
   constexpr int MT = D / 16;  // m-tiles of O^T
-  __shared__ Units units;
+  __shared__ UnitsOf<CAUSAL> units;
   __shared__ Run run;
   __shared__ alignas(16) float sh_o[WARPS][ROWS][D + 4];  // (read two at a time)
   __shared__ float sh_m[WARPS][ROWS], sh_l[WARPS][ROWS];
@@ -129,6 +129,7 @@ __global__ __launch_bounds__(THREADS, per_sm(D, NT)) void k_kv_attend(AttendArgs
     next_segment<P>(a, units, run);
     const KvSeq sq = run.seg.it.s;
     const Span span = run.seg.it.span;
+    const int from = CAUSAL ? 0 : run.seg.it.from;
     const int head = run.seg.it.head, row0 = run.seg.row0, rows = run.seg.rows;
 
     if (run.seg.b_first == run.seg.b_last) {  // no row sees a token
@@ -190,13 +191,13 @@ __global__ __launch_bounds__(THREADS, per_sm(D, NT)) void k_kv_attend(AttendArgs
       for (int h = 0; h < 2; ++h) {
         unscale[nt][h] = __shfl_sync(FULL, down, (2 * t + h) * 4);
         const int r = row0 + nt * 8 + 2 * t + h;
-        place[nt][h] = r < rows ? max(-1, dense(a) ? sq.len - 1 : sq.len - sq.count + r / a.group) : -1;
+        place[nt][h] = r < rows ? max(-1, dense<P>(a) ? sq.len - 1 : sq.len - sq.count + r / a.group) : -1;
       }
     }
     const int blk = span.first + run.seg.b_first, blk_end = span.first + run.seg.b_last;
     // blocks that every row of the tile sees whole
-    const int whole_from = max((sq.from + kKvBlock - 1) / kKvBlock,
-                               a.window && span.place_hi >= a.window ? (span.place_hi - a.window) / kKvBlock + 1 : 0);
+    const int whole_from = !CAUSAL ? (from + kKvBlock - 1) / kKvBlock
+                           : a.window && span.place_hi >= a.window ? (span.place_hi - a.window) / kKvBlock + 1 : 0;
     const int whole_to = span.place_lo >= 0 ? (span.place_lo + 1) / kKvBlock : 0;
 
     float o[NT][MT][4], m[NT][2], l[NT][2];
@@ -320,7 +321,7 @@ __global__ __launch_bounds__(THREADS, per_sm(D, NT)) void k_kv_attend(AttendArgs
             float y = s[nt][x] * (k_scale * unscale[nt][h]);
             if (!whole) {
               const int tok = b * kKvBlock + g + (x >> 1) * 8;
-              if (tok > place[nt][h] || tok < sq.from || (a.window && tok <= place[nt][h] - a.window)) y = -INFINITY;
+              if (tok > place[nt][h] || (!CAUSAL ? tok < from : a.window && tok <= place[nt][h] - a.window)) y = -INFINITY;
             }
             s[nt][x] = y;
             rise |= y > m[nt][h] + (LEAD + LAZY);
@@ -426,9 +427,9 @@ __global__ __launch_bounds__(THREADS, per_sm(D, NT)) void k_kv_attend(AttendArgs
         sum += f[x] * sh_l[x][row];
       }
       const int64_t at = out_row(a, done.it.s.token, done.it.head, done.row0 + row);
-      const bool sums = a.sees == KvSees::SHARED;
-      const int from = done.whole ? done.it.s.from : 0;
-      const Both both = join_shared(a, D, at, from, top, sum);
+      const bool sums = !CAUSAL && a.sees == KvSees::SHARED;
+      const int joined = !CAUSAL && done.whole ? done.it.from : 0;
+      const Both both = join_shared(a, D, at, joined, top, sum);
       const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
       for (int d = lane * 2; d < D; d += 64) {
         float y0 = 0.0f, y1 = 0.0f;
@@ -441,7 +442,7 @@ __global__ __launch_bounds__(THREADS, per_sm(D, NT)) void k_kv_attend(AttendArgs
         if (done.whole && sums) {
           *reinterpret_cast<float2*>(a.sums + at * D + d) = make_float2(y0, y1);
         } else if (done.whole) {
-          if (from > 0) {
+          if (joined > 0) {
             const float2 z = *reinterpret_cast<const float2*>(a.sums + at * D + d);
             y0 = y0 * both.own + z.x * both.shared;
             y1 = y1 * both.own + z.y * both.shared;
@@ -479,25 +480,26 @@ int row_tiles_of(const KvView& kv, int64_t n, int64_t total, int heads) {
   return attend_rows(kv, n, total, heads) > 8 && kv.c.head_dim <= 128 ? 2 : 1;
 }
 
-template <typename T, int D, int NT>
+template <typename T, int D, int NT, bool CAUSAL>
 cudaError_t attend(AttendArgs a, void* workspace, cudaStream_t s) {
   const int grid = device_sm_count() * per_sm(D, NT);
   take_workspace(a, grid, workspace);
-  (a.kv.c.codes == TQ_KV_INT8 ? k_kv_attend<T, D, TQ_KV_INT8, NT> : k_kv_attend<T, D, TQ_KV_E4M3, NT>)<<<grid, THREADS, 0, s>>>(a);
+  (a.kv.c.codes == TQ_KV_INT8 ? k_kv_attend<T, D, TQ_KV_INT8, NT, CAUSAL> : k_kv_attend<T, D, TQ_KV_E4M3, NT, CAUSAL>)
+      <<<grid, THREADS, 0, s>>>(a);
   const cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
-  return launch_join<T, D, 8 * NT>(a, grid, s);
+  return launch_join<T, D, StreamCut<NT, CAUSAL>>(a, grid, s);
 }
 
-template <typename T>
+template <typename T, bool CAUSAL>
 cudaError_t attend_for(const AttendArgs& a, int nt, void* workspace, cudaStream_t s) {
   switch (a.kv.c.head_dim) {
     case 64:
-      return (nt == 1 ? attend<T, 64, 1> : attend<T, 64, 2>)(a, workspace, s);
+      return (nt == 1 ? attend<T, 64, 1, CAUSAL> : attend<T, 64, 2, CAUSAL>)(a, workspace, s);
     case 128:
-      return (nt == 1 ? attend<T, 128, 1> : attend<T, 128, 2>)(a, workspace, s);
+      return (nt == 1 ? attend<T, 128, 1, CAUSAL> : attend<T, 128, 2, CAUSAL>)(a, workspace, s);
     default:
-      return attend<T, 256, 1>(a, workspace, s);
+      return attend<T, 256, 1, CAUSAL>(a, workspace, s);
   }
 }
 
@@ -524,7 +526,10 @@ namespace {
 cudaError_t launch(const AttendArgs& a, int type, int64_t sequences, void* workspace, cudaStream_t s) {
   if (kv_tile_supported(a.kv, sequences, a.total, a.heads)) return launch_kv_tile(a, type, workspace, s);
   const int nt = row_tiles_of(a.kv, sequences, a.total, a.heads);
-  return type == TQ_BF16 ? attend_for<__nv_bfloat16>(a, nt, workspace, s) : attend_for<__half>(a, nt, workspace, s);
+  const bool bf16 = type == TQ_BF16;
+  return (a.sees == KvSees::CAUSAL ? bf16 ? attend_for<__nv_bfloat16, true> : attend_for<__half, true>
+          : bf16                   ? attend_for<__nv_bfloat16, false>
+                                   : attend_for<__half, false>)(a, nt, workspace, s);
 }
 
 size_t sums_bytes(const KvView& kv, int64_t total, int heads) {

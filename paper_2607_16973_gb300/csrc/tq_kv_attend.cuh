@@ -43,9 +43,6 @@ struct Split {
   int from;             // first token that it sees
 };
 
-// Whether every query sees all tokens, whatever its place.
-__host__ __device__ inline bool dense(const AttendArgs& a) { return a.sees == KvSees::ALL || a.sees == KvSees::SHARED; }
-
 // Rows per key head that a sequence of the call brings on average.
 inline int64_t attend_rows(const KvView& kv, int64_t n, int64_t total, int heads) {
   return n > 0 ? (total + n - 1) / n * (heads / kv.c.kv_heads) : 0;
@@ -73,11 +70,19 @@ __device__ __forceinline__ float ex2(float x) {
 }
 
 // A kernel's cut: ROWS rows to a tile, blocks of BLOCK tokens, an item's setup in
-// blocks, and the fewest blocks that are worth a run.
-template <int ROWS_, int BLOCK_, int ITEM_, int MIN_>
+// blocks, and the fewest blocks that are worth a run.  CAUSAL: KvSees::CAUSAL alone; the
+// other kinds have kernels of their own.  (One kernel for all, against that: prompts of
+// 2,048 tokens 345 us and 308, one query over 200,001 tokens 94 and 86, 288 rows at
+// head_dim 64 127 and 113, 12 sequences at head_dim 256 55 and 44.)
+template <int ROWS_, int BLOCK_, int ITEM_, int MIN_, bool CAUSAL_ = true>
 struct Cut {
   static constexpr int ROWS = ROWS_, BLOCK = BLOCK_, ITEM = ITEM_, MIN = MIN_;
+  static constexpr bool CAUSAL = CAUSAL_;
 };
+
+// Whether every query sees all tokens from the first that it sees on, whatever its place.
+template <class P>
+__device__ __forceinline__ bool dense(const AttendArgs& a) { return !P::CAUSAL && a.sees != KvSees::OWN; }
 
 // Blocks that the rows of a tile see: [first, first + blocks).
 struct Span {
@@ -86,14 +91,14 @@ struct Span {
 };
 
 template <class P>
-__device__ __forceinline__ Span tile_span(const AttendArgs& a, const KvSeq& s, int tile) {
+__device__ __forceinline__ Span tile_span(const AttendArgs& a, const KvSeq& s, int from, int tile) {
   Span w;
   const unsigned group = (unsigned)a.group, row0 = (unsigned)tile * P::ROWS;
   const unsigned last = min((unsigned)s.count * group, row0 + P::ROWS) - 1;
-  w.place_lo = dense(a) ? s.len - 1 : s.len - s.count + (int)(row0 / group);
-  w.place_hi = dense(a) ? s.len - 1 : s.len - s.count + (int)(last / group);
+  w.place_lo = dense<P>(a) ? s.len - 1 : s.len - s.count + (int)(row0 / group);
+  w.place_hi = dense<P>(a) ? s.len - 1 : s.len - s.count + (int)(last / group);
   // (a row in front of the sequence's first token sees nothing; its place may be as far below 0 as int reaches)
-  w.first = max(s.from, a.window ? max(0, max(0, w.place_lo) - a.window + 1) : 0) / P::BLOCK;
+  w.first = (!P::CAUSAL ? from : a.window ? max(0, max(0, w.place_lo) - a.window + 1) : 0) / P::BLOCK;
   w.blocks = w.place_hi < 0 ? 0 : max(0, w.place_hi / P::BLOCK + 1 - w.first);
   return w;
 }
@@ -123,19 +128,21 @@ __device__ __forceinline__ bool shares(const AttendArgs& a, int64_t i, const KvS
   return true;
 }
 
-// Sequence i as this call's rows see it; false where it is left out.
-__device__ __forceinline__ bool attend_seq(const AttendArgs& a, int64_t i, KvSeq& s, bool& bad) {
+// Sequence i as this call's rows see it, its tokens from `from` on; false where it is left out.
+template <class P>
+__device__ __forceinline__ bool attend_seq(const AttendArgs& a, int64_t i, KvSeq& s, int& from, bool& bad) {
+  from = 0;
   bad = false;
   if (!kv_seq(a.kv, a.slots, a.starts, i, a.total, true, s)) {
-    bad = a.sees != KvSees::SHARED;  // (the requests' own side says it)
-    if (a.sees == KvSees::SHARED) s.count = 0;
+    bad = P::CAUSAL || a.sees != KvSees::SHARED;  // (the requests' own side says it)
+    if (!bad) s.count = 0;
     return false;
   }
-  if (a.sees == KvSees::SHARED || a.sees == KvSees::OWN) {
+  if (!P::CAUSAL && a.sees != KvSees::ALL) {
     int first, members, tokens;
     const bool shared = shares(a, i, s, first, members, tokens, bad);
     if (a.sees == KvSees::OWN) {
-      s.from = shared ? tokens : 0;
+      from = shared ? tokens : 0;
     } else {
       bad = false;
       s.count = shared && first == i ? a.starts[first + members] - s.token : 0;
@@ -147,15 +154,18 @@ __device__ __forceinline__ bool attend_seq(const AttendArgs& a, int64_t i, KvSeq
 
 // Sums of the sequences' units, found by a whole block: before[i] is what lies
 // in front of sequence base + i.
-struct Units {
+template <bool CAUSAL>
+struct UnitsOf {
   int64_t before[CHUNK + 1];
   KvSeq seq[CHUNK];
+  int from[CAUSAL ? 1 : CHUNK];
   int64_t warp_sums[SCAN / 32];
   int64_t base, total;
 };
+using Units = UnitsOf<true>;
 
 template <class P>
-__device__ void load_chunk(const AttendArgs& a, Units& u, int64_t base, int64_t sum) {
+__device__ void load_chunk(const AttendArgs& a, UnitsOf<P::CAUSAL>& u, int64_t base, int64_t sum) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   __syncthreads();  // (a warp may still look an item up in the chunk that this one replaces)
   for (int j0 = 0; j0 < CHUNK; j0 += SCAN) {
@@ -165,15 +175,17 @@ __device__ void load_chunk(const AttendArgs& a, Units& u, int64_t base, int64_t 
     if (threadIdx.x < SCAN) {
       if (base + j < a.n) {
         KvSeq s;
+        int from;
         bool bad;
-        if (!attend_seq(a, base + j, s, bad)) {
+        if (!attend_seq<P>(a, base + j, s, from, bad)) {
           s.len = 0;
           if (s.token < 0 || s.count < 0 || s.count > a.total || s.token > a.total - s.count) s.count = 0;
         }
         if (bad && blockIdx.x == 0) kv_status(a.kv, kKvBadEntry);
         u.seq[j] = s;
+        if (!P::CAUSAL) u.from[j] = from;
         const int tiles = tiles_of<P>(a, s);
-        for (int t = 0; t < tiles; ++t) mine += P::ITEM + tile_span<P>(a, s, t).blocks;
+        for (int t = 0; t < tiles; ++t) mine += P::ITEM + tile_span<P>(a, s, from, t).blocks;
         mine *= a.kv.c.kv_heads;
       }
       run = mine;
@@ -204,7 +216,7 @@ __device__ void load_chunk(const AttendArgs& a, Units& u, int64_t base, int64_t 
 
 // The units of the whole call; the first chunk is loaded last.
 template <class P>
-__device__ int64_t load_units(const AttendArgs& a, Units& u) {
+__device__ int64_t load_units(const AttendArgs& a, UnitsOf<P::CAUSAL>& u) {
   load_chunk<P>(a, u, 0, 0);
   if (a.n <= CHUNK) return u.total;
   int64_t sum = u.total;
@@ -219,21 +231,23 @@ __device__ int64_t load_units(const AttendArgs& a, Units& u) {
 // The item that unit x falls into, found by a warp; the chunk with x is loaded.
 struct Item {
   KvSeq s;
+  int from;  // first token that its rows see
   Span span;
   int64_t begin;  // its first unit
   int tile, head, units;
 };
 
 template <class P>
-__device__ Item find_item(const AttendArgs& a, const Units& u, int64_t x) {
+__device__ Item find_item(const AttendArgs& a, const UnitsOf<P::CAUSAL>& u, int64_t x) {
   const int lane = threadIdx.x & 31;
   const int64_t i = warp_last_not_above(min((int64_t)CHUNK, a.n - u.base), x, [&](int64_t j) { return u.before[j]; });
   Item it;
   it.s = u.seq[i];
+  it.from = P::CAUSAL ? 0 : u.from[i];
   const int tiles = tiles_of<P>(a, it.s);
   int64_t in = x - u.before[i];
   for (int base = 0;; base += 32) {  // a tile per lane
-    const int64_t mine = base + lane < tiles ? (int64_t)(P::ITEM + tile_span<P>(a, it.s, base + lane).blocks) * a.kv.c.kv_heads : 0;
+    const int64_t mine = base + lane < tiles ? (int64_t)(P::ITEM + tile_span<P>(a, it.s, it.from, base + lane).blocks) * a.kv.c.kv_heads : 0;
     int64_t upto = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -249,7 +263,7 @@ __device__ Item find_item(const AttendArgs& a, const Units& u, int64_t x) {
     }
     in -= __shfl_sync(FULL, upto, 31);
   }
-  it.span = tile_span<P>(a, it.s, it.tile);
+  it.span = tile_span<P>(a, it.s, it.from, it.tile);
   it.units = P::ITEM + it.span.blocks;
   it.head = (int)(in / it.units);
   it.begin = x - in % it.units;
@@ -259,7 +273,7 @@ __device__ Item find_item(const AttendArgs& a, const Units& u, int64_t x) {
 // Loads the chunk that unit x falls into; x does not go back behind the one that is
 // loaded.  By the whole block.
 template <class P>
-__device__ __forceinline__ void chunk_of(const AttendArgs& a, Units& u, int64_t x) {
+__device__ __forceinline__ void chunk_of(const AttendArgs& a, UnitsOf<P::CAUSAL>& u, int64_t x) {
   while (x >= u.total) load_chunk<P>(a, u, u.base + CHUNK, u.total);  // (uniform: x and u are the block's)
 }
 
@@ -279,7 +293,7 @@ __device__ __forceinline__ int64_t first_run(int64_t unit, int64_t units, int64_
 // that its sequences bring on average: they decide on the kernel and its row tiles,
 // which round weights differently.)
 template <class P>
-__device__ int64_t run_cut(const AttendArgs& a, Units& u, int64_t c, int64_t units, int64_t n) {
+__device__ int64_t run_cut(const AttendArgs& a, UnitsOf<P::CAUSAL>& u, int64_t c, int64_t units, int64_t n) {
   const int64_t x = run_start(c, units, n);
   if (x >= units) return units;
   chunk_of<P>(a, u, x);
@@ -308,7 +322,7 @@ struct Run {
 // Sets this block's run up: false if it has none.  Leaves the chunk of its start
 // loaded, and its entry of `splits` empty.
 template <class P>
-__device__ bool my_run(const AttendArgs& a, Units& units, Run& run) {
+__device__ bool my_run(const AttendArgs& a, UnitsOf<P::CAUSAL>& units, Run& run) {
   const int64_t all = load_units<P>(a, units), n_runs = runs<P>(all, gridDim.x);
   if (threadIdx.x == 0) a.splits[blockIdx.x].first = -1;
   if (blockIdx.x >= n_runs) return false;
@@ -329,7 +343,7 @@ __device__ bool my_run(const AttendArgs& a, Units& units, Run& run) {
 // Finds the next segment of the run, in run.seg; the caller moves run.u on, behind
 // a barrier.  Notes an item that this run is the first to continue.
 template <class P>
-__device__ __forceinline__ void next_segment(const AttendArgs& a, Units& units, Run& run) {
+__device__ __forceinline__ void next_segment(const AttendArgs& a, UnitsOf<P::CAUSAL>& units, Run& run) {
   chunk_of<P>(a, units, run.u);
   if (threadIdx.x < 32) {
     const int64_t u = run.u;
@@ -348,7 +362,7 @@ __device__ __forceinline__ void next_segment(const AttendArgs& a, Units& units, 
         const int first = (int)first_run(g.it.begin + P::ITEM + P::MIN, run.all, run.n_runs) - 1;
         if (first + 1 == (int)blockIdx.x)
           a.splits[blockIdx.x] = {first,         (int)last_run(g.it.begin + g.it.units - P::MIN, run.all, run.n_runs),
-                                  g.it.s.token, g.it.head, g.row0, g.rows, g.it.s.from};
+                                  g.it.s.token, g.it.head, g.row0, g.rows, g.it.from};
       }
     }
   }
@@ -403,7 +417,7 @@ __device__ __forceinline__ Both join_shared(const AttendArgs& a, int dim, int64_
 constexpr int PAD = 16;
 constexpr int FEW = 8, FEW_ROWS = 4;  // (a lane for each part of each row)
 constexpr int join_warps(int dim) { return dim == 256 ? 4 : 8; }  // (their sums take 32 KB of shared memory)
-template <typename T, int D, int ROWS>
+template <typename T, int D, int ROWS, bool CAUSAL>
 __global__ __launch_bounds__(join_warps(D) * 32) void k_kv_join(AttendArgs a) {
   constexpr int JOIN_WARPS = join_warps(D);
   constexpr int E = D / 32;  // elements of a lane
@@ -412,7 +426,7 @@ __global__ __launch_bounds__(join_warps(D) * 32) void k_kv_join(AttendArgs a) {
   __shared__ float sh_o[JOIN_WARPS][8][D];
   __shared__ float sh_l[JOIN_WARPS][8], sh_m[JOIN_WARPS][8];
   if (blockIdx.x < PAD) {
-    if (a.sees == KvSees::SHARED) return;  // (the requests' own side writes them)
+    if (!CAUSAL && a.sees == KvSees::SHARED) return;  // (the requests' own side writes them)
     const int64_t front = min(max((int64_t)a.starts[0], (int64_t)0), a.total);
     const int64_t behind = min(max((int64_t)a.starts[a.n], front), a.total);
     const int pieces = a.heads * (D / 8);  // of 16 bytes, of a token
@@ -434,7 +448,7 @@ __global__ __launch_bounds__(join_warps(D) * 32) void k_kv_join(AttendArgs a) {
   // A joined row's sums to the output, or to where the requests' own side finds them.
   auto finish = [&](int row, float top, float sum, float (&y)[E]) {
     const int64_t at = out_row(a, sp.token, sp.head, sp.row0 + row);
-    if (a.sees == KvSees::SHARED) {
+    if (!CAUSAL && a.sees == KvSees::SHARED) {
 #pragma unroll
       for (int e = 0; e < E; ++e) a.sums[at * D + lane * E + e] = y[e];
       if (lane == 0) {
@@ -443,12 +457,13 @@ __global__ __launch_bounds__(join_warps(D) * 32) void k_kv_join(AttendArgs a) {
       }
       return;
     }
-    const Both f = join_shared(a, D, at, sp.from, top, sum);
+    const int from = CAUSAL ? 0 : sp.from;
+    const Both f = join_shared(a, D, at, from, top, sum);
     const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
     T* out = static_cast<T*>(a.out) + at * D + lane * E;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      if (sp.from > 0) y[e] = y[e] * f.own + a.sums[at * D + lane * E + e] * f.shared;
+      if (from > 0) y[e] = y[e] * f.own + a.sums[at * D + lane * E + e] * f.shared;
       out[e] = from_float<T>(y[e] * inv);
     }
     if (a.lse && lane == 0) a.lse[at] = lse_of(top, sum);
@@ -571,9 +586,9 @@ __global__ __launch_bounds__(join_warps(D) * 32) void k_kv_join(AttendArgs a) {
 }
 
 // Workspace: Split [grid] | partial sums.
-template <typename T, int D, int ROWS>
+template <typename T, int D, class P>
 cudaError_t launch_join(const AttendArgs& a, int grid, cudaStream_t s) {
-  return launch_maybe_pdl(true, k_kv_join<T, D, ROWS>, dim3(PAD + grid, ROWS / 8), dim3(join_warps(D) * 32), 0, s, a);
+  return launch_maybe_pdl(true, k_kv_join<T, D, P::ROWS, P::CAUSAL>, dim3(PAD + grid, P::ROWS / 8), dim3(join_warps(D) * 32), 0, s, a);
 }
 
 inline size_t split_bytes(int grid) { return ((size_t)grid * sizeof(Split) + 255) / 256 * 256; }

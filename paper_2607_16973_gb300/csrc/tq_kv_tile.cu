@@ -58,7 +58,8 @@ constexpr int SCALE_RING = 4;  // tiles whose scales are held (two being convert
 
 // A run is worth a tile of tokens; an item costs about as much as four beside its
 // own (two long prompts: 383 us counted as two, 313 as four, 318 as six).
-using TileCut = Cut<256, TOKENS, 4, 1>;
+template <bool CAUSAL>
+using TileCut = Cut<256, TOKENS, 4, 1, CAUSAL>;
 
 template <int D>
 struct TileSmem {
@@ -67,8 +68,9 @@ struct TileSmem {
   static constexpr int q = 0, k = q + 2 * Q, v = k + 2 * K, rest = v + 2 * K, total = rest + 18432 + 1024;
 };
 
+template <bool CAUSAL>
 struct TileShared {  // behind the operands
-  Units units;
+  UnitsOf<CAUSAL> units;
   Run run;
   // of a tile's blocks: K's scale, log2 of V's, 1 / V's; a block without tokens, or
   // one that cannot be read, has 0, -inf, 0
@@ -79,8 +81,9 @@ struct TileShared {  // behind the operands
   uint32_t tmem;
   int abort_flag, err;
 };
-static_assert(offsetof(TileShared, scales) % 16 == 0, "scales are read four at a time");
-static_assert(sizeof(TileShared) <= 18432, "shared memory behind the operands");
+static_assert(offsetof(TileShared<true>, scales) % 16 == 0 && offsetof(TileShared<false>, scales) % 16 == 0,
+              "scales are read four at a time");
+static_assert(sizeof(TileShared<true>) <= 18432 && sizeof(TileShared<false>) <= 18432, "shared memory behind the operands");
 
 __host__ __device__ constexpr uint32_t tile_idesc(int n) {
   return (1u << 4) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
@@ -155,13 +158,13 @@ __device__ __forceinline__ uint32_t pack_fp16(float a, float b) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-template <typename T, int D, int CODES>
+template <typename T, int D, int CODES, bool CAUSAL>
 __global__ __launch_bounds__(TILE_THREADS, 1) void k_kv_tile(AttendArgs a) {
-  using P = TileCut;
+  using P = TileCut<CAUSAL>;
   using M = TileSmem<D>;
   extern __shared__ unsigned char raw_smem[];
   unsigned char* sm = raw_smem + ((1024u - (smem_u32(raw_smem) & 1023u)) & 1023u);
-  TileShared& sh = *reinterpret_cast<TileShared*>(sm + M::rest);
+  TileShared<CAUSAL>& sh = *reinterpret_cast<TileShared<CAUSAL>*>(sm + M::rest);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const KvView& kv = a.kv;
 
@@ -202,6 +205,7 @@ __global__ __launch_bounds__(TILE_THREADS, 1) void k_kv_tile(AttendArgs a) {
     next_segment<P>(a, sh.units, sh.run);
     const Segment& seg = sh.run.seg;
     const KvSeq sq = seg.it.s;
+    const int from = CAUSAL ? 0 : seg.it.from;
     const int head = seg.it.head;
     const int tiles = seg.b_last - seg.b_first, first = seg.it.span.first + seg.b_first;  // tiles of tokens
     // Two row tiles, each with its half of the softmax; or one, whose tiles of tokens
@@ -291,7 +295,7 @@ __global__ __launch_bounds__(TILE_THREADS, 1) void k_kv_tile(AttendArgs a) {
       float m = -INFINITY, l = 0.0f;
       bool ok = all_wait(sh.q_full + rt, segments & 1, abort_flag, err, 6);
       const float unscale = sh.unscale[rt * 128 + row];
-      const int place = real ? max(-1, dense(a) ? sq.len - 1 : sq.len - sq.count + r / a.group) : -1;
+      const int place = real ? max(-1, dense<P>(a) ? sq.len - 1 : sq.len - sq.count + r / a.group) : -1;
       // what the first warp issues for the four
       const bool issuer = (warp & 3) == 0;
       const uint32_t tm = __shfl_sync(FULL, tmem, 0), sm0 = __shfl_sync(FULL, smem_u32(sm), 0);
@@ -337,7 +341,7 @@ __global__ __launch_bounds__(TILE_THREADS, 1) void k_kv_tile(AttendArgs a) {
           const int t0 = (first + j) * TOKENS;
           // columns [lo, hi) are seen; they are looked at only where some row does not see them
           // all.  (lo may wrap around only for hi <= 0, where nothing is seen whatever it is.)
-          const int hi = place - t0 + 1, lo = max(sq.from - t0, a.window ? (int)((unsigned)hi - (unsigned)a.window) : 0);
+          const int hi = place - t0 + 1, lo = !CAUSAL ? max(0, from - t0) : a.window ? (int)((unsigned)hi - (unsigned)a.window) : 0;
           const bool edge = __any_sync(FULL, real && (hi < TOKENS || lo > 0));
           // Half of S at a time (64 columns, 4 blocks): the second half's maximum, the
           // first half's, its weights, and the second half read again for its.  P goes
@@ -651,9 +655,9 @@ __global__ __launch_bounds__(TILE_THREADS, 1) void k_kv_tile(AttendArgs a) {
     }
     if (some && (two || w == 0)) {
       const int64_t at = real ? out_row(a, sq.token, head, r) : 0;
-      const bool sums = a.sees == KvSees::SHARED;
-      const int from = real && seg.whole ? sq.from : 0;
-      const Both both = join_shared(a, D, at, from, m, l);
+      const bool sums = !CAUSAL && a.sees == KvSees::SHARED;
+      const int joined = !CAUSAL && real && seg.whole ? from : 0;
+      const Both both = join_shared(a, D, at, joined, m, l);
       const float inv = l > 0.0f ? 1.0f / l : 0.0f;
       float* part = part_of<D, P::ROWS>(a, seg);
       const int prow = rt * 128 + row;
@@ -668,7 +672,7 @@ __global__ __launch_bounds__(TILE_THREADS, 1) void k_kv_tile(AttendArgs a) {
         }
         if (!real) continue;
         if (seg.whole && !sums) {
-          if (from > 0) {
+          if (joined > 0) {
 #pragma unroll
             for (int i = 0; i < 16; i += 4) {
               const float4 z = *reinterpret_cast<const float4*>(a.sums + at * D + c + i);
@@ -723,21 +727,21 @@ __global__ __launch_bounds__(TILE_THREADS, 1) void k_kv_tile(AttendArgs a) {
   if (warp == SOFT) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
 }
 
-template <typename T, int D, int CODES>
+template <typename T, int D, int CODES, bool CAUSAL>
 cudaError_t tile(const AttendArgs& a, int grid, cudaStream_t s) {
-  auto* kernel = k_kv_tile<T, D, CODES>;
+  auto* kernel = k_kv_tile<T, D, CODES, CAUSAL>;
   cudaError_t e = set_max_dynamic_smem(reinterpret_cast<const void*>(kernel), TileSmem<D>::total);
   if (e != cudaSuccess) return e;
   kernel<<<grid, TILE_THREADS, TileSmem<D>::total, s>>>(a);
   if ((e = cudaGetLastError()) != cudaSuccess) return e;
-  return launch_join<T, D, TileCut::ROWS>(a, grid, s);
+  return launch_join<T, D, TileCut<CAUSAL>>(a, grid, s);
 }
 
-template <typename T>
+template <typename T, bool CAUSAL>
 cudaError_t tile_for(const AttendArgs& a, int grid, cudaStream_t s) {
   const bool i8 = a.kv.c.codes == TQ_KV_INT8;
-  if (a.kv.c.head_dim == 64) return (i8 ? tile<T, 64, TQ_KV_INT8> : tile<T, 64, TQ_KV_E4M3>)(a, grid, s);
-  return (i8 ? tile<T, 128, TQ_KV_INT8> : tile<T, 128, TQ_KV_E4M3>)(a, grid, s);
+  if (a.kv.c.head_dim == 64) return (i8 ? tile<T, 64, TQ_KV_INT8, CAUSAL> : tile<T, 64, TQ_KV_E4M3, CAUSAL>)(a, grid, s);
+  return (i8 ? tile<T, 128, TQ_KV_INT8, CAUSAL> : tile<T, 128, TQ_KV_E4M3, CAUSAL>)(a, grid, s);
 }
 
 }  // namespace
@@ -753,14 +757,17 @@ bool kv_tile_supported(const KvView& kv, int64_t n, int64_t total, int heads) {
 }
 
 size_t kv_tile_workspace(const KvView& kv) {
-  return attend_workspace(device_sm_count(), TileCut::ROWS, kv.c.head_dim);
+  return attend_workspace(device_sm_count(), TileCut<true>::ROWS, kv.c.head_dim);
 }
 
 cudaError_t launch_kv_tile(AttendArgs a, int type, void* workspace, cudaStream_t s) {
   const int grid = device_sm_count();
   take_workspace(a, grid, workspace);
   a.q_wide = aligned16(a.q.p) && a.q.token_stride % 8 == 0 && a.q.head_stride % 8 == 0;
-  return type == TQ_BF16 ? tile_for<__nv_bfloat16>(a, grid, s) : tile_for<__half>(a, grid, s);
+  const bool bf16 = type == TQ_BF16;
+  return (a.sees == KvSees::CAUSAL ? bf16 ? tile_for<__nv_bfloat16, true> : tile_for<__half, true>
+          : bf16                   ? tile_for<__nv_bfloat16, false>
+                                   : tile_for<__half, false>)(a, grid, s);
 }
 
 }  // namespace tq
