@@ -469,9 +469,12 @@ __global__ __launch_bounds__(join_warps(D) * 32) void k_kv_join(AttendArgs a) {
     if (a.lse && lane == 0) a.lse[at] = lse_of(top, sum);
   };
   const int n = sp.last - sp.first + 1;
-  if (n <= FEW) {
-    // Few parts: a warp joins FEW_ROWS rows by itself, in the same order.  (As below, 1,200 rows
-    // over 7 sequences took 35 us, most of it the parts' one load, a barrier and idle warps.)
+  if (ROWS > 16 && n <= FEW) {
+    // Few parts of a tensor-core tile: a warp joins FEW_ROWS rows by itself, in the same order.  (As
+    // below, 1,200 rows over 7 sequences took 35 us, most of it the parts' one load, a barrier and
+    // idle warps.  The stream's 8 or 16 rows are one or two blocks' as below: 86 us for 200,001
+    // tokens, 89 this way; and at head_dim 256 four warps add their two parts each up first.)
+    static_assert(ROWS <= 16 || JOIN_WARPS == FEW, "a warp for each part below");
     const int first = (blockIdx.y * JOIN_WARPS + warp) * FEW_ROWS;
     if (sp.row0 + first >= sp.rows || first >= ROWS) return;
     const int live = min(FEW_ROWS, min(ROWS - first, sp.rows - sp.row0 - first));

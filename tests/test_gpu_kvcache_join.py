@@ -1,0 +1,25 @@
+"""How the parts of a sequence that is cut are joined (tq_kv_attend)."""
+import numpy as np
+import pytest
+
+from test_gpu_kvcache import Case, compare
+
+pytestmark = pytest.mark.gpu
+
+
+def test_parts_of_one_warp_are_added_first_at_head_dim_256(cuda_lib):
+    """384 tokens in six parts of 64, each block of 16 its scale: what cancels between the first part and the fifth, which one
+    of four warps takes, leaves the second's in place.  Scores are 0, so a part's sum is its values'."""
+    torch = __import__("torch")
+    case = Case(cuda_lib, [384], [1], kv_heads=1, dim=256, page=64, seed=1)
+    for name in "kv":
+        case.pool[name][:] = 0
+        case.scale[name][:] = 1.0
+    pages = case.table[case.slots[0]]
+    for token, code, scale in ((5, 127, 2.0 ** 30), (4 * 64 + 5, -127, 2.0 ** 30), (64 + 9, 127, 1.0)):
+        p, inside = pages[token // 64], token % 64
+        case.pool["v"][case.layer, p, 0, inside] = np.uint8(code % 256)
+        case.scale["v"][case.layer, p, 0, inside // 16] = scale
+    q = torch.zeros(1, 1, 256, dtype=torch.float16, device="cuda")
+    out = case.cache().attention(case.layer, case.device(case.slots), case.device(case.starts), q)
+    assert (out == torch.tensor(127 / 384, dtype=torch.float16, device="cuda")).all()
