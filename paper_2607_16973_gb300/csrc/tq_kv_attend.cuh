@@ -489,6 +489,7 @@ __global__ __launch_bounds__(join_warps(D) * 32) void k_kv_join(AttendArgs a) {
 #pragma unroll
     for (int w = 1; w < FEW; w <<= 1) top = fmaxf(top, __shfl_sync(FULL, top, lane ^ w));
     const float f = top > -INFINITY ? ex2(m - top) : 1.0f;  // (1: sums of 0, or NaN)
+    const unsigned some = __ballot_sync(FULL, m > -INFINITY || l != 0.0f);  // the row saw something there
     float y[FEW_ROWS][E], sum[FEW_ROWS];
 #pragma unroll
     for (int r = 0; r < FEW_ROWS; ++r) {
@@ -511,8 +512,8 @@ __global__ __launch_bounds__(join_warps(D) * 32) void k_kv_join(AttendArgs a) {
 #pragma unroll
       for (int r = 0; r < FEW_ROWS; ++r) {
         const float fr = __shfl_sync(FULL, f, r * FEW + x), lr = __shfl_sync(FULL, l, r * FEW + x);
-        sum[r] += fr * lr;
-        if (r < live) {
+        if (some >> (r * FEW + x) & 1) {  // (r < live)
+          sum[r] += fr * lr;
 #pragma unroll
           for (int e = 0; e < E; ++e) y[r][e] += fr * z[r].f[e];
         }

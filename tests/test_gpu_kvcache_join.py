@@ -23,3 +23,20 @@ def test_parts_of_one_warp_are_added_first_at_head_dim_256(cuda_lib):
     q = torch.zeros(1, 1, 256, dtype=torch.float16, device="cuda")
     out = case.cache().attention(case.layer, case.device(case.slots), case.device(case.starts), q)
     assert (out == torch.tensor(127 / 384, dtype=torch.float16, device="cuda")).all()
+
+
+@pytest.mark.parametrize("length", [700, 1300])
+def test_a_part_that_a_row_does_not_see_is_left_out(cuda_lib, length):
+    """256 prompted tokens in parts of 128, up to eight and more: values that are not numbers behind the first queries' places do
+    not reach them, whatever they are multiplied by."""
+    case = Case(cuda_lib, [length], [256], kv_heads=1, dim=128, codes="e4m3", seed=length).fill()
+    q = case.queries(1, "bfloat16")
+    last = length // 128 * 128
+    good = case.expected(q.double().cpu().numpy())
+    for token in range(last, length):
+        case.pool["v"][case.layer, case.table[case.slots[0], token // case.page], 0, token % case.page] = 0x7F
+    out, lse = case.cache().attention(case.layer, case.device(case.slots), case.device(case.starts), q, return_lse=True)
+    n = last - (length - 256)  # queries in front
+    case.expected = lambda *_: [x[:n] for x in good]
+    compare(case, q[:n], out[:n], lse[:n])
+    assert out[n:].isnan().all()
