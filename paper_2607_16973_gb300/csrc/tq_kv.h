@@ -72,6 +72,13 @@ cudaError_t launch_kv_attend_shared(const KvView& kv, int layer, const int32_t* 
                                     cudaStream_t s);
 cudaError_t launch_kv_share(const KvView& kv, const int32_t* slots, const int32_t* starts, int64_t n, int32_t* plan,
                             cudaStream_t s);
+// What a plan's entry comes to: the tokens that its request shares (0: none), and the
+// queries of its group if it is the group's first (else 0).
+struct KvShared {
+  int tokens, queries;
+};
+cudaError_t launch_kv_entries(const KvView& kv, const int32_t* slots, const int32_t* starts, const int32_t* plan,
+                              int64_t n, int64_t total, KvShared* entries, cudaStream_t s);
 
 cudaError_t launch_kv_fork(const KvView& kv, const int32_t* dst, const int32_t* src, int64_t n, cudaStream_t s);
 size_t kv_extend_workspace(const KvView& kv, int64_t n);

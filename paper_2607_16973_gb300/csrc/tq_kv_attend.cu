@@ -535,6 +535,7 @@ cudaError_t launch(const AttendArgs& a, int type, int64_t sequences, void* works
 size_t sums_bytes(const KvView& kv, int64_t total, int heads) {
   return ((size_t)total * heads * (kv.c.head_dim + 2) * sizeof(float) + 255) / 256 * 256;
 }
+size_t entries_bytes(int64_t n) { return ((size_t)n * sizeof(KvShared) + 255) / 256 * 256; }
 
 }  // namespace
 
@@ -546,9 +547,10 @@ cudaError_t launch_kv_attend(const KvView& kv, int layer, const int32_t* slots, 
   return launch(a, type, n, workspace, s);
 }
 
-// Workspace: the shared tokens' sums | what either attention needs (one after the other).
+// Workspace: the shared tokens' sums | what the plan's entries come to | what either attention
+// needs (one after the other).
 size_t kv_shared_workspace(const KvView& kv, int64_t n, int64_t total, int heads) {
-  return sums_bytes(kv, total, heads) + kv_attend_workspace(kv, n, total, heads);
+  return sums_bytes(kv, total, heads) + entries_bytes(n) + kv_attend_workspace(kv, n, total, heads);
 }
 
 // The shared tokens first, each group's once for all its queries, their sums left in
@@ -557,10 +559,13 @@ cudaError_t launch_kv_attend_shared(const KvView& kv, int layer, const int32_t* 
                                     const int32_t* plan, int64_t n, int64_t groups, const KvRows& q, int type,
                                     int64_t total, int heads, float scale, void* out, float* lse, void* workspace,
                                     cudaStream_t s) {
+  char* behind = static_cast<char*>(workspace) + sums_bytes(kv, total, heads);
+  KvShared* entries = reinterpret_cast<KvShared*>(behind);
+  void* rest = behind + entries_bytes(n);
   AttendArgs a = {kv, layer, slots, starts, n, total, q, false, heads, heads / kv.c.kv_heads, scale, 0, out, lse,
-                  nullptr, nullptr, KvSees::SHARED, plan, static_cast<float*>(workspace)};
-  void* rest = static_cast<char*>(workspace) + sums_bytes(kv, total, heads);
-  const cudaError_t e = launch(a, type, groups, rest, s);
+                  nullptr, nullptr, KvSees::SHARED, entries, static_cast<float*>(workspace)};
+  cudaError_t e = launch_kv_entries(kv, slots, starts, plan, n, total, entries, s);
+  if (e == cudaSuccess) e = launch(a, type, groups, rest, s);
   if (e != cudaSuccess) return e;
   a.sees = KvSees::OWN;
   return launch(a, type, n, rest, s);

@@ -31,7 +31,7 @@ struct AttendArgs {
   float* parts;          // [2 * grid][rows * (D + 2)]: partial O, m, l
   struct Split* splits;  // [grid]
   KvSees sees;
-  const int32_t* plan;   // [3][n]: tq_kv_share
+  const KvShared* entries;  // [n]: of a plan's requests
   float* sums;           // shared tokens: O [total * heads][D], then m, then l of every row
 };
 
@@ -109,25 +109,6 @@ __device__ __forceinline__ int tiles_of(const AttendArgs& a, const KvSeq& s) {
   return (int)(((unsigned)s.count * (unsigned)a.group + P::ROWS - 1) / P::ROWS);
 }
 
-// Whether request i shares tokens that its plan's entry says: false, with `bad` set,
-// where the entry does not fit the call (it is then attended by itself).  Both sides
-// of the call, the shared tokens' and the requests' own, ask here.
-__device__ __forceinline__ bool shares(const AttendArgs& a, int64_t i, const KvSeq& s, int& first, int& members,
-                                       int& tokens, bool& bad) {
-  first = a.plan[i], members = a.plan[a.n + i], tokens = a.plan[2 * a.n + i];
-  bad = tokens < 0;
-  if (tokens <= 0 || members <= 1) return false;
-  bad = true;
-  if (first < 0 || first > i || members > a.n - first || i >= (int64_t)first + members) return false;
-  if (a.plan[first] != first || a.plan[a.n + first] != members || a.plan[2 * a.n + first] != tokens) return false;
-  KvSeq lead;  // its pages hold the tokens, its group's queries lie side by side
-  if (!kv_seq(a.kv, a.slots, a.starts, first, a.total, true, lead) || lead.len - lead.count < tokens) return false;
-  const int end = a.starts[first + members];
-  if (end > a.total || s.token < lead.token || s.token + s.count > end || s.len - s.count < tokens) return false;
-  bad = false;
-  return true;
-}
-
 // Sequence i as this call's rows see it, its tokens from `from` on; false where it is left out.
 template <class P>
 __device__ __forceinline__ bool attend_seq(const AttendArgs& a, int64_t i, KvSeq& s, int& from, bool& bad) {
@@ -139,14 +120,12 @@ __device__ __forceinline__ bool attend_seq(const AttendArgs& a, int64_t i, KvSeq
     return false;
   }
   if (!P::CAUSAL && a.sees != KvSees::ALL) {
-    int first, members, tokens;
-    const bool shared = shares(a, i, s, first, members, tokens, bad);
+    const KvShared e = a.entries[i];
     if (a.sees == KvSees::OWN) {
-      from = shared ? tokens : 0;
+      from = e.tokens;
     } else {
-      bad = false;
-      s.count = shared && first == i ? a.starts[first + members] - s.token : 0;
-      s.len = tokens;
+      s.count = e.queries;
+      s.len = e.tokens;
     }
   }
   return true;

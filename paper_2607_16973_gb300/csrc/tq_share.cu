@@ -12,6 +12,13 @@
 // Bound: latency of two launches and of the chain slot -> length -> table; the tables are
 // read once or, from L2, twice.  2,000 requests of up to 1,000 pages (5 MB of tables): 13 us
 // a call on a GB300, 16 requests 11.
+//
+// k_share_entries says what a given plan's entries come to (tq_kv_attend_shared): a
+// group counts where all its entries name it, so that no two groups' queries are the
+// same.  Whether they do is seen without going over the group's entries for each of
+// them: entries are compared with the ones in front, and a prefix sum of those that
+// differ is alike at both ends.  Of the group that a block's first or last entry is
+// in, the block compares what lies outside of it.
 #include "tq_kv.cuh"
 #include "tq_topk.cuh"
 
@@ -124,7 +131,66 @@ __global__ __launch_bounds__(GROUPS) void k_share_groups(int64_t n, int32_t* pla
   }
 }
 
+struct Entry {
+  int first, members, tokens;
+  __device__ __forceinline__ bool operator==(const Entry& x) const {
+    return first == x.first && members == x.members && tokens == x.tokens;
+  }
+};
+
+__global__ __launch_bounds__(GROUPS) void k_share_entries(KvView kv, const int32_t* __restrict__ slots,
+                                                          const int32_t* __restrict__ starts,
+                                                          const int32_t* __restrict__ plan, int64_t n, int64_t total,
+                                                          KvShared* __restrict__ entries) {
+  __shared__ int changes[GROUPS];  // of this block's entries up to each one: how many differ from the one in front
+  __shared__ int warps[GROUPS / 32];
+  const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
+  const int64_t base = (int64_t)blockIdx.x * GROUPS, last = min(n, base + GROUPS) - 1, i = base + t;
+  auto entry = [&](int64_t j) { return Entry{plan[j], plan[n + j], plan[2 * n + j]}; };
+  const Entry e = i <= last ? entry(i) : Entry{0, 0, 0}, head = entry(base), tail = entry(last);
+  // this request, its group's first, and where the group's queries end (all asked for before anything is waited for)
+  KvSeq s, lead;
+  const int64_t end = (int64_t)e.first + e.members;
+  const bool there = i <= last && kv_seq(kv, slots, starts, i, total, true, s);
+  const bool inside = i <= last && e.first >= 0 && e.first <= i && i < end && end <= n;
+  const bool led = inside && kv_seq(kv, slots, starts, e.first, total, true, lead);
+  const int stop = inside ? starts[end] : 0;
+  const unsigned differ = __ballot_sync(FULL, t > 0 && i <= last && !(entry(i - 1) == e));
+  if (lane == 31) warps[warp] = __popc(differ);
+  __syncthreads();
+  int front = 0;
+  for (int w = 0; w < warp; ++w) front += warps[w];
+  changes[t] = front + __popc(differ & (2u << lane) - 1u);
+  // the groups of the block's first and last entries, outside of it
+  bool same = true;
+  for (int64_t j = max(head.first, 0) + t; j < base; j += GROUPS) same &= entry(j) == head;
+  const bool left = __syncthreads_and(same);  // (and the changes are there)
+  same = true;
+  for (int64_t j = last + 1 + t; j < min(n, (int64_t)tail.first + tail.members); j += GROUPS) same &= entry(j) == tail;
+  const bool right = __syncthreads_and(same);
+  if (i > last) return;
+  KvShared out = {0, 0};
+  bool bad = there && e.tokens < 0;  // (where there is no such request the attention says so)
+  if (there && e.tokens > 0 && e.members > 1) {
+    // the first one's pages hold the tokens, the group's queries lie side by side, this one's among them
+    const bool fits = led && changes[min(end - 1, last) - base] == changes[max((int64_t)e.first, base) - base] &&
+                      (e.first >= base || left) && (end - 1 <= last || right) && lead.len - lead.count >= e.tokens &&
+                      s.len - s.count >= e.tokens && stop <= total && lead.token + lead.count <= stop &&
+                      s.token >= lead.token && s.token + s.count <= stop;
+    if (fits) out = {e.tokens, e.first == i ? stop - s.token : 0};
+    bad = !fits;
+  }
+  if (bad) kv_status(kv, kKvBadEntry);
+  entries[i] = out;
+}
+
 }  // namespace
+
+cudaError_t launch_kv_entries(const KvView& kv, const int32_t* slots, const int32_t* starts, const int32_t* plan,
+                              int64_t n, int64_t total, KvShared* entries, cudaStream_t s) {
+  k_share_entries<<<(unsigned)((n + GROUPS - 1) / GROUPS), GROUPS, 0, s>>>(kv, slots, starts, plan, n, total, entries);
+  return cudaGetLastError();
+}
 
 cudaError_t launch_kv_share(const KvView& kv, const int32_t* slots, const int32_t* starts, int64_t n, int32_t* plan,
                             cudaStream_t s) {
