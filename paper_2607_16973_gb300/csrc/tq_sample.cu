@@ -567,7 +567,7 @@ __device__ int cut_list(const Setting& s, const Weigh& weigh, int n, Shared& sh)
 // What tokens below are too light: together less than the part that top-p leaves out.
 __device__ __forceinline__ float least_value(const Setting& s, float top, uint64_t sum, int vocab) {
   const float least = (1.0f - s.top_p) * ((float)sum / FIXED) / (float)vocab;
-  return fmaxf(top + logf(least) * s.temperature * 1.0001f - 1e-3f, -3.0e38f);
+  return fmaxf(top + logf(least) * s.temperature * 1.0001f - 1e-3f, -3.402823466e38f);  // (not a masked one's, nor above top)
 }
 
 // What tokens below are ruled out by min-p (> 0).

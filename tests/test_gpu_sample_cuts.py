@@ -107,3 +107,15 @@ def test_a_small_top_p_of_many_tokens(cuda_lib, place):
     noise[0, place - 1] = noise[1, place] = 2.0 ** -60
     tokens = check(cuda_lib, logits, noise, top_p=[float(top_p)] * 2)
     assert int(tokens[0]) == place - 1 and int(tokens[1]) == 0
+
+
+@pytest.mark.parametrize("type", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("vocab", [900, 20_000, 128_000])
+def test_rows_of_the_lowest_value(cuda_lib, vocab, type):
+    """All tokens at the type's lowest value, which masks nothing: they are kept in their own order."""
+    torch = __import__("torch")
+    logits, noise = row(vocab, torch.finfo(getattr(torch, type)).min, type)
+    noise[0, vocab // 2 - 1] = noise[1, vocab // 2 + 1] = 2.0 ** -60
+    tokens = check(cuda_lib, logits, noise, top_p=[0.5] * 2)
+    assert tokens.tolist() == [vocab // 2 - 1, 0]
+    assert check(cuda_lib, logits, noise, top_p=[0.5] * 2, temperature=[1e30] * 2).tolist() == [vocab // 2 - 1, 0]
