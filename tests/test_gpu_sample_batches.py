@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 
 from sampleref import sample
-from test_gpu_sample import SLACK, rows
+from test_gpu_sample import MIXED, SLACK, rows
 
 pytestmark = pytest.mark.gpu
 
@@ -113,3 +113,73 @@ def test_a_border_of_min_p_far_below_the_first(cuda_lib):
     noise.copy_(torch.from_numpy(e))
     t = torch.full((n,), temperature, device="cuda")
     assert cuda_lib.sample_tokens(logits, noise, temperature=t, min_p=torch.from_numpy(min_p).cuda()).tolist() == want
+
+
+BATCHES = [("bfloat16", 128_000), ("float16", 128_000), ("float32", 100_003)]
+
+
+@pytest.mark.parametrize("type,vocab", BATCHES)
+@pytest.mark.parametrize("likely", [0, 24])
+def test_settings_of_all_kinds(cuda_lib, type, vocab, likely):
+    n = 64
+    logits, noise = rows(n, vocab, type, seed=vocab + likely + 1, likely=likely)
+    settings = [MIXED[i % len(MIXED)] for i in range(n)]
+    check(cuda_lib, logits, noise, picked=range(24), **dict(zip(("temperature", "top_k", "top_p", "min_p"), map(list, zip(*settings)))))
+
+
+@pytest.mark.parametrize("type,vocab", BATCHES)
+@pytest.mark.parametrize("values", [1, 2, 5])
+def test_ties_in_batches(cuda_lib, type, vocab, values):
+    torch = __import__("torch")
+    n = 64
+    x, noise = rows(n, vocab, seed=vocab + values)
+    x = (x * 10).long().remainder(values).to(getattr(torch, type)) * 0.25
+    top_k, top_p = [0, 700, 100, 1, 0, 2500, 0, 3] * 8, [0.3, 1.0, 0.5, 1.0, 0.9, 0.5, 1.0, 1.0] * 8
+    check(cuda_lib, x, noise, picked=range(8), top_k=top_k, top_p=top_p)
+    check(cuda_lib, x, torch.ones_like(noise), picked=range(8, 16), top_k=top_k, top_p=top_p)
+    check(cuda_lib, x * -400, noise, picked=range(8), temperature=[3.0] * n, top_k=top_k, top_p=top_p)
+
+
+@pytest.mark.parametrize("type,vocab", BATCHES)
+def test_masks_and_values_that_are_not_finite_in_batches(cuda_lib, type, vocab):
+    torch = __import__("torch")
+    inf, n = float("inf"), 64
+    low = torch.finfo(getattr(torch, type)).min
+    x, noise = rows(n, vocab, type, seed=4, likely=3)
+    x[0] = -inf
+    x[1, 5:] = -inf
+    x[2, : vocab - 1] = -inf
+    x[3, ::2] = float("nan")
+    x[4, 7] = x[4, 2000] = inf
+    x[5] = low
+    x[6, 100:] = low
+    x[7, ::3] = -inf
+    x[8, 9000:] = -inf  # whole parts that are masked
+    x[9, : vocab - 9000] = -inf
+    for settings in (dict(), dict(top_p=0.8), dict(top_k=30), dict(top_k=2000, top_p=0.7), dict(min_p=0.02), dict(temperature=0.0),
+                     dict(temperature=1e30, top_p=0.5)):
+        tokens = check(cuda_lib, x, noise, picked=range(10), **{name: [v] * n for name, v in settings.items()})
+        assert tokens[0] == 0 and tokens[2] == vocab - 1
+
+
+@pytest.mark.parametrize("type,vocab", BATCHES)
+def test_cuts_beside_a_step_in_batches(cuda_lib, type, vocab):
+    """Values on two levels, each with half of the weight but for some 2^-22 (float32) or what the type rounds it to."""
+    torch = __import__("torch")
+    n, few = 64, vocab // 50
+    x = torch.zeros(n, vocab, device="cuda")
+    for i, off in enumerate((0.0, 2.0 ** -22, -2.0 ** -22, 2.0 ** -21, -2.0 ** -21, 1e-3)):
+        x[i, :few] = float(np.log((vocab - few) / few * (1 + off)))
+    noise = rows(n, vocab, seed=31)[1]
+    check(cuda_lib, x.to(getattr(torch, type)), noise, picked=range(7), top_p=[0.5] * n)
+
+
+@pytest.mark.parametrize("type,vocab", BATCHES)
+def test_quotients_alike_in_batches(cuda_lib, type, vocab):
+    torch = __import__("torch")
+    n = 64
+    x, _ = rows(n, vocab, type, seed=7, spread=1.0)
+    noise = torch.exp(x.double() - x.max(1, keepdim=True).values.double()).float()
+    check(cuda_lib, x, noise, picked=range(3))
+    check(cuda_lib, x, noise, picked=range(3), top_p=[0.7] * n)
+    check(cuda_lib, x, noise, picked=range(3), top_k=[25] * n)
