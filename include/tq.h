@@ -640,7 +640,8 @@ tq_status tq_kv_attend(const tq_kv_cache* cache, int layer, const int32_t* slots
  * the order of places.  Arguments, workspace (tq_kv_attend_workspace), arithmetic
  * and what becomes of empty, padded and invalid entries as there, but every query of
  * sequence i sees every token of slots[i], whatever the number of queries, and there
- * is no window.  A slot may be named by several sequences.
+ * is no window.  A slot may be named by several sequences, n of them up to the cache's
+ * slots as there; the queries of one slot may as well be one sequence's.
  */
 tq_status tq_kv_cross(const tq_kv_cache* cache, int layer, const int32_t* slots,
                       const int32_t* starts, int64_t n, const void* q, int type,
@@ -674,12 +675,15 @@ tq_status tq_kv_share(const tq_kv_cache* cache, const int32_t* slots,
  *            steps of the same requests
  *   groups   in [1, n]: how many groups and single requests the plan has; it decides
  *            which kernel takes the shared tokens, and costs time alone where it is wrong
+ *            (256 requests of one group over 60,001 tokens: 390 us with 1, 2,050 with 256;
+ *            8 of one group over 1,500: 49 and 37)
  *   workspace  device, 16-byte aligned, of ws_bytes >= tq_kv_attend_shared_workspace
  *            (enough for every smaller call too)
  * The other arguments as for tq_kv_attend.  An entry with tokens <= 0 or members <= 1
  * shares nothing.  One that does not fit (tokens < 0; another request of its group
  * that names another group; shared tokens that the request or the group's first does
- * not hold before its new ones) is attended by itself (status).
+ * not hold before its new ones; queries outside of its group's) is attended by itself
+ * (status).
  */
 tq_status tq_kv_attend_shared_workspace(const tq_kv_cache* cache, int64_t n,
                                         int64_t total, int heads, size_t* bytes);

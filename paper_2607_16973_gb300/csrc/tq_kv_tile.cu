@@ -37,8 +37,8 @@
 // M128 N128 K16, ~100 each) and per row tile 620 for the maxima and 1,400 for the
 // weights.  (Weighing in one pass with the old reference and again where it has to
 // move was slower: 448 us against 418 for two prompts, for want of registers.)
-// A prompt of 2,048 tokens and the last 2,046 of 6,000 (201 GFLOP): 320 us, 628
-// TFLOP/s, 0.33 of the measured rate.  Up to 128 rows the converters bound it: 255 MB of codes in
+// A prompt of 2,048 tokens and the last 2,046 of 6,000 (201 GFLOP): 307 us, 655
+// TFLOP/s, 0.34 of the measured rate.  Up to 128 rows the converters bound it: 255 MB of codes in
 // 154 us.
 #include <algorithm>
 #include <cstddef>

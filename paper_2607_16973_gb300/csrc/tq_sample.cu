@@ -19,14 +19,14 @@
 //
 // Three forms.  Rows of up to 256 pieces of 16 bytes, and rows beyond 256 parts, by a block
 // that reads them again for every step (whole_row).  Rows of up to 8 pieces for each of
-// 1,024 threads by a block that holds them in registers (k_sample_one).  Longer ones in
-// parts, by four kernels.
+// 1,024 threads by a block that holds them in registers (k_sample_one; with 8 pieces 100
+// to 116 bytes a thread spill).  Longer ones in parts, by four kernels.
 //
 // Bound: HBM for the parts' first reading; the rest is the chain of a row's steps and, for
 // code that runs once a launch, its fetching.  256 rows of 128,000 bf16 logits with settings
 // of all kinds (65.5 MB, and 16 to 20 MB of noise): 106 us on a GB300, of which the first
-// reading 31, the cuts 12, the race 51, the lists 20.  48 rows of 100,003 float32, flat, top-p
-// 0.9: 56 us (14, 11, 24, 14).  One row of 32,000: 18 us, 22 a call.  (A block per row
+// reading 32, the cuts 12, the race 53, the lists 21.  48 rows of 100,003 float32, flat, top-p
+// 0.9: 57 us (14, 12, 26, 14).  One row of 32,000: 18 us, 20 to 24 a call.  (A block per row
 // throughout: 236, 138 and 25 us; the settling steps in the last block of each kernel
 // instead of kernels of their own: 225 and 81.)
 #include <algorithm>
