@@ -429,10 +429,11 @@ def sample_tokens(logits, noise, temperature=None, top_k=None, top_p=None, min_p
         logprobs = _empty(n, f32, dev, stream)
     if workspace is None:
         workspace = _empty(_sample_need(n, vocab), torch.uint8, dev, stream)
-    check(load().tq_sample(logits.data_ptr(), types[logits.dtype], logits.stride(0), noise.data_ptr(), noise.stride(0),
-                           n, vocab, *settings, ptr(tokens, "tokens", i32), ptr(logprobs, "logprobs", f32),
-                           _dev_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size(),
-                           _stream(stream)))
+    # (one row has no next one: a view of it may say any stride)
+    step, noise_step = (logits.stride(0), noise.stride(0)) if n > 1 else (vocab, vocab)
+    check(load().tq_sample(logits.data_ptr(), types[logits.dtype], step, noise.data_ptr(), noise_step, n, vocab,
+                           *settings, ptr(tokens, "tokens", i32), ptr(logprobs, "logprobs", f32), _dev_ptr(workspace, "workspace"),
+                           workspace.numel() * workspace.element_size(), _stream(stream)))
     return (tokens, logprobs) if return_logprobs else tokens
 
 
