@@ -292,13 +292,13 @@ __device__ uint64_t find_cut(const Source& row, const Weigh& weigh, uint64_t kep
       if (!BY_COUNT) more[i] = 0;
     }
     __syncthreads();
-    int held = 0;  // a thread's tokens in a row that share a bin go there together
+    int held = 0;  // weights of a thread's tokens in a row that share a bin go there together
     uint64_t some = 0;
     auto put = [&] {
       if (some == 0) return;
       const uint32_t part = (uint32_t)some, old = atomicAdd(&sh.bins[held], part);
       const uint32_t up = (uint32_t)(some >> 32) + (old + part < old);
-      if (!BY_COUNT && up) atomicAdd(&more[held], up);
+      if (up) atomicAdd(&more[held], up);
       some = 0;
     };
     for (int g = threadIdx.x; g < row.pieces(); g += N) {
@@ -308,9 +308,13 @@ __device__ uint64_t find_cut(const Source& row, const Weigh& weigh, uint64_t kep
       for (int i = 0; i < E; ++i)
         if (x[i] >= low && x[i] <= high && place_of(x[i], v + i) >= kept) {
           const int b = bin_of(x[i]);
+          if (BY_COUNT) {
+            atomicAdd(&sh.bins[b], 1u);
+            continue;
+          }
           if (b != held) put();
           held = b;
-          some += BY_COUNT ? 1 : fixed(weigh(x[i]));
+          some += fixed(weigh(x[i]));
         }
     }
     put();
