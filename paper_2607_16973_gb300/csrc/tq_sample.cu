@@ -26,7 +26,7 @@
 // code that runs once a launch, its fetching.  256 rows of 128,000 bf16 logits with settings
 // of all kinds (65.5 MB, and 16 to 20 MB of noise): 106 us on a GB300, of which the first
 // reading 32, the cuts 12, the race 53, the lists 21.  48 rows of 100,003 float32, flat, top-p
-// 0.9: 57 us (14, 12, 26, 14).  One row of 32,000: 18 us, 20 to 24 a call.  (A block per row
+// 0.9: 55 us (14, 12, 26, 14 one by one).  One row of 32,000: 18 us, 20 to 24 a call.  (A block per row
 // throughout: 236, 138 and 25 us; the settling steps in the last block of each kernel
 // instead of kernels of their own: 225 and 81.)
 #include <algorithm>
@@ -1626,6 +1626,13 @@ cudaError_t one_block(const SampleArgs& a, int64_t n, cudaStream_t s) {
   return cudaGetLastError();
 }
 
+// Shared memory that k_sample_finish asks for and does not use: two of its blocks to an SM.  They
+// start where k_sample_race's blocks end, three to an SM where they may, and then a row that is
+// left to whole_row waits for its neighbours: 64 rows of 128,000 bf16 with top-k 1,000 took 348
+// us, 286 this way, 48 flat float32 rows 55.8 and 54.8; one to an SM: 256 and 53.3, but 256 rows
+// of all settings 106.2 instead of 104.6.
+constexpr size_t SPREAD = 80 * 1024;
+
 template <typename T>
 cudaError_t sample(const SampleArgs& a, int64_t n, void* workspace, cudaStream_t s) {
   constexpr int E = Row<T>::E;
@@ -1655,6 +1662,8 @@ cudaError_t sample(const SampleArgs& a, int64_t n, void* workspace, cudaStream_t
   q.steps = reinterpret_cast<uint32_t*>(p), p += z.steps;
   q.list = reinterpret_cast<uint64_t*>(p);
   const int jp = few ? 2 : 8;
+  const cudaError_t spread = set_max_dynamic_smem(reinterpret_cast<const void*>(k_sample_finish<T>), SPREAD);
+  if (spread != cudaSuccess) return spread;
   for (q.row0 = 0; q.row0 < n; q.row0 += rows) {
     const dim3 grid((unsigned)parts, (unsigned)std::min(rows, n - q.row0)), per_row(grid.y), block(SPLIT);
     (few ? k_sample_parts<T, 2> : k_sample_parts<T, 8>)<<<grid, block, 0, s>>>(q);
@@ -1662,7 +1671,7 @@ cudaError_t sample(const SampleArgs& a, int64_t n, void* workspace, cudaStream_t
     if (e == cudaSuccess)
       e = launch_maybe_pdl(true, k_sample_cut, per_row, block, 0, s, q, SPLIT * jp * E / GROUP, unit_of(SPLIT * jp * E));
     if (e == cudaSuccess) e = launch_maybe_pdl(true, few ? k_sample_race<T, 2> : k_sample_race<T, 8>, grid, block, 0, s, q);
-    if (e == cudaSuccess) e = launch_maybe_pdl(true, k_sample_finish<T>, per_row, block, 0, s, q);
+    if (e == cudaSuccess) e = launch_maybe_pdl(true, k_sample_finish<T>, per_row, block, SPREAD, s, q);
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;
